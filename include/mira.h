@@ -343,6 +343,148 @@ int mira_predict_mixture(const mira_mixture_shape* p, const mira_mixture_weights
                          int32_t n_tokens, float* probs, float* alpha, void* workspace,
                          uint64_t workspace_bytes, hipStream_t stream);
 
+/* ---- balance loss of a router ---------------------------------------------
+ * The auxiliary loss that a router is tuned with, its per-expert counts and
+ * its gradient, from what mira_moe_route / mira_moe_forward write.  Rows are
+ * grouped (a group is a sequence, or the whole batch): group g holds rows
+ * [offsets[g], offsets[g+1]).  With n_g its rows that the mask keeps,
+ *   p_te = softmax(logits_t)_e,
+ *   counts[g][e]    = pairs (t, j) of kept rows with topk_idx[t][j] = e,
+ *   mean_prob[g][e] = (1/n_g) sum over kept rows of p_te,
+ *   f_ge            = E counts[g][e] / (k n_g),
+ *   loss[g]         = coef sum_e f_ge mean_prob[g][e]   (coef where balanced),
+ *   dlogits[t][e]   = grad_loss[g] (coef / n_g) p_te (f_ge - sum_j f_gj p_tj),
+ * the gradient of sum_g grad_loss[g] loss[g] with the counts held constant.
+ * A group without kept rows has loss, counts and mean_prob 0.  A row that the
+ * mask drops has gradient 0 whatever its logits; rows of no group keep their
+ * dlogits bytes.  Logits of -inf have probability and gradient 0 (a row of
+ * nothing else as well); a NaN or +inf logit makes its row's probabilities
+ * NaN.  Entries of topk_idx outside 0..E-1 are not counted.  All arithmetic is
+ * fp32; sums are taken in a fixed order, so repeated calls give the same bits.
+ * Offsets that are not ascending or leave 0..n_tokens are clamped: such a call
+ * stays in its buffers, its results are unspecified. */
+typedef struct mira_balance_args {
+  const void* logits;      /* [T][E] logits_dtype; with logits_dtype MIRA_F32 the logits
+                              output of mira_moe_forward */
+  const int32_t* topk_idx; /* [T][k] */
+  const int32_t* offsets;  /* [n_groups+1], ascending, or NULL: one group of all rows */
+  const uint8_t* mask;     /* [T]: 0 drops a row (padding), or NULL: all rows kept */
+  const float* grad_loss;  /* [n_groups] gradient arriving at loss, or NULL: 1 */
+  int32_t logits_dtype;    /* mira_dtype of logits and dlogits */
+  int32_t n_tokens;        /* T >= 0 */
+  int32_t n_experts;       /* E: 1..MIRA_MAX_EXPERTS */
+  int32_t top_k;           /* k: 1..MIRA_MAX_TOPK */
+  int32_t n_groups;        /* G >= 1; 1 with offsets NULL */
+  float coef;              /* finite */
+  uint64_t ld_logits;      /* elements between rows of logits, >= E; 0 = E */
+  uint64_t ld_dlogits;     /* elements between rows of dlogits, >= E; 0 = E */
+  int32_t* counts;         /* optional [G][E] */
+  float* mean_prob;        /* optional [G][E] */
+  float* loss;             /* optional [G] */
+  void* dlogits;           /* optional [T][E] logits_dtype; may be logits itself (same ld) */
+  void* workspace;         /* mira_balance_workspace_bytes bytes, 256-byte aligned */
+  uint64_t workspace_bytes;
+} mira_balance_args;
+
+/* Bytes of workspace for calls with up to max_tokens tokens and max_groups
+ * groups.  Returns 0 for a negative max_tokens, max_groups < 1 or n_experts
+ * outside 1..MIRA_MAX_EXPERTS. */
+size_t mira_balance_workspace_bytes(int32_t max_tokens, int32_t n_experts, int32_t max_groups);
+
+/* The loss, its counts and its gradient in one call: any of the four outputs
+ * may be NULL, so a program takes loss and gradient together (the logits are
+ * read once) or the gradient in a later call, when grad_loss is known.  Only
+ * launches kernels (a HIP graph may capture it). */
+int mira_balance_loss(const mira_balance_args* a, hipStream_t stream);
+
+/* ---- 8-bit floating point with a scale for each block of 128 ---------------
+ * A matrix [rows][cols] held in e4m3 (OCP: 4 exponent and 3 mantissa bits,
+ * largest value 448, no infinities): one byte per value, row-major, and one
+ * fp32 scale per block of 1 row x 128 columns (activations) or 128 rows x 128
+ * columns (weights); the value is scale * e4m3.  Blocks at the right and lower
+ * edge may be shorter.  The bytes of a row from cols up to the next multiple of
+ * 16 are zero, and rows start 16-byte aligned: this is what mira_fp8_quantize
+ * writes and mira_fp8_gemm reads. */
+#define MIRA_FP8_BLOCK 128
+
+/* mira_fp8_quant_args.flags: x holds gate and up side by side, [rows][2 cols],
+ * and silu(gate) * up is quantized (between the two expert products). */
+#define MIRA_FP8_SWIGLU 0x1u
+
+typedef struct mira_fp8_quant_args {
+  const void* x;      /* [rows][cols] (MIRA_FP8_SWIGLU: [rows][2 cols]) x_dtype */
+  int32_t x_dtype;    /* mira_dtype */
+  int32_t rows;       /* >= 0 */
+  int32_t cols;       /* >= 1 */
+  int32_t block_rows; /* 1 or 128 */
+  float eps;          /* smallest block maximum: 1e-30..1e30, e.g. 1e-8 */
+  uint32_t flags;     /* MIRA_FP8_SWIGLU (block_rows 1) or 0 */
+  uint64_t ldx;       /* elements between rows of x; 0 = dense */
+  void* q;            /* [rows][ldq] e4m3 bytes, 16-byte aligned */
+  uint64_t ldq;       /* bytes between rows of q: a multiple of 16; 0 = cols rounded up to one */
+  float* scale;       /* [ceil(rows/block_rows)][ceil(cols/128)] */
+  uint64_t ld_scale;  /* floats between rows of scale; 0 = dense */
+  void* qt;           /* block_rows 128: optional transposed copy [cols][ldqt], 16-byte aligned */
+  uint64_t ldqt;      /* as ldq, 0 = rows rounded up to a multiple of 16 */
+  float* scale_t;     /* its scales [ceil(cols/128)][ceil(rows/128)]; with qt, and only with it */
+  uint64_t ld_scale_t; /* 0 = dense */
+} mira_fp8_quant_args;
+
+/* Quantize: per block, a = max(max |x|, eps), scale = fl32(a / 448),
+ * q = e4m3 of fl32(x * fl32(448 / a)), nearest, ties to even; both divisions
+ * correctly rounded.  Values are expected finite; a NaN becomes e4m3's NaN at
+ * its own place (it does not count for the maximum), an infinity gives its
+ * block an infinite scale, so the block holds NaN.  silu(g) = g / (1 + exp(-g)) in
+ * fp32.  The transposed copy holds the same bytes and scales, for products
+ * that contract over the weight's rows (the gradient dX = dY W of a product
+ * x W^T is the same product on the transposed copy). */
+int mira_fp8_quantize(const mira_fp8_quant_args* a, hipStream_t stream);
+
+/* out[i][j] = sum_b xs[r][b] ws[g][j/128][b] sum over k of block b of
+ *             x[r][k] w[g][j][k],
+ * for the rows i of group g, [offsets[g], offsets[g+1]), with r the source row
+ * of i.  One group of all m rows without offsets; with them, rows of no group
+ * keep their bytes.  Source rows: r = i, or, with pair_order as mira_moe_route
+ * writes it (expert_offsets are the offsets then), the token of pair p =
+ * pair_order[i]: p / top_k for p < x_rows * top_k, (p - x_rows * top_k) mod
+ * x_rows for shared pairs; a negative p gives a row of zeros.
+ * Each block's products are summed by the fp8 matrix cores, the blocks in
+ * fp32; out is rounded once.  Deterministic.  NaN operands give NaN. */
+typedef struct mira_fp8_gemm_args {
+  int32_t m;           /* rows of out, >= 0 */
+  int32_t n;           /* columns of out = rows of each w, >= 1 */
+  int32_t k;           /* contraction, >= 1 */
+  int32_t n_groups;    /* G: 1..MIRA_MAX_EXPERTS; 1 with offsets NULL */
+  int32_t out_dtype;   /* mira_dtype of out */
+  int32_t x_rows;      /* rows of x: >= m without pair_order, >= 1 with it */
+  int32_t top_k;       /* pairs per token; with pair_order 1..MIRA_MAX_TOPK, else 0 */
+  int32_t reserved;    /* must be 0 */
+  const void* x;       /* [x_rows][ldx] e4m3, 16-byte aligned */
+  uint64_t ldx;        /* a multiple of 16, >= k rounded up to one; 0 = that */
+  const float* x_scale; /* [x_rows][ceil(k/128)] */
+  uint64_t ld_xs;      /* 0 = dense */
+  const void* w;       /* G matrices [n][ldw] e4m3, 16-byte aligned */
+  uint64_t ldw;        /* as ldx */
+  uint64_t w_stride;   /* bytes between matrices, a multiple of 16; 0 = n * ldw */
+  const float* w_scale; /* G of [ceil(n/128)][ceil(k/128)] */
+  uint64_t ld_ws;      /* 0 = dense */
+  uint64_t ws_stride;  /* floats between matrices' scales; 0 = ceil(n/128) * ld_ws */
+  const int32_t* offsets;    /* [G+1] device, ascending; or NULL */
+  const int32_t* pair_order; /* [m] device, or NULL */
+  void* out;           /* [m][ldo] out_dtype */
+  uint64_t ldo;        /* elements, >= n; 0 = n */
+  void* workspace;     /* mira_fp8_gemm_workspace_bytes bytes, 256-byte aligned (NULL if 0) */
+  uint64_t workspace_bytes;
+} mira_fp8_gemm_args;
+
+/* Bytes of workspace of this call (its sizes, types and whether offsets is NULL
+ * count, other pointers are not looked at); 0 is possible.  SIZE_MAX for sizes
+ * that mira_fp8_gemm refuses. */
+size_t mira_fp8_gemm_workspace_bytes(const mira_fp8_gemm_args* a);
+
+/* Only launches kernels (a HIP graph may capture it). */
+int mira_fp8_gemm(const mira_fp8_gemm_args* a, hipStream_t stream);
+
 /* ---- expert staging (sections IV-C, IV-E, IV-F) ------------------------- */
 /* Copy one packed expert from pinned host memory into slot `slot` of a slot
  * pool with hipMemcpyAsync on copy_stream, then record `done` (if not NULL)

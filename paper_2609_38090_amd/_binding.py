@@ -20,6 +20,8 @@ MIRA_DECODE_MAX_TOKENS = 16
 MIRA_MAX_EXPERTS = 256
 MIRA_MAX_TOPK = 16
 MIRA_NOALLOC_SCRATCH_BYTES = 16 << 20
+MIRA_FP8_BLOCK = 128
+MIRA_FP8_SWIGLU = 0x1
 MIRA_VRAM_LARGE, MIRA_VRAM_SMALL = 0, 1
 MIRA_HEAD_NONE, MIRA_HEAD_MLP, MIRA_HEAD_MIXTURE, MIRA_HEAD_GIVEN = 0, 1, 2, 3
 MIRA_STACK_EVENTS = ("hot_hit", "stage_hit", "demand", "predicted", "prefetch", "prefetch_cached",
@@ -66,6 +68,35 @@ _MIX_PTRS = ("wah", "wal", "ba1", "wa2", "ba2", "whq", "whu", "bh1", "wh2", "bh2
 class _MixWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in _MIX_PTRS] + [("bg", ctypes.c_float),
                                                              ("reserved", ctypes.c_int32)]
+
+
+_I32, _U32, _U64, _F32, _VP = (ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float, ctypes.c_void_p)
+
+
+class _BalanceArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("logits", "topk_idx", "offsets", "mask", "grad_loss")] + \
+        [(n, _I32) for n in ("logits_dtype", "n_tokens", "n_experts", "top_k", "n_groups")] + \
+        [("coef", _F32), ("ld_logits", _U64), ("ld_dlogits", _U64)] + \
+        [(n, _VP) for n in ("counts", "mean_prob", "loss", "dlogits", "workspace")] + [("workspace_bytes", _U64)]
+
+
+class _Fp8QuantArgs(ctypes.Structure):
+    _fields_ = [("x", _VP), ("x_dtype", _I32), ("rows", _I32), ("cols", _I32), ("block_rows", _I32),
+                ("eps", _F32), ("flags", _U32), ("ldx", _U64), ("q", _VP), ("ldq", _U64), ("scale", _VP),
+                ("ld_scale", _U64), ("qt", _VP), ("ldqt", _U64), ("scale_t", _VP), ("ld_scale_t", _U64)]
+
+
+class _Fp8GemmArgs(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("m", "n", "k", "n_groups", "out_dtype", "x_rows", "top_k", "reserved")] + \
+        [("x", _VP), ("ldx", _U64), ("x_scale", _VP), ("ld_xs", _U64), ("w", _VP), ("ldw", _U64),
+         ("w_stride", _U64), ("w_scale", _VP), ("ld_ws", _U64), ("ws_stride", _U64), ("offsets", _VP),
+         ("pair_order", _VP), ("out", _VP), ("ldo", _U64), ("workspace", _VP), ("workspace_bytes", _U64)]
+
+
+def _fill(struct, args):
+    """The C structure of an argument dataclass whose fields have its names."""
+    return struct(**{n: _ptr(getattr(args, n)) if t is _VP else getattr(args, n)
+                     for n, t in struct._fields_ if n != "reserved"})
 
 
 @dataclass
@@ -168,6 +199,88 @@ class MoEArgs:
         return _Args(**vals)
 
 
+@dataclass
+class BalanceArgs:
+    """mira_balance_args.  Pointer fields take torch tensors, integer addresses or None."""
+    logits: Any = None
+    topk_idx: Any = None
+    offsets: Any = None
+    mask: Any = None
+    grad_loss: Any = None
+    logits_dtype: int = MIRA_F32
+    n_tokens: int = 0
+    n_experts: int = 0
+    top_k: int = 0
+    n_groups: int = 1
+    coef: float = 1.0
+    ld_logits: int = 0
+    ld_dlogits: int = 0
+    counts: Any = None
+    mean_prob: Any = None
+    loss: Any = None
+    dlogits: Any = None
+    workspace: Any = None
+    workspace_bytes: int = 0
+
+    def _c(self) -> _BalanceArgs:
+        return _fill(_BalanceArgs, self)
+
+
+@dataclass
+class Fp8QuantArgs:
+    """mira_fp8_quant_args.  Pointer fields take torch tensors, integer addresses or None."""
+    x: Any = None
+    x_dtype: int = MIRA_BF16
+    rows: int = 0
+    cols: int = 0
+    block_rows: int = 1
+    eps: float = 1e-8
+    flags: int = 0
+    ldx: int = 0
+    q: Any = None
+    ldq: int = 0
+    scale: Any = None
+    ld_scale: int = 0
+    qt: Any = None
+    ldqt: int = 0
+    scale_t: Any = None
+    ld_scale_t: int = 0
+
+    def _c(self) -> _Fp8QuantArgs:
+        return _fill(_Fp8QuantArgs, self)
+
+
+@dataclass
+class Fp8GemmArgs:
+    """mira_fp8_gemm_args.  Pointer fields take torch tensors, integer addresses or None."""
+    m: int = 0
+    n: int = 0
+    k: int = 0
+    n_groups: int = 1
+    out_dtype: int = MIRA_BF16
+    x_rows: int = 0
+    top_k: int = 0
+    x: Any = None
+    ldx: int = 0
+    x_scale: Any = None
+    ld_xs: int = 0
+    w: Any = None
+    ldw: int = 0
+    w_stride: int = 0
+    w_scale: Any = None
+    ld_ws: int = 0
+    ws_stride: int = 0
+    offsets: Any = None
+    pair_order: Any = None
+    out: Any = None
+    ldo: int = 0
+    workspace: Any = None
+    workspace_bytes: int = 0
+
+    def _c(self) -> _Fp8GemmArgs:
+        return _fill(_Fp8GemmArgs, self)
+
+
 def _ptr(v) -> Optional[int]:
     if v is None:
         return None
@@ -257,6 +370,11 @@ def load():
             "mira_mixture_workspace_bytes": (sz, [ctypes.POINTER(_MixShape), i32]),
             "mira_predict_mixture": (ctypes.c_int, [ctypes.POINTER(_MixShape), ctypes.POINTER(_MixWeights),
                                                     vp, vp, vp, i32, vp, vp, vp, u64, vp]),
+            "mira_balance_workspace_bytes": (sz, [i32, i32, i32]),
+            "mira_balance_loss": (ctypes.c_int, [ctypes.POINTER(_BalanceArgs), vp]),
+            "mira_fp8_quantize": (ctypes.c_int, [ctypes.POINTER(_Fp8QuantArgs), vp]),
+            "mira_fp8_gemm_workspace_bytes": (sz, [ctypes.POINTER(_Fp8GemmArgs)]),
+            "mira_fp8_gemm": (ctypes.c_int, [ctypes.POINTER(_Fp8GemmArgs), vp]),
             "mira_stage_expert": (ctypes.c_int, [vp, u64, i32, vp, u64, vp, vp]),
             "mira_set_slot": (ctypes.c_int, [vp, i32, i32, vp]),
             "mira_stack_create": (ctypes.c_int, [ctypes.POINTER(_StackConfig), ctypes.POINTER(_Shape), vp, vp, vp,
@@ -364,6 +482,32 @@ def mira_predict_mixture(mshape: MixtureShape, weights: MixtureWeights, x, logit
     _check(load().mira_predict_mixture(ctypes.byref(mshape._c()), ctypes.byref(weights._c()), _ptr(x),
                                        _ptr(logits), _ptr(topk_idx), n_tokens, _ptr(probs), _ptr(alpha),
                                        _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mira_balance_workspace_bytes(max_tokens: int, n_experts: int, max_groups: int = 1) -> int:
+    n = int(load().mira_balance_workspace_bytes(max_tokens, n_experts, max_groups))
+    if n == 0:
+        raise MiraError(-2, "invalid sizes for mira_balance_workspace_bytes")
+    return n
+
+
+def mira_balance_loss(args: BalanceArgs, stream=None):
+    _check(load().mira_balance_loss(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_fp8_quantize(args: Fp8QuantArgs, stream=None):
+    _check(load().mira_fp8_quantize(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_fp8_gemm_workspace_bytes(args: Fp8GemmArgs) -> int:
+    n = int(load().mira_fp8_gemm_workspace_bytes(ctypes.byref(args._c())))
+    if n == ctypes.c_size_t(-1).value:
+        raise MiraError(-2, mira_last_error())
+    return n
+
+
+def mira_fp8_gemm(args: Fp8GemmArgs, stream=None):
+    _check(load().mira_fp8_gemm(ctypes.byref(args._c()), _stream(stream)))
 
 
 def mira_stage_expert(slot_pool, slot_stride: int, slot: int, pinned_src, nbytes: int,

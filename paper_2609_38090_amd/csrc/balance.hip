@@ -1,0 +1,465 @@
+// Balance loss of a router, its per-expert counts and its gradient.
+//
+//   loss_g = coef * sum_e f_ge P_ge,  f_ge = E c_ge / (k n_g),  P_ge = mean of p_te,
+//   d/dlogit_te = grad_g * (coef / n_g) * p_te * (f_ge - sum_j f_gj p_tj),
+// with c the counts of the selected experts and p the row softmax.  The
+// gradient needs the counts of the whole group but not P, so the counts (which
+// read the small topk_idx only) come first and one pass over the logits then
+// gives both the gradient and the sums of p: the logits are read once and the
+// gradient written once.
+//
+// Rows are split into at most kMaxChunks chunks, a workgroup each; a chunk
+// walks the groups that it meets.  Over the chunks in order, (chunk, group)
+// pairs that meet only ever step one of the two up, so chunk + group numbers
+// the partial sums without gaps to search: kMaxChunks + G slots hold any
+// layout of groups, and the finishing kernel adds a group's slots in order.
+// Calls of few logits run one workgroup per group in a single launch.
+#include "device_util.h"
+#include "mira_internal.h"
+
+namespace mira {
+
+namespace {
+
+constexpr int kMaxChunks = 256;   // one 1024-thread workgroup per CU
+constexpr int kBigThreads = 1024;
+constexpr int kSmallThreads = 256;
+
+struct BalanceParams {
+  const void* logits;
+  const int32_t* idx;
+  const int32_t* offsets;  // may be null
+  const uint8_t* mask;     // may be null
+  const float* grad_loss;  // may be null
+  void* dlogits;           // may be null
+  int32_t* counts;         // output or workspace
+  int32_t* kept;           // [G] rows kept (with a mask)
+  float* mean;             // may be null
+  float* loss;             // may be null
+  float* partial;          // [chunks + G][E]
+  size_t ld_x, ld_d;
+  int T, E, k, G, chunk_rows;
+  float coef;
+};
+
+// Reductions over groups of L = 1, 2, .. 64 consecutive lanes.  After each step all
+// lanes of the smaller group agree, so mirrors serve as exchanges.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+struct MaxOp {
+  __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+struct AddOp {
+  __device__ __forceinline__ static float of(float a, float b) { return a + b; }
+};
+template <int L, typename Op>
+__device__ __forceinline__ float lanes_reduce(float v) {
+  if constexpr (L >= 2) v = Op::of(v, dpp<0xB1>(v));    // quad_perm 1,0,3,2
+  if constexpr (L >= 4) v = Op::of(v, dpp<0x4E>(v));    // quad_perm 2,3,0,1
+  if constexpr (L >= 8) v = Op::of(v, dpp<0x141>(v));   // mirror in 8
+  if constexpr (L >= 16) v = Op::of(v, dpp<0x140>(v));  // mirror in 16
+  if constexpr (L >= 32) v = Op::of(v, __shfl_xor(v, 16, 64));
+  if constexpr (L >= 64) v = Op::of(v, __shfl_xor(v, 32, 64));
+  return v;
+}
+
+// exp(x) for x <= 0 with the product x log2(e) carried to two parts, so that
+// its rounding does not grow with |x| (2 ulp; exp(-inf) = 0, NaN stays).
+__device__ __forceinline__ float exp_neg(float x) {
+  x = x < -200.f ? -200.f : x;
+  const float log2e = 1.44269502162933349609375f, rest = 1.92596299112661746887e-8f;
+  const float t = x * log2e;
+  const float r = fmaf(x, rest, fmaf(x, log2e, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, r * 0.693147182464599609375f, e);
+}
+
+// The four logits of a row that a lane holds: VEC: 4l .. 4l+3 (E a multiple of
+// 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.
+template <int L, bool VEC>
+__device__ __forceinline__ int expert_of(int l, int i) {
+  return VEC ? 4 * l + i : l + L * i;
+}
+template <int L, bool VEC, typename T>
+__device__ __forceinline__ void load_row(const T* row, int l, int E, float v[4]) {
+  if constexpr (VEC) {
+    if (4 * l < E) {
+      load4_act(row + 4 * l, v);
+    } else {
+      v[0] = v[1] = v[2] = v[3] = -INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = l + L * i;
+      v[i] = e < E ? load_act(row, e) : -INFINITY;
+    }
+  }
+}
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+// (a NaN keeps its upper half: the rounding increment must not carry it into infinity or zero)
+__device__ __forceinline__ uint16_t to_bf16(float v) {
+  return v != v ? (uint16_t)((__float_as_uint(v) >> 16) | 0x40u) : f32_to_bf16_rne(v);
+}
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = to_bf16(v); }
+__device__ __forceinline__ void store4(float* p, const float v[4]) { *(v4f*)p = v4f{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store4(uint16_t* p, const float v[4]) {
+  *(uint2*)p = uint2{(uint32_t)to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16,
+                     (uint32_t)to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16};
+}
+template <int L, bool VEC, typename T>
+__device__ __forceinline__ void store_row(T* row, int l, int E, const float v[4]) {
+  if constexpr (VEC) {
+    if (4 * l < E) store4(row + 4 * l, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = l + L * i;
+      if (e < E) store1(row + e, v[i]);
+    }
+  }
+}
+
+// Group bounds, clamped so that any offsets stay inside the buffers.
+struct Segment {
+  int lo, hi;
+};
+__device__ __forceinline__ Segment group_rows(const BalanceParams& q, int g) {
+  if (!q.offsets) return Segment{0, q.T};
+  const int lo = min(max(q.offsets[g], 0), q.T);
+  return Segment{lo, min(max(q.offsets[g + 1], lo), q.T)};
+}
+// Last group g with offsets[g] <= row (the group that holds it if any does); -1 if none.
+__device__ __forceinline__ int group_of(const BalanceParams& q, int row) {
+  if (!q.offsets) return 0;
+  int lo = 0, hi = q.G + 1;  // first index with offsets[i] > row
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (q.offsets[mid] > row) hi = mid; else lo = mid + 1;
+  }
+  return lo - 1;
+}
+
+// Softmax, gradient and sums of p of rows lo, lo + step, .. < hi for one lane
+// group of L lanes (lane l of it); acc holds the lane's sums of p.  U rows are
+// in flight at once.
+template <int L, bool VEC, int U, typename T>
+__device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi, int step, int l,
+                                          const float f[4], float gscale, float acc[4]) {
+  const T* x = (const T*)q.logits;
+  T* d = (T*)q.dlogits;
+  for (int r0 = lo; r0 < hi; r0 += U * step) {
+    float v[U][4];
+    bool keep[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * step;
+      keep[u] = r < hi;
+      if (r < hi) {
+        load_row<L, VEC>(x + (size_t)r * q.ld_x, l, q.E, v[u]);
+        if (q.mask) keep[u] = q.mask[r] != 0;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * step;
+      if (r >= hi) break;
+      float m = lanes_reduce<L, MaxOp>(fmaxf(fmaxf(v[u][0], v[u][1]), fmaxf(v[u][2], v[u][3])));
+      m = m == -INFINITY ? 0.f : m;
+      float s = 0.f, w = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[u][i] = exp_neg(v[u][i] - m);
+        s += v[u][i];
+        w = fmaf(f[i], v[u][i], w);
+      }
+      s = lanes_reduce<L, AddOp>(s);
+      w = lanes_reduce<L, AddOp>(w);
+      const float inv = s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
+      w *= inv;
+      float o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = v[u][i] * inv;
+        acc[i] += keep[u] ? p : 0.f;
+        o[i] = keep[u] ? gscale * p * (f[i] - w) : 0.f;
+      }
+      if (d) store_row<L, VEC>(d + (size_t)r * q.ld_d, l, q.E, o);
+    }
+  }
+}
+
+// Sum over the lane groups of the workgroup: sums[e] for e < E, in LDS.
+template <int L, bool VEC, int THREADS>
+__device__ __forceinline__ void reduce_groups(float acc[4], int E, float (*wave_sums)[MIRA_MAX_EXPERTS]) {
+  const int lane = threadIdx.x & 63, l = lane % L, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int o = L; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o, 64);
+    const int e = expert_of<L, VEC>(l, i);
+    if (lane < L && e < E) wave_sums[wave][e] = acc[i];
+  }
+}
+
+// Counts the pairs of rows [lo, hi) into hist and the kept rows into *kept
+// (both in LDS, zeroed before).
+template <int THREADS>
+__device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int hi, int* hist, int* kept) {
+  const uint32_t end = (uint32_t)hi * q.k;  // T * k is at most 2^30
+  for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += THREADS) {
+    const int e = q.idx[i];
+    if ((uint32_t)e < (uint32_t)q.E && (!q.mask || q.mask[i / q.k])) atomicAdd(hist + e, 1);
+  }
+  if (q.mask) {
+    int n = 0;
+    for (int r = lo + threadIdx.x; r < hi; r += THREADS) n += q.mask[r] != 0;
+    if (n) atomicAdd(kept, n);
+  }
+}
+
+__device__ __forceinline__ float count_scale(const BalanceParams& q, int n) {
+  return n > 0 ? (float)q.E / ((float)q.k * (float)n) : 0.f;
+}
+__device__ __forceinline__ float grad_scale(const BalanceParams& q, int g, int n) {
+  return n > 0 ? (q.grad_loss ? q.grad_loss[g] : 1.f) * q.coef / (float)n : 0.f;
+}
+
+// One workgroup per group: counts, rows, means and loss.
+template <int L, bool VEC, typename T>
+__global__ __launch_bounds__(kSmallThreads) void balance_group_kernel(BalanceParams q) {
+  __shared__ int hist[MIRA_MAX_EXPERTS];
+  __shared__ int kept;
+  __shared__ float wave_sums[kSmallThreads / 64][MIRA_MAX_EXPERTS];
+  __shared__ float part[kSmallThreads / 64];
+  const int g = blockIdx.x, t = threadIdx.x, l = t % L;
+  const Segment s = group_rows(q, g);
+  for (int e = t; e < q.E; e += kSmallThreads) hist[e] = 0;
+  if (t == 0) kept = 0;
+  __syncthreads();
+  count_pairs<kSmallThreads>(q, s.lo, s.hi, hist, &kept);
+  __syncthreads();
+  const int n = q.mask ? kept : s.hi - s.lo;
+  const float cs = count_scale(q, n);
+  float f[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = expert_of<L, VEC>(l, i);
+    f[i] = e < q.E ? (float)hist[e] * cs : 0.f;
+  }
+  rows_pass<L, VEC, 2, T>(q, s.lo + t / L, s.hi, kSmallThreads / L, l, f, grad_scale(q, g, n), acc);
+  reduce_groups<L, VEC, kSmallThreads>(acc, q.E, wave_sums);
+  __syncthreads();
+  float term = 0.f;
+  for (int e = t; e < q.E; e += kSmallThreads) {
+    float sum = 0.f;
+    for (int w = 0; w < kSmallThreads / 64; ++w) sum += wave_sums[w][e];
+    const float mean = n > 0 ? sum / (float)n : 0.f;
+    if (q.mean) q.mean[(size_t)g * q.E + e] = mean;
+    q.counts[(size_t)g * q.E + e] = hist[e];
+    term += (float)hist[e] * cs * mean;
+  }
+  term = wave_sum(term);
+  if ((t & 63) == 0) part[t >> 6] = term;
+  __syncthreads();
+  if (t == 0 && q.loss) {
+    float sum = 0.f;
+    for (int w = 0; w < kSmallThreads / 64; ++w) sum += part[w];
+    q.loss[g] = q.coef * sum;
+  }
+}
+
+// ---- many logits: zero, count, rows, finish ---------------------------------
+
+__global__ __launch_bounds__(256) void balance_zero_kernel(int32_t* counts, size_t n, int32_t* kept, int G) {
+  const size_t i0 = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
+  for (size_t i = i0; i < n; i += step) counts[i] = 0;
+  for (size_t i = i0; i < (size_t)G; i += step) kept[i] = 0;
+}
+
+// Walks the groups that rows [lo, hi) meet: f(g, first row, end row).
+template <typename F>
+__device__ __forceinline__ void for_groups(const BalanceParams& q, int lo, int hi, F&& f) {
+  int g = max(group_of(q, lo), 0);
+  while (g < q.G) {
+    const Segment s = group_rows(q, g);
+    if (s.lo >= hi) break;
+    const int a = max(s.lo, lo), b = min(s.hi, hi);
+    if (a < b) f(g, a, b);
+    if (s.hi >= hi) break;
+    // the next group that holds a row (empty ones are passed over); always upwards
+    g = max(g + 1, group_of(q, s.hi));
+  }
+}
+
+__global__ __launch_bounds__(kBigThreads) void balance_count_kernel(BalanceParams q) {
+  __shared__ int hist[MIRA_MAX_EXPERTS];
+  __shared__ int kept;
+  const int lo = blockIdx.x * q.chunk_rows, hi = min(lo + q.chunk_rows, q.T);
+  for_groups(q, lo, hi, [&](int g, int a, int b) {
+    for (int e = threadIdx.x; e < q.E; e += kBigThreads) hist[e] = 0;
+    if (threadIdx.x == 0) kept = 0;
+    __syncthreads();
+    count_pairs<kBigThreads>(q, a, b, hist, &kept);
+    __syncthreads();
+    // integers: the order of these additions does not change the result
+    for (int e = threadIdx.x; e < q.E; e += kBigThreads)
+      if (hist[e]) atomicAdd(q.counts + (size_t)g * q.E + e, hist[e]);
+    if (threadIdx.x == 0 && kept) atomicAdd(q.kept + g, kept);
+    __syncthreads();
+  });
+}
+
+template <int L, bool VEC, typename T>
+__global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams q) {
+  __shared__ float wave_sums[kBigThreads / 64][MIRA_MAX_EXPERTS];
+  const int t = threadIdx.x, l = t % L;
+  const int lo = blockIdx.x * q.chunk_rows, hi = min(lo + q.chunk_rows, q.T);
+  for_groups(q, lo, hi, [&](int g, int a, int b) {
+    const Segment s = group_rows(q, g);
+    const int n = q.mask ? q.kept[g] : s.hi - s.lo;
+    const float cs = count_scale(q, n);
+    float f[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = expert_of<L, VEC>(l, i);
+      f[i] = e < q.E ? (float)q.counts[(size_t)g * q.E + e] * cs : 0.f;
+    }
+    rows_pass<L, VEC, 4, T>(q, a + t / L, b, kBigThreads / L, l, f, grad_scale(q, g, n), acc);
+    reduce_groups<L, VEC, kBigThreads>(acc, q.E, wave_sums);
+    __syncthreads();
+    for (int e = t; e < q.E; e += kBigThreads) {
+      float sum = 0.f;
+      for (int w = 0; w < kBigThreads / 64; ++w) sum += wave_sums[w][e];
+      q.partial[(size_t)(blockIdx.x + g) * q.E + e] = sum;
+    }
+    __syncthreads();
+  });
+}
+
+// Means and loss of a group from its chunks' sums: thread (e, part) adds every
+// parts-th slot in order, then the parts are added in order.
+__global__ __launch_bounds__(kBigThreads) void balance_finish_kernel(BalanceParams q, int width) {
+  __shared__ float sums[kBigThreads];
+  __shared__ float part_loss[kBigThreads / 64];
+  const int g = blockIdx.x, t = threadIdx.x, e = t % width, part = t / width, parts = kBigThreads / width;
+  const Segment s = group_rows(q, g);
+  const int n = q.mask ? q.kept[g] : s.hi - s.lo;
+  float sum = 0.f;
+  if (e < q.E && s.lo < s.hi) {
+    const int c1 = (s.hi - 1) / q.chunk_rows;
+    for (int c = s.lo / q.chunk_rows + part; c <= c1; c += parts) sum += q.partial[(size_t)(c + g) * q.E + e];
+  }
+  sums[t] = sum;
+  __syncthreads();
+  float term = 0.f;
+  if (part == 0 && e < q.E) {
+    for (int i = 1; i < parts; ++i) sum += sums[i * width + e];
+    const float mean = n > 0 ? sum / (float)n : 0.f;
+    if (q.mean) q.mean[(size_t)g * q.E + e] = mean;
+    term = (float)q.counts[(size_t)g * q.E + e] * count_scale(q, n) * mean;
+  }
+  term = wave_sum(term);
+  if ((t & 63) == 0) part_loss[t >> 6] = term;
+  __syncthreads();
+  if (t == 0 && q.loss) {
+    float total = 0.f;
+    for (int w = 0; w < kBigThreads / 64; ++w) total += part_loss[w];
+    q.loss[g] = q.coef * total;
+  }
+}
+
+struct BalanceLayout {
+  size_t counts, kept, partial, total;
+};
+BalanceLayout balance_layout(int E, int G) {
+  BalanceLayout w;
+  w.counts = 0;
+  w.kept = align_up((size_t)G * E * 4, 256);
+  w.partial = w.kept + align_up((size_t)G * 4, 256);
+  w.total = w.partial + align_up((size_t)(kMaxChunks + G) * E * 4, 256);
+  return w;
+}
+
+template <int L, bool VEC, typename T>
+void launch_rows(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
+  if (small)
+    launch_timed("balance_group", balance_group_kernel<L, VEC, T>, dim3(q.G), dim3(kSmallThreads), 0, st, q);
+  else
+    launch_timed("balance_rows", balance_rows_kernel<L, VEC, T>, dim3(chunks), dim3(kBigThreads), 0, st, q);
+}
+
+template <bool VEC, typename T>
+void launch_lanes(const BalanceParams& q, int lanes, bool small, int chunks, hipStream_t st) {
+  switch (lanes) {
+    case 1: return launch_rows<1, VEC, T>(q, small, chunks, st);
+    case 2: return launch_rows<2, VEC, T>(q, small, chunks, st);
+    case 4: return launch_rows<4, VEC, T>(q, small, chunks, st);
+    case 8: return launch_rows<8, VEC, T>(q, small, chunks, st);
+    case 16: return launch_rows<16, VEC, T>(q, small, chunks, st);
+    case 32: return launch_rows<32, VEC, T>(q, small, chunks, st);
+    default: return launch_rows<64, VEC, T>(q, small, chunks, st);
+  }
+}
+
+}  // namespace
+
+size_t balance_ws_bytes(int E, int G) { return balance_layout(E, G).total; }
+
+hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
+  const BalanceLayout w = balance_layout(a.n_experts, a.n_groups);
+  char* ws = (char*)a.workspace;
+  BalanceParams q{};
+  q.logits = a.logits;
+  q.idx = a.topk_idx;
+  q.offsets = a.offsets;
+  q.mask = a.mask;
+  q.grad_loss = a.grad_loss;
+  q.dlogits = a.dlogits;
+  q.counts = a.counts ? a.counts : (int32_t*)(ws + w.counts);
+  q.kept = (int32_t*)(ws + w.kept);
+  q.mean = a.mean_prob;
+  q.loss = a.loss;
+  q.partial = (float*)(ws + w.partial);
+  q.ld_x = a.ld_logits ? a.ld_logits : a.n_experts;
+  q.ld_d = a.ld_dlogits ? a.ld_dlogits : a.n_experts;
+  q.T = a.n_tokens;
+  q.E = a.n_experts;
+  q.k = a.top_k;
+  q.G = a.n_groups;
+  q.coef = a.coef;
+  int lanes = 1;
+  while (lanes * 4 < q.E) lanes *= 2;
+  const size_t esz = a.logits_dtype == MIRA_F32 ? 4 : 2;
+  const bool vec = q.E % 4 == 0 && q.ld_x % 4 == 0 && (uintptr_t)q.logits % (4 * esz) == 0 &&
+                   (!q.dlogits || (q.ld_d % 4 == 0 && (uintptr_t)q.dlogits % (4 * esz) == 0));
+  const bool small = (size_t)q.T * q.E <= 32768;
+  int chunks = 0;
+  if (!small) {
+    // whole passes of the workgroup's lane groups, at most kMaxChunks chunks
+    const int rows = kBigThreads / lanes;
+    q.chunk_rows = (int)align_up((size_t)(q.T + kMaxChunks - 1) / kMaxChunks, rows);
+    chunks = (q.T + q.chunk_rows - 1) / q.chunk_rows;
+    const size_t n = (size_t)q.G * q.E;
+    const int zb = (int)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024);
+    launch_timed("balance_zero", balance_zero_kernel, dim3(zb), dim3(256), 0, st, q.counts, n, q.kept, q.G);
+    launch_timed("balance_count", balance_count_kernel, dim3(chunks), dim3(kBigThreads), 0, st, q);
+  }
+  if (a.logits_dtype == MIRA_F32) {
+    if (vec) launch_lanes<true, float>(q, lanes, small, chunks, st);
+    else launch_lanes<false, float>(q, lanes, small, chunks, st);
+  } else {
+    if (vec) launch_lanes<true, uint16_t>(q, lanes, small, chunks, st);
+    else launch_lanes<false, uint16_t>(q, lanes, small, chunks, st);
+  }
+  if (!small) {
+    int width = 1;
+    while (width < q.E) width *= 2;
+    launch_timed("balance_finish", balance_finish_kernel, dim3(q.G), dim3(kBigThreads), 0, st, q, width);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mira

@@ -265,6 +265,11 @@ size_t mixture_ws_bytes(int n_groups, const mira_mixture_shape& p);
 hipError_t launch_mixture(const mira_mixture_shape& p, const mira_mixture_weights& w,
                           const void* x, const float* logits, const int32_t* topk_idx, int T,
                           float* probs, float* alpha, void* ws, hipStream_t st);
+size_t balance_ws_bytes(int E, int G);
+hipError_t launch_balance(const mira_balance_args& a, hipStream_t st);
+hipError_t launch_fp8_quantize(const mira_fp8_quant_args& a, hipStream_t st);
+size_t fp8_gemm_ws_bytes(const mira_fp8_gemm_args& a);
+hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st);
 hipError_t launch_set_slot(int32_t* table, int expert, int slot, hipStream_t st);
 // Device address of the library's scratch array on the current device
 // (noalloc.hip), looked up on the first call per device.

@@ -128,6 +128,261 @@ __global__ __launch_bounds__(256) void fp8_gemm_rows_kernel(GemmParams p) {
   }
 }
 
+
+// ---- many rows: tiles through LDS ---------------------------------------------
+//
+// A workgroup of WN x WM waves owns BN weight rows by BM token rows; a wave owns
+// 16 NT x 16 MT of them, within one scale block of the weights.  Stages of one
+// block of the contraction (128 bytes of every row, and their scales) go to LDS
+// by direct loads, two stages in turn: the loads of the next one are in flight
+// while this one is multiplied.
+
+// One direct-to-LDS load of a wave: lane l's bytes go to LDS address m0 + 16 l
+// (or 4 l).  The compiler does not see these loads; every wait for them is the
+// explicit one at the stage's start.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16(const void* src, uint32_t m0) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const void* src, uint32_t m0) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+
+// All loads to LDS have landed and all LDS reads have returned, in every wave.
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The 16 x 16 sums of one block on the fp8 matrix cores.
+__device__ __forceinline__ v4f block_fp8(v8i a, v8i b) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+
+struct Tile {
+  int g, m0, m1, nt;  // group, rows [m0, m1), tile of weight rows
+};
+
+// Tiles are numbered so that the workgroups of one XCD (ids equal modulo 8) take
+// consecutive ones, and consecutive tiles run down kTileRun row tiles that share
+// their weights before the next weight rows.
+constexpr int kTileRun = 8;
+__device__ __forceinline__ bool tile_number(int mT, int nT, int& mt, int& nt) {
+  const int total = mT * nT, per = (total + 7) >> 3, i = blockIdx.x >> 3;
+  const int id = (blockIdx.x & 7) * per + i;
+  if (i >= per || id >= total) return false;
+  const int run = id / (kTileRun * nT), first = run * kTileRun, rows = min(mT - first, kTileRun);
+  const int at = id - first * nT;
+  nt = at / rows;
+  mt = first + at - nt * rows;
+  return true;
+}
+
+// The tile of this workgroup, from the groups' row counts; false if there is none.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shared, Tile& t) {
+  if (!p.offsets) {
+    int mt;
+    if (!tile_number((p.M + BM - 1) / BM, nT, mt, t.nt)) return false;
+    t.g = 0;
+    t.m0 = mt * BM;
+    t.m1 = min(t.m0 + BM, p.M);
+    return true;
+  }
+  if (threadIdx.x < 64) {  // one wave: lane l has groups 4l .. 4l+3
+    const int l = threadIdx.x;
+    Rows r[4];
+    int n[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[i] = 4 * l + i < p.G ? rows_of(p, 4 * l + i) : Rows{0, 0};
+      n[i] = (r[i].hi - r[i].lo + BM - 1) / BM;
+      sum += n[i];
+    }
+    int end = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(end, o, 64);
+      if (l >= o) end += v;
+    }
+    const int mT = __shfl(end, 63, 64);
+    int mt = 0, nt = 0;
+    const bool any = tile_number(mT, nT, mt, nt);
+    if (l == 0) shared[0] = any ? nt : -1;
+    int at = end - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (any && mt >= at && mt < at + n[i]) {
+        shared[1] = 4 * l + i;
+        shared[2] = r[i].lo + (mt - at) * BM;
+        shared[3] = r[i].hi;
+      }
+      at += n[i];
+    }
+  }
+  __syncthreads();
+  t.nt = shared[0];
+  t.g = shared[1];
+  t.m0 = shared[2];
+  t.m1 = min(shared[2] + BM, shared[3]);
+  return t.nt >= 0;
+}
+
+template <typename OutT>
+__device__ __forceinline__ void store_out4(OutT* p, v4f v, int n) {
+  if (n >= 4 && ((uintptr_t)p & (4 * sizeof(OutT) - 1)) == 0) {
+    if constexpr (sizeof(OutT) == 4) {
+      *(v4f*)p = v;
+    } else {
+      uint16_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) store_out(h + i, v[i]);
+      *(uint2*)p = uint2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) store_out(p + i, v[i]);
+  }
+}
+
+template <int NT, int MT, int WN, int WM, bool EXACT, typename OutT>
+__global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams p, int nT) {
+  constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM, W = WN * WM;
+  constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX + (BM + 64) * 4;
+  constexpr int GW = BN / 8 / W, GX = BM / 8 / W;  // loads of 8 rows per wave and stage
+  static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && BM % 64 == 0 && BM / 64 < W && 128 % (16 * NT) == 0, "tile shape");
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+  __shared__ int tile_s[4];
+  Tile t;
+  if (!find_tile<BM>(p, nT, tile_s, t)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, kg = lane >> 4, wn = wave % WN, wm = wave / WN;
+  const int n0 = t.nt * BN;
+  const uint8_t* w = p.w + (size_t)t.g * p.w_stride;
+  const float* ws = p.ws + (size_t)t.g * p.ws_stride;
+
+  // Row r stores its 16-byte chunk c at chunk c ^ ((r >> 1) & 7): a 128-bit read
+  // serves rows 0-3 and 12-15 of one k-group with rows 4-11 of the next, and
+  // these fall on distinct banks (64 banks, two rows).
+  const uint8_t* gw[GW];
+  const uint8_t* gx[GX];
+  int chunk[2];  // the lane's chunk of even and odd groups of eight rows
+#pragma unroll
+  for (int j = 0; j < 2; ++j) chunk[j] = (lane & 7) ^ ((4 * j + (lane >> 4)) & 7);
+#pragma unroll
+  for (int j = 0; j < GW; ++j) {
+    const int grp = wave * GW + j;
+    const int n = min(n0 + grp * 8 + (lane >> 3), p.N - 1);
+    gw[j] = w + (size_t)n * p.ldw + chunk[grp & 1] * 16;
+  }
+#pragma unroll
+  for (int j = 0; j < GX; ++j) {
+    const int grp = wave * GX + j;
+    const int src = max(source_row(p, min(t.m0 + grp * 8 + (lane >> 3), t.m1 - 1)), 0);
+    gx[j] = p.x + (size_t)src * p.ldx + chunk[grp & 1] * 16;
+  }
+  const float* gs = nullptr;  // the scales that the wave loads
+  if (wave < BM / 64)
+    gs = p.xs + (size_t)max(source_row(p, min(t.m0 + wave * 64 + lane, t.m1 - 1)), 0) * p.ld_xs;
+  else if (wave == BM / 64)
+    gs = ws + (size_t)min((n0 >> 7) + (lane & (BN / 128 - 1)), (p.N - 1) >> 7) * p.ld_ws;
+
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+  const int k16 = (p.K + 15) & ~15;
+  const auto load_stage = [&](int b) {
+    const int buf = (b & 1) * kStage;
+    const uint32_t at = lds0 + buf;
+    if ((b + 1) * 128 <= k16) {
+#pragma unroll
+      for (int j = 0; j < GW; ++j) dma16(gw[j], at + (wave * GW + j) * 1024);
+#pragma unroll
+      for (int j = 0; j < GX; ++j) dma16(gx[j], at + kW + (wave * GX + j) * 1024);
+    } else {  // the contraction ends inside the block: chunks behind its end are zeros
+#pragma unroll
+      for (int j = 0; j < GW; ++j) {
+        const int grp = wave * GW + j;
+        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], at + grp * 1024);
+        else *(v4i*)(lds + buf + grp * 1024 + lane * 16) = zero16();
+      }
+#pragma unroll
+      for (int j = 0; j < GX; ++j) {
+        const int grp = wave * GX + j;
+        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gx[j], at + kW + grp * 1024);
+        else *(v4i*)(lds + buf + kW + grp * 1024 + lane * 16) = zero16();
+      }
+    }
+    if (wave <= BM / 64) dma4(gs + b, at + kW + kX + wave * 256);
+#pragma unroll
+    for (int j = 0; j < GW; ++j) gw[j] += 128;
+#pragma unroll
+    for (int j = 0; j < GX; ++j) gx[j] += 128;
+  };
+
+  v4f acc[NT][MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  const int sw7 = (r16 >> 1) & 7;
+  const int o0 = r16 * 128 + (kg ^ sw7) * 16, o1 = r16 * 128 + ((kg + 4) ^ sw7) * 16;
+  load_stage(0);
+  for (int b = 0; b < p.KB; ++b) {
+    stage_barrier();
+    if (b + 1 < p.KB) load_stage(b + 1);
+    const char* st = lds + (b & 1) * kStage;
+    const char* sx = st + kW + wm * (MT * 2048);
+    const char* sw = st + wn * (NT * 2048);
+    const float* sc = (const float*)(st + kW + kX);
+    const float wsc = sc[BM + (BN > 128 ? (wn * NT) / 8 : 0)];
+    v8i xb[MT];
+    float s[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      xb[j] = join(*(const v4i*)(sx + j * 2048 + o0), *(const v4i*)(sx + j * 2048 + o1));
+      s[j] = sc[wm * (MT * 16) + j * 16 + r16] * wsc;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const v8i a = join(*(const v4i*)(sw + i * 2048 + o0), *(const v4i*)(sw + i * 2048 + o1));
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        const v4f d = EXACT ? block_bf16(a, xb[j]) : block_fp8(a, xb[j]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(d[e], s[j], acc[i][j][e]);
+      }
+    }
+  }
+  OutT* out = (OutT*)p.out;
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int m = t.m0 + wm * (MT * 16) + j * 16 + r16;
+    if (m >= t.m1) continue;
+    const bool none = p.order && source_row(p, m) < 0;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int n = n0 + wn * (NT * 16) + i * 16 + 4 * kg;
+      if (n < p.N) store_out4(out + (size_t)m * p.ldo + n, none ? v4f{0.f, 0.f, 0.f, 0.f} : acc[i][j], p.N - n);
+    }
+  }
+}
+
+template <int NT, int MT, int WN, int WM, bool EXACT, typename OutT>
+void launch_tile(const GemmParams& p, hipStream_t st) {
+  constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM;
+  const int nT = (p.N + BN - 1) / BN;
+  // an upper bound of the row tiles: every group may end inside one
+  const long mT = p.offsets ? p.M / BM + (p.G < p.M ? p.G : p.M) : (p.M + BM - 1) / BM;
+  const long grid = (mT * nT + 7) / 8 * 8;
+  launch_timed("fp8_gemm_tile", fp8_gemm_tile_kernel<NT, MT, WN, WM, EXACT, OutT>, dim3((uint32_t)grid),
+               dim3(64 * WN * WM), 0, st, p, nT);
+}
+
 }  // namespace
 
 size_t fp8_gemm_ws_bytes(const mira_fp8_gemm_args& a) {
@@ -159,6 +414,11 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.w_stride = a.w_stride ? a.w_stride : a.n * p.ldw;
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
+  if (p.M > 16 * p.G) {
+    if (a.out_dtype == MIRA_F32) launch_tile<4, 4, 4, 2, true, float>(p, st);
+    else launch_tile<8, 4, 2, 4, false, uint16_t>(p, st);
+    return hipGetLastError();
+  }
   const dim3 grid((p.N + 15) / 16, p.G);
   if (a.out_dtype == MIRA_F32)
     launch_timed("fp8_gemm_rows", fp8_gemm_rows_kernel<float>, grid, dim3(256), 0, st, p);

@@ -95,8 +95,12 @@ class _Fp8GemmArgs(ctypes.Structure):
 
 def _fill(struct, args):
     """The C structure of an argument dataclass whose fields have its names."""
-    return struct(**{n: _ptr(getattr(args, n)) if t is _VP else getattr(args, n)
-                     for n, t in struct._fields_ if n != "reserved"})
+    d = args.__dict__
+    return struct(*[_ptr(d[n]) if p else d[n] for n, p in struct._plan])
+
+
+for _s in (_BalanceArgs, _Fp8QuantArgs, _Fp8GemmArgs):
+    _s._plan = [(n, t is _VP) for n, t in _s._fields_]
 
 
 @dataclass
@@ -260,6 +264,7 @@ class Fp8GemmArgs:
     out_dtype: int = MIRA_BF16
     x_rows: int = 0
     top_k: int = 0
+    reserved: int = 0
     x: Any = None
     ldx: int = 0
     x_scale: Any = None
@@ -286,8 +291,9 @@ def _ptr(v) -> Optional[int]:
         return None
     if isinstance(v, int):
         return v or None
-    if hasattr(v, "data_ptr"):
-        return v.data_ptr() or None
+    address = getattr(v, "data_ptr", None)
+    if address is not None:
+        return address() or None
     raise TypeError(f"cannot take the address of {type(v).__name__}")
 
 

@@ -460,7 +460,7 @@ typedef struct mira_fp8_gemm_args {
   int32_t top_k;       /* pairs per token; with pair_order 1..MIRA_MAX_TOPK, else 0 */
   int32_t reserved;    /* must be 0 */
   const void* x;       /* [x_rows][ldx] e4m3, 16-byte aligned */
-  uint64_t ldx;        /* a multiple of 16, >= k rounded up to one; 0 = that */
+  uint64_t ldx;        /* a multiple of 16, >= k rounded up to one, <= 2^24; 0 = k so rounded */
   const float* x_scale; /* [x_rows][ceil(k/128)] */
   uint64_t ld_xs;      /* 0 = dense */
   const void* w;       /* G matrices [n][ldw] e4m3, 16-byte aligned */

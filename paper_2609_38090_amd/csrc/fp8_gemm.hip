@@ -10,6 +10,8 @@
 // on lone pairs of products; on normal data a block's sum is off by 1.3e-5 to
 // 1.6e-5 of its 2-norm, 5e-5 with uniformly random bytes).  Products of e4m3
 // values widened to bf16 (exact) sum to fp32 accuracy (1e-8).
+#include <type_traits>
+
 #include "device_util.h"
 #include "mira_internal.h"
 
@@ -145,6 +147,9 @@ __global__ __launch_bounds__(256) void fp8_gemm_rows_kernel(GemmParams p) {
 __device__ __forceinline__ void dma16(const void* src, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
 }
+__device__ __forceinline__ void dma16(uint32_t off, const void* base, uint32_t m0) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
+}
 __device__ __forceinline__ void dma4(const void* src, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
 }
@@ -157,11 +162,6 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
 // All loads to LDS have landed and all LDS reads have returned, in every wave.
 __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-// The 16 x 16 sums of one block on the fp8 matrix cores.
-__device__ __forceinline__ v4f block_fp8(v8i a, v8i b) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
 
 struct Tile {
@@ -251,26 +251,61 @@ __device__ __forceinline__ void store_out4(OutT* p, v4f v, int n) {
   }
 }
 
+// Compile-time loop: f(std::integral_constant<int, I>) for I in [B, E).
+template <int B, int E, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>{});
+    static_for<B + 1, E>(f);
+  }
+}
+
+// Operand fragments of one block: as loaded, or widened to bf16.
+template <bool EXACT>
+struct Frag;
+template <>
+struct Frag<false> {
+  v8i v;
+  __device__ __forceinline__ void set(v8i a) { v = a; }
+  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+  }
+};
+template <>
+struct Frag<true> {
+  v4i v[4];
+  __device__ __forceinline__ void set(v8i a) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) v[s] = widen8(a[2 * s], a[2 * s + 1]);
+  }
+  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b) {
+    v4f d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) d = mfma_bf16(a.v[s], b.v[s], d);
+    return d;
+  }
+};
+
 template <int NT, int MT, int WN, int WM, bool EXACT, typename OutT>
 __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams p, int nT) {
   constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM, W = WN * WM;
-  constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX + (BM + 64) * 4;
+  constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX, kScales = (BM + 64) * 16;
   constexpr int GW = BN / 8 / W, GX = BM / 8 / W;  // loads of 8 rows per wave and stage
   static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && BM % 64 == 0 && BM / 64 < W && 128 % (16 * NT) == 0, "tile shape");
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+  __shared__ __attribute__((aligned(1024))) char lds[2 * (kStage + kScales)];
   __shared__ int tile_s[4];
   Tile t;
   if (!find_tile<BM>(p, nT, tile_s, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, kg = lane >> 4, wn = wave % WN, wm = wave / WN;
   const int n0 = t.nt * BN;
-  const uint8_t* w = p.w + (size_t)t.g * p.w_stride;
+  const uint8_t* w = p.w + (size_t)t.g * p.w_stride + (size_t)n0 * p.ldw;  // advances with the stages
   const float* ws = p.ws + (size_t)t.g * p.ws_stride;
 
   // Row r stores its 16-byte chunk c at chunk c ^ ((r >> 1) & 7): a 128-bit read
   // serves rows 0-3 and 12-15 of one k-group with rows 4-11 of the next, and
   // these fall on distinct banks (64 banks, two rows).
-  const uint8_t* gw[GW];
+  uint32_t gw[GW];  // 32-bit offsets: a tile's weight rows lie within 256 * ldw < 2^32 bytes
   const uint8_t* gx[GX];
   int chunk[2];  // the lane's chunk of even and odd groups of eight rows
 #pragma unroll
@@ -278,8 +313,8 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
 #pragma unroll
   for (int j = 0; j < GW; ++j) {
     const int grp = wave * GW + j;
-    const int n = min(n0 + grp * 8 + (lane >> 3), p.N - 1);
-    gw[j] = w + (size_t)n * p.ldw + chunk[grp & 1] * 16;
+    const int r = min(grp * 8 + (lane >> 3), p.N - 1 - n0);
+    gw[j] = (uint32_t)r * (uint32_t)p.ldw + chunk[grp & 1] * 16;
   }
 #pragma unroll
   for (int j = 0; j < GX; ++j) {
@@ -287,27 +322,47 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     const int src = max(source_row(p, min(t.m0 + grp * 8 + (lane >> 3), t.m1 - 1)), 0);
     gx[j] = p.x + (size_t)src * p.ldx + chunk[grp & 1] * 16;
   }
-  const float* gs = nullptr;  // the scales that the wave loads
+  // Scales go to LDS for four stages at a time, [row][4] (a load touches a line
+  // of memory per row, as many as the rows themselves take): a wave of 64 token
+  // rows each, and one for the weights' blocks.  The last four are the last of
+  // the row, so that no load passes its end.
+  const float* gs = nullptr;
   if (wave < BM / 64)
     gs = p.xs + (size_t)max(source_row(p, min(t.m0 + wave * 64 + lane, t.m1 - 1)), 0) * p.ld_xs;
   else if (wave == BM / 64)
-    gs = ws + (size_t)min((n0 >> 7) + (lane & (BN / 128 - 1)), (p.N - 1) >> 7) * p.ld_ws;
-
+    gs = ws + (size_t)min((n0 >> 7) + (lane & ((BN + 127) / 128 - 1)), (p.N - 1) >> 7) * p.ld_ws;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
   const int k16 = (p.K + 15) & ~15;
+  // Load d of the wave's GW + GX of a whole stage.
+  const auto load_one = [&](auto d, uint32_t at) {
+    constexpr int D = d;
+    if constexpr (D < GW) {
+      dma16(gw[D], w, at + (wave * GW + D) * 1024);
+    } else {
+      dma16(gx[D - GW], at + kW + (wave * GX + D - GW) * 1024);
+      gx[D - GW] += 128;
+    }
+  };
+  const auto load_scales = [&](int q) {  // those of stages 4q .. 4q+3
+    const int at = 2 * kStage + (q & 1) * kScales + wave * 1024;
+    if (wave > BM / 64 || 4 * q >= p.KB) return;
+    if (p.KB >= 4) {
+      dma16(gs + min(4 * q, p.KB - 4), lds0 + at);
+    } else {
+      for (int i = 0; i < p.KB; ++i) *(float*)(lds + at + lane * 16 + i * 4) = gs[i];
+    }
+  };
+  // Any stage at once; where the contraction ends inside it, the chunks behind its end are zeros.
   const auto load_stage = [&](int b) {
     const int buf = (b & 1) * kStage;
     const uint32_t at = lds0 + buf;
     if ((b + 1) * 128 <= k16) {
-#pragma unroll
-      for (int j = 0; j < GW; ++j) dma16(gw[j], at + (wave * GW + j) * 1024);
-#pragma unroll
-      for (int j = 0; j < GX; ++j) dma16(gx[j], at + kW + (wave * GX + j) * 1024);
-    } else {  // the contraction ends inside the block: chunks behind its end are zeros
+      static_for<0, GW + GX>([&](auto d) { load_one(d, at); });
+    } else {
 #pragma unroll
       for (int j = 0; j < GW; ++j) {
         const int grp = wave * GW + j;
-        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], at + grp * 1024);
+        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], w, at + grp * 1024);
         else *(v4i*)(lds + buf + grp * 1024 + lane * 16) = zero16();
       }
 #pragma unroll
@@ -317,11 +372,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
         else *(v4i*)(lds + buf + kW + grp * 1024 + lane * 16) = zero16();
       }
     }
-    if (wave <= BM / 64) dma4(gs + b, at + kW + kX + wave * 256);
-#pragma unroll
-    for (int j = 0; j < GW; ++j) gw[j] += 128;
-#pragma unroll
-    for (int j = 0; j < GX; ++j) gx[j] += 128;
+    w += 128;
   };
 
   v4f acc[NT][MT];
@@ -331,33 +382,70 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     for (int j = 0; j < MT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
   const int sw7 = (r16 >> 1) & 7;
   const int o0 = r16 * 128 + (kg ^ sw7) * 16, o1 = r16 * 128 + ((kg + 4) ^ sw7) * 16;
-  load_stage(0);
-  for (int b = 0; b < p.KB; ++b) {
-    stage_barrier();
-    if (b + 1 < p.KB) load_stage(b + 1);
+  const auto read = [&](const char* base) { return join(*(const v4i*)(base + o0), *(const v4i*)(base + o1)); };
+
+  // Multiplies stage b.  Step i * MT + j multiplies weight tile i by token tile j
+  // and adds the sums of kBehind steps before, so that neither the matrix core
+  // nor the fp32 additions wait for one another; the fences keep this order.
+  // LOAD: the loads of stage b + 1, a whole one, are issued between the steps.
+  constexpr int kSteps = NT * MT, kBehind = EXACT ? 1 : 2, kLoads = GW + GX;
+  const auto multiply = [&](int b, auto load) {
+    constexpr bool LOAD = load;
     const char* st = lds + (b & 1) * kStage;
+    const uint32_t next = lds0 + ((b + 1) & 1) * kStage;
     const char* sx = st + kW + wm * (MT * 2048);
     const char* sw = st + wn * (NT * 2048);
-    const float* sc = (const float*)(st + kW + kX);
-    const float wsc = sc[BM + (BN > 128 ? (wn * NT) / 8 : 0)];
-    v8i xb[MT];
+    const int q = b >> 2;
+    const float* sc = (const float*)(lds + 2 * kStage + (q & 1) * kScales) + (b - max(min(4 * q, p.KB - 4), 0));
+    v4f d[kBehind + 1];
+    Frag<EXACT> a[2], x[MT];
     float s[MT];
+    v8i raw = read(sw);
+    v8i xr[MT];
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      xb[j] = join(*(const v4i*)(sx + j * 2048 + o0), *(const v4i*)(sx + j * 2048 + o1));
-      s[j] = sc[wm * (MT * 16) + j * 16 + r16] * wsc;
-    }
+    for (int j = 0; j < MT; ++j) xr[j] = read(sx + j * 2048);
+    const float wsc = sc[(BM + (wn * NT) / 8) * 4];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const v8i a = join(*(const v4i*)(sw + i * 2048 + o0), *(const v4i*)(sw + i * 2048 + o1));
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const v4f d = EXACT ? block_bf16(a, xb[j]) : block_fp8(a, xb[j]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(d[e], s[j], acc[i][j][e]);
+    for (int j = 0; j < MT; ++j) s[j] = sc[(wm * (MT * 16) + j * 16 + r16) * 4];
+    a[0].set(raw);
+    static_for<0, kSteps + kBehind>([&](auto step) {
+      constexpr int S = step, i = S / MT, j = S % MT;
+      if constexpr (S < kSteps) {
+        if constexpr (i == 0) {
+          x[j].set(xr[j]);
+          s[j] *= wsc;
+        }
+        if constexpr (j == 0 && i + 1 < NT) raw = read(sw + (i + 1) * 2048);
+        d[S % (kBehind + 1)] = Frag<EXACT>::mul(a[i & 1], x[j]);
+        if constexpr (j == MT - 1 && i + 1 < NT) a[(i + 1) & 1].set(raw);
       }
-    }
+      if constexpr (S >= kBehind) {
+        constexpr int P = S - kBehind;
+        v4f& c = acc[P / MT][P % MT];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = fmaf(d[P % (kBehind + 1)][e], s[P % MT], c[e]);
+      }
+      if constexpr (LOAD && S >= 1 && S <= kLoads) load_one(std::integral_constant<int, S - 1>{}, next);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (LOAD) w += 128;
+  };
+  const int whole = k16 >> 7;
+  load_scales(0);
+  load_stage(0);
+  int b = 0;
+  for (; b + 1 < whole; ++b) {
+    stage_barrier();
+    if ((b & 3) == 1) load_scales((b >> 2) + 1);
+    multiply(b, std::true_type{});
   }
+  for (; b < p.KB; ++b) {
+    stage_barrier();
+    if ((b & 3) == 1) load_scales((b >> 2) + 1);
+    if (b + 1 < p.KB) load_stage(b + 1);
+    multiply(b, std::false_type{});
+  }
+
   OutT* out = (OutT*)p.out;
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
@@ -415,7 +503,7 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
   if (p.M > 16 * p.G) {
-    if (a.out_dtype == MIRA_F32) launch_tile<4, 4, 4, 2, true, float>(p, st);
+    if (a.out_dtype == MIRA_F32) launch_tile<8, 4, 2, 4, true, float>(p, st);
     else launch_tile<8, 4, 2, 4, false, uint16_t>(p, st);
     return hipGetLastError();
   }

@@ -153,6 +153,7 @@ int mira_fp8_gemm(const mira_fp8_gemm_args* a, hipStream_t stream) {
   if (!rc) rc = check_ld("ld_ws", a->ld_ws, kb, 1);
   if (!rc) rc = check_ld("ldo", a->ldo, a->n, 1);
   if (rc) return rc;
+  if (a->ldx > 1 << 24 || a->ldw > 1 << 24) return set_error(MIRA_ERR_SHAPE, "ldx and ldw must be at most 2^24");
   const uint64_t ldw = a->ldw ? a->ldw : k16, ld_ws = a->ld_ws ? a->ld_ws : kb;
   if (a->w_stride && (a->w_stride < (a->n - 1) * ldw + k16 || a->w_stride > 1ull << 50))
     return set_error(MIRA_ERR_SHAPE, "w_stride (%llu) is smaller than a matrix, or too large", (unsigned long long)a->w_stride);

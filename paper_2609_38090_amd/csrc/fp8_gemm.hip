@@ -32,16 +32,6 @@ __device__ __forceinline__ v4i widen8(int lo, int hi) {
   return r;
 }
 
-// The 16 x 16 sums of one block, D = A(16 x 128) * B(128 x 16), through bf16.
-// Lane l holds the same 32 k-values of A row l%16 and of B column l%16 (those
-// of its k-group l/16); D row 4*(l/16)+i, column l%16.
-__device__ __forceinline__ v4f block_bf16(v8i a, v8i b) {
-  v4f d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int s = 0; s < 4; ++s) d = mfma_bf16(widen8(a[2 * s], a[2 * s + 1]), widen8(b[2 * s], b[2 * s + 1]), d);
-  return d;
-}
-
 struct GemmParams {
   const uint8_t* x;
   const float* xs;
@@ -50,8 +40,9 @@ struct GemmParams {
   const int32_t* offsets;
   const int32_t* order;
   void* out;
+  float* part;  // fp32 [S][M][N] sums of the contraction's S parts, or null (S = 1)
   size_t ldx, ld_xs, ldw, w_stride, ld_ws, ws_stride, ldo;
-  int M, N, K, KB, G, x_rows, top_k;
+  int M, N, K, KB, G, x_rows, top_k, S;
 };
 
 struct Rows {
@@ -76,15 +67,6 @@ __device__ __forceinline__ v8i join(v4i a, v4i b) {
   return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// The 32 bytes from k on of a row (null: zeros); zeros from K on (a row's last
-// 16 bytes are padded with zeros in memory).
-__device__ __forceinline__ v8i load32(const uint8_t* row, int k, int K) {
-  v4i a = zero16(), b = zero16();
-  if (row && k < K) a = ld16(row + k);
-  if (row && k + 16 < K) b = ld16(row + k + 16);
-  return join(a, b);
-}
-
 template <typename OutT>
 __device__ __forceinline__ void store_out(OutT* p, float v);
 template <>
@@ -94,44 +76,7 @@ __device__ __forceinline__ void store_out<uint16_t>(uint16_t* p, float v) {
   *p = v != v ? (uint16_t)((__float_as_uint(v) >> 16) | 0x40u) : f32_to_bf16_rne(v);
 }
 
-// Few rows: a workgroup owns 16 weight rows of one group; its four waves split
-// the blocks of the contraction and add up in LDS.
-template <typename OutT>
-__global__ __launch_bounds__(256) void fp8_gemm_rows_kernel(GemmParams p) {
-  __shared__ float sums[4][16][17];
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, r16 = lane & 15, kg = lane >> 4;
-  const int g = blockIdx.y, n0 = blockIdx.x * 16;
-  const Rows rows = rows_of(p, g);
-  const int n = n0 + r16;
-  const uint8_t* wrow = n < p.N ? p.w + g * p.w_stride + (size_t)n * p.ldw : nullptr;
-  const float* wsc = p.ws + g * p.ws_stride + (size_t)(n0 >> 7) * p.ld_ws;
-  OutT* out = (OutT*)p.out;
-  const int per = (p.KB + 3) / 4, b0 = wave * per, b1 = min(b0 + per, p.KB);
-  for (int m0 = rows.lo; m0 < rows.hi; m0 += 16) {
-    const int m = m0 + r16;
-    const int src = m < rows.hi ? source_row(p, m) : -1;
-    const uint8_t* xrow = src >= 0 ? p.x + (size_t)src * p.ldx : nullptr;
-    const float* xsc = src >= 0 ? p.xs + (size_t)src * p.ld_xs : nullptr;
-    v4f acc = {0.f, 0.f, 0.f, 0.f};
-    for (int b = b0; b < b1; ++b) {
-      const v4f d = block_bf16(load32(wrow, b * 128 + kg * 32, p.K), load32(xrow, b * 128 + kg * 32, p.K));
-      const float s = xsc ? xsc[b] * wsc[b] : 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = fmaf(d[i], s, acc[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sums[wave][r16][4 * kg + i] = acc[i];
-    __syncthreads();
-    const int mi = t >> 4, ni = t & 15;
-    if (m0 + mi < rows.hi && n0 + ni < p.N)
-      store_out(out + (size_t)(m0 + mi) * p.ldo + n0 + ni,
-                (sums[0][mi][ni] + sums[1][mi][ni]) + (sums[2][mi][ni] + sums[3][mi][ni]));
-    __syncthreads();
-  }
-}
-
-
-// ---- many rows: tiles through LDS ---------------------------------------------
+// ---- tiles through LDS ----------------------------------------------------------
 //
 // A workgroup of WN x WM waves owns BN weight rows by BM token rows; a wave owns
 // 16 NT x 16 MT of them, within one scale block of the weights.  Stages of one
@@ -139,9 +84,9 @@ __global__ __launch_bounds__(256) void fp8_gemm_rows_kernel(GemmParams p) {
 // by direct loads, two stages in turn: the loads of the next one are in flight
 // while this one is multiplied.
 
-// One direct-to-LDS load of a wave: lane l's bytes go to LDS address m0 + 16 l
-// (or 4 l).  The compiler does not see these loads; every wait for them is the
-// explicit one at the stage's start.
+// One direct-to-LDS load of a wave: lane l's bytes go to LDS address m0 + 16 l.  The
+// compiler does not see these loads; every wait for them is the explicit one at
+// the stage's start.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(const void* src, uint32_t m0) {
@@ -150,32 +95,43 @@ __device__ __forceinline__ void dma16(const void* src, uint32_t m0) {
 __device__ __forceinline__ void dma16(uint32_t off, const void* base, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
 }
-__device__ __forceinline__ void dma4(const void* src, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
-}
 #pragma clang diagnostic pop
+
+// A pointer that all lanes agree on, in scalar registers.
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t v = (uint64_t)p;
+  // (the builtin returns a signed int: without the casts the low half's sign would spread)
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+  return (const uint8_t*)((uint64_t)hi << 32 | lo);
+}
 
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
-// All loads to LDS have landed and all LDS reads have returned, in every wave.
+// In every wave, all but the newest N loads to LDS have landed and all LDS reads
+// have returned.
+template <int N>
 __device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(N) : "memory");
 }
 
 struct Tile {
-  int g, m0, m1, nt;  // group, rows [m0, m1), tile of weight rows
+  int g, m0, m1, nt, part;  // group, rows [m0, m1), tile of weight rows, part of the contraction
 };
 
 // Tiles are numbered so that the workgroups of one XCD (ids equal modulo 8) take
 // consecutive ones, and consecutive tiles run down kTileRun row tiles that share
 // their weights before the next weight rows.
 constexpr int kTileRun = 8;
-__device__ __forceinline__ bool tile_number(int mT, int nT, int& mt, int& nt) {
-  const int total = mT * nT, per = (total + 7) >> 3, i = blockIdx.x >> 3;
-  const int id = (blockIdx.x & 7) * per + i;
+__device__ __forceinline__ bool tile_number(int mT, int nT, int S, int& mt, int& nt, int& part) {
+  const int each = mT * nT, total = each * S, per = (total + 7) >> 3, i = blockIdx.x >> 3;
+  int id = (blockIdx.x & 7) * per + i;
   if (i >= per || id >= total) return false;
+  part = id / each;
+  id -= part * each;
   const int run = id / (kTileRun * nT), first = run * kTileRun, rows = min(mT - first, kTileRun);
   const int at = id - first * nT;
   nt = at / rows;
@@ -188,7 +144,7 @@ template <int BM>
 __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shared, Tile& t) {
   if (!p.offsets) {
     int mt;
-    if (!tile_number((p.M + BM - 1) / BM, nT, mt, t.nt)) return false;
+    if (!tile_number((p.M + BM - 1) / BM, nT, p.S, mt, t.nt, t.part)) return false;
     t.g = 0;
     t.m0 = mt * BM;
     t.m1 = min(t.m0 + BM, p.M);
@@ -210,10 +166,13 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
       const int v = __shfl_up(end, o, 64);
       if (l >= o) end += v;
     }
-    const int mT = __shfl(end, 63, 64);
-    int mt = 0, nt = 0;
-    const bool any = tile_number(mT, nT, mt, nt);
-    if (l == 0) shared[0] = any ? nt : -1;
+    const int mT = min(__shfl(end, 63, 64), p.M / BM + min(p.G, p.M));  // (more only where offsets overlap)
+    int mt = 0, nt = 0, part = 0;
+    const bool any = tile_number(mT, nT, p.S, mt, nt, part);
+    if (l == 0) {
+      shared[0] = any ? nt : -1;
+      shared[4] = part;
+    }
     int at = end - sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -226,10 +185,11 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
     }
   }
   __syncthreads();
-  t.nt = shared[0];
-  t.g = shared[1];
-  t.m0 = shared[2];
-  t.m1 = min(shared[2] + BM, shared[3]);
+  t.nt = __builtin_amdgcn_readfirstlane(shared[0]);
+  t.g = __builtin_amdgcn_readfirstlane(shared[1]);
+  t.m0 = __builtin_amdgcn_readfirstlane(shared[2]);
+  t.m1 = min(t.m0 + BM, __builtin_amdgcn_readfirstlane(shared[3]));
+  t.part = __builtin_amdgcn_readfirstlane(shared[4]);
   return t.nt >= 0;
 }
 
@@ -286,20 +246,26 @@ struct Frag<true> {
   }
 };
 
-template <int NT, int MT, int WN, int WM, bool EXACT, typename OutT>
+template <int NT, int MT, int WN, int WM, int NS, bool EXACT, typename OutT>
 __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams p, int nT) {
   constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM, W = WN * WM;
-  constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX, kScales = (BM + 64) * 16;
-  constexpr int GW = BN / 8 / W, GX = BM / 8 / W;  // loads of 8 rows per wave and stage
-  static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && BM % 64 == 0 && BM / 64 < W && 128 % (16 * NT) == 0, "tile shape");
-  __shared__ __attribute__((aligned(1024))) char lds[2 * (kStage + kScales)];
-  __shared__ int tile_s[4];
+  constexpr int SX = (BM + 63) / 64;  // waves that load token scales; the next one loads the weights'
+  constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX, kScales = (SX + 1) * 1024;
+  // Loads of 8 rows per wave and stage; with fewer than W such groups of token
+  // rows, several waves load the same ones to the same place.
+  constexpr int GW = BN / 8 / W, GX = BM / 8 / W > 0 ? BM / 8 / W : 1;
+  static_assert(BN % (8 * W) == 0 && (BM % (8 * W) == 0 || W % (BM / 8) == 0) && BN % 128 == 0 && SX < W && 128 % (16 * NT) == 0,
+                "tile shape");
+  static_assert(NS >= 2 && NS <= 4, "a block's scales land before they are read");
+  __shared__ __attribute__((aligned(1024))) char lds[NS * kStage + 2 * kScales];
+  __shared__ int tile_s[5];
   Tile t;
   if (!find_tile<BM>(p, nT, tile_s, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, kg = lane >> 4, wn = wave % WN, wm = wave / WN;
   const int n0 = t.nt * BN;
-  const uint8_t* w = p.w + (size_t)t.g * p.w_stride + (size_t)n0 * p.ldw;  // advances with the stages
+  const int per = (p.KB + p.S - 1) / p.S, b0 = t.part * per, b1 = min(b0 + per, p.KB);  // the blocks of this part
+  const uint8_t* w = p.w + (size_t)t.g * p.w_stride + (size_t)n0 * p.ldw + (size_t)b0 * 128;  // advances with the stages
   const float* ws = p.ws + (size_t)t.g * p.ws_stride;
 
   // Row r stores its 16-byte chunk c at chunk c ^ ((r >> 1) & 7): a 128-bit read
@@ -318,56 +284,56 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   }
 #pragma unroll
   for (int j = 0; j < GX; ++j) {
-    const int grp = wave * GX + j;
+    const int grp = (wave * GX + j) % (BM / 8);
     const int src = max(source_row(p, min(t.m0 + grp * 8 + (lane >> 3), t.m1 - 1)), 0);
-    gx[j] = p.x + (size_t)src * p.ldx + chunk[grp & 1] * 16;
+    gx[j] = p.x + (size_t)src * p.ldx + (size_t)b0 * 128 + chunk[grp & 1] * 16;
   }
   // Scales go to LDS for four stages at a time, [row][4] (a load touches a line
   // of memory per row, as many as the rows themselves take): a wave of 64 token
   // rows each, and one for the weights' blocks.  The last four are the last of
   // the row, so that no load passes its end.
   const float* gs = nullptr;
-  if (wave < BM / 64)
+  if (wave < SX)
     gs = p.xs + (size_t)max(source_row(p, min(t.m0 + wave * 64 + lane, t.m1 - 1)), 0) * p.ld_xs;
-  else if (wave == BM / 64)
+  else if (wave == SX)
     gs = ws + (size_t)min((n0 >> 7) + (lane & ((BN + 127) / 128 - 1)), (p.N - 1) >> 7) * p.ld_ws;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
   const int k16 = (p.K + 15) & ~15;
   // Load d of the wave's GW + GX of a whole stage.
-  const auto load_one = [&](auto d, uint32_t at) {
+  const auto load_one = [&](auto d, const uint8_t* wb, uint32_t at) {
     constexpr int D = d;
     if constexpr (D < GW) {
-      dma16(gw[D], w, at + (wave * GW + D) * 1024);
+      dma16(gw[D], wb, at + (wave * GW + D) * 1024);
     } else {
-      dma16(gx[D - GW], at + kW + (wave * GX + D - GW) * 1024);
+      dma16(gx[D - GW], at + kW + (wave * GX + D - GW) % (BM / 8) * 1024);
       gx[D - GW] += 128;
     }
   };
-  const auto load_scales = [&](int q) {  // those of stages 4q .. 4q+3
-    const int at = 2 * kStage + (q & 1) * kScales + wave * 1024;
-    if (wave > BM / 64 || 4 * q >= p.KB) return;
+  const auto load_scales = [&](int q) {  // those of blocks b0 + 4q .. b0 + 4q+3
+    const int at = NS * kStage + (q & 1) * kScales + wave * 1024;
+    if (wave > SX || b0 + 4 * q >= b1) return;
     if (p.KB >= 4) {
-      dma16(gs + min(4 * q, p.KB - 4), lds0 + at);
+      dma16(gs + min(b0 + 4 * q, p.KB - 4), lds0 + at);
     } else {
       for (int i = 0; i < p.KB; ++i) *(float*)(lds + at + lane * 16 + i * 4) = gs[i];
     }
   };
   // Any stage at once; where the contraction ends inside it, the chunks behind its end are zeros.
-  const auto load_stage = [&](int b) {
-    const int buf = (b & 1) * kStage;
+  const auto load_stage = [&](int b, int buf) {
     const uint32_t at = lds0 + buf;
+    const uint8_t* wb = uniform(w);
     if ((b + 1) * 128 <= k16) {
-      static_for<0, GW + GX>([&](auto d) { load_one(d, at); });
+      static_for<0, GW + GX>([&](auto d) { load_one(d, wb, at); });
     } else {
 #pragma unroll
       for (int j = 0; j < GW; ++j) {
         const int grp = wave * GW + j;
-        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], w, at + grp * 1024);
+        if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], wb, at + grp * 1024);
         else *(v4i*)(lds + buf + grp * 1024 + lane * 16) = zero16();
       }
 #pragma unroll
       for (int j = 0; j < GX; ++j) {
-        const int grp = wave * GX + j;
+        const int grp = (wave * GX + j) % (BM / 8);
         if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gx[j], at + kW + grp * 1024);
         else *(v4i*)(lds + buf + kW + grp * 1024 + lane * 16) = zero16();
       }
@@ -389,14 +355,16 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   // nor the fp32 additions wait for one another; the fences keep this order.
   // LOAD: the loads of stage b + 1, a whole one, are issued between the steps.
   constexpr int kSteps = NT * MT, kBehind = EXACT ? 1 : 2, kLoads = GW + GX;
-  const auto multiply = [&](int b, auto load) {
+  constexpr int kPerStep = (kLoads + kSteps - 2) / (kSteps - 1);  // all issued by step kSteps - 1
+  const auto multiply = [&](int b, int buf, int free, auto load) {
     constexpr bool LOAD = load;
-    const char* st = lds + (b & 1) * kStage;
-    const uint32_t next = lds0 + ((b + 1) & 1) * kStage;
+    const char* st = lds + buf;
+    const uint32_t next = lds0 + free;
+    const uint8_t* wb = uniform(w);
     const char* sx = st + kW + wm * (MT * 2048);
     const char* sw = st + wn * (NT * 2048);
-    const int q = b >> 2;
-    const float* sc = (const float*)(lds + 2 * kStage + (q & 1) * kScales) + (b - max(min(4 * q, p.KB - 4), 0));
+    const int q = (b - b0) >> 2;
+    const float* sc = (const float*)(lds + NS * kStage + (q & 1) * kScales) + (b - max(min(b0 + 4 * q, p.KB - 4), 0));
     v4f d[kBehind + 1];
     Frag<EXACT> a[2], x[MT];
     float s[MT];
@@ -404,7 +372,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     v8i xr[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) xr[j] = read(sx + j * 2048);
-    const float wsc = sc[(BM + (wn * NT) / 8) * 4];
+    const float wsc = sc[(SX * 64 + (wn * NT) / 8) * 4];
 #pragma unroll
     for (int j = 0; j < MT; ++j) s[j] = sc[(wm * (MT * 16) + j * 16 + r16) * 4];
     a[0].set(raw);
@@ -425,25 +393,41 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
 #pragma unroll
         for (int e = 0; e < 4; ++e) c[e] = fmaf(d[P % (kBehind + 1)][e], s[P % MT], c[e]);
       }
-      if constexpr (LOAD && S >= 1 && S <= kLoads) load_one(std::integral_constant<int, S - 1>{}, next);
+      if constexpr (LOAD && S >= 1) {
+        constexpr int from = (S - 1) * kPerStep < kLoads ? (S - 1) * kPerStep : kLoads;
+        constexpr int to = S * kPerStep < kLoads ? S * kPerStep : kLoads;
+        static_for<from, to>([&](auto l) { load_one(l, wb, next); });
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (LOAD) w += 128;
   };
-  const int whole = k16 >> 7;
+  // A ring of NS stages: NS - 1 in flight ahead of the one multiplied.  buf is the
+  // current stage's place, free that of the stage before, which stage b + NS - 1
+  // takes once every wave has passed the barrier.
   load_scales(0);
-  load_stage(0);
-  int b = 0;
-  for (; b + 1 < whole; ++b) {
-    stage_barrier();
-    if ((b & 3) == 1) load_scales((b >> 2) + 1);
-    multiply(b, std::true_type{});
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (b0 + i < b1) load_stage(b0 + i, i * kStage);
+  const int whole = min(k16 >> 7, b1);
+  int b = b0, buf = 0, free = (NS - 1) * kStage;
+  const auto step = [&] {
+    free = buf;
+    buf = buf == (NS - 1) * kStage ? 0 : buf + kStage;
+    ++b;
+  };
+  while (b + NS - 1 < whole) {
+    stage_barrier<(NS - 2) * kLoads>();
+    if (((b - b0) & 3) == 1) load_scales(((b - b0) >> 2) + 1);
+    multiply(b, buf, free, std::true_type{});
+    step();
   }
-  for (; b < p.KB; ++b) {
-    stage_barrier();
-    if ((b & 3) == 1) load_scales((b >> 2) + 1);
-    if (b + 1 < p.KB) load_stage(b + 1);
-    multiply(b, std::false_type{});
+  while (b < b1) {
+    stage_barrier<0>();
+    if (((b - b0) & 3) == 1) load_scales(((b - b0) >> 2) + 1);
+    if (b + NS - 1 < b1) load_stage(b + NS - 1, free);
+    multiply(b, buf, free, std::false_type{});
+    step();
   }
 
   OutT* out = (OutT*)p.out;
@@ -455,30 +439,127 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int n = n0 + wn * (NT * 16) + i * 16 + 4 * kg;
-      if (n < p.N) store_out4(out + (size_t)m * p.ldo + n, none ? v4f{0.f, 0.f, 0.f, 0.f} : acc[i][j], p.N - n);
+      if (n >= p.N) continue;
+      const v4f v = none ? v4f{0.f, 0.f, 0.f, 0.f} : acc[i][j];
+      if (p.part) store_out4(p.part + ((size_t)t.part * p.M + m) * p.N + n, v, p.N - n);
+      else store_out4(out + (size_t)m * p.ldo + n, v, p.N - n);
     }
   }
 }
 
-template <int NT, int MT, int WN, int WM, bool EXACT, typename OutT>
-void launch_tile(const GemmParams& p, hipStream_t st) {
-  constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM;
-  const int nT = (p.N + BN - 1) / BN;
-  // an upper bound of the row tiles: every group may end inside one
-  const long mT = p.offsets ? p.M / BM + (p.G < p.M ? p.G : p.M) : (p.M + BM - 1) / BM;
-  const long grid = (mT * nT + 7) / 8 * 8;
-  launch_timed("fp8_gemm_tile", fp8_gemm_tile_kernel<NT, MT, WN, WM, EXACT, OutT>, dim3((uint32_t)grid),
-               dim3(64 * WN * WM), 0, st, p, nT);
+// Adds the S parts of the contraction in order.
+template <typename OutT>
+__global__ __launch_bounds__(256) void fp8_gemm_join_kernel(GemmParams p) {
+  const int lo = p.offsets ? rows_of(p, 0).lo : 0, hi = p.offsets ? rows_of(p, p.G - 1).hi : p.M;
+  const size_t total = (size_t)p.M * p.N;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+    const int m = (int)(i / p.N), n = (int)(i - (size_t)m * p.N);
+    if (m < lo || m >= hi) continue;
+    float sum = p.part[i];
+    for (int s = 1; s < p.S; ++s) sum += p.part[s * total + i];
+    store_out((OutT*)p.out + (size_t)m * p.ldo + n, sum);
+  }
+}
+
+// ---- choice of a tile shape ------------------------------------------------------
+//
+// Time of a call = rounds of tiles over the chip * (stages * time of a stage + a
+// tile's start and end), beside what its operands take to arrive.  us per
+// stage with one tile on a CU and (one) with as many as its LDS holds (all),
+// measured over 43 products of 1 to 4096 rows, N 300 to 28672, K 700 to 14336
+// (e.g. 4096 x 28672 x 4096, fp8 cores: 460 us in 256 x 256 tiles, 539 in 256 x
+// 128, 729 in 128 x 64; 64 x 28672 x 4096: 54, 34, 21 and 32 in 128 x 16; 2048 x
+// 4096 x 4096: 57, 39, 53; 16 x 28672 x 4096: 128 x 64 20 us, 128 x 16 19, with fp32
+// output 27 and 20).  Tiles of 128 x 128 were measured too (594, 33, 44) and are
+// best nowhere.  Parts of the contraction fill the chip where the tiles do not:
+// 1 x 4096 x 14336 takes 32 us in one part, 17 in eight.
+struct Shape {
+  const char* name;  // in the kernel timing
+  int bn, bm, per_cu;
+  float one[2], all[2];  // fp8, bf16 matrix cores
+};
+constexpr Shape kShapes[] = {
+    {"fp8_gemm_256x256", 256, 256, 1, {2.0f, 3.3f}, {2.0f, 3.3f}},
+    {"fp8_gemm_256x128", 256, 128, 1, {1.1f, 1.85f}, {1.1f, 1.85f}},
+    {"fp8_gemm_128x64", 128, 64, 2, {0.5f, 0.72f}, {0.8f, 1.15f}},
+    {"fp8_gemm_128x16", 128, 16, 2, {0.28f, 0.36f}, {0.42f, 0.52f}},
+};
+constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
+constexpr float kTileUs = 2.5f, kJoinUs = 4.5f, kJoinBytesPerUs = 4e6f, kBytesPerUs = 5.5e6f;
+constexpr int kMaxParts = 32;
+constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
+
+struct Plan {
+  int shape, S;  // S = 0: no shape fits one launch
+};
+
+long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
+  // with offsets an upper bound: every group may end inside a tile
+  const long mT = a.offsets ? a.m / s.bm + (a.n_groups < a.m ? a.n_groups : a.m) : (a.m + s.bm - 1) / s.bm;
+  return mT * ((a.n + s.bn - 1) / s.bn);
+}
+
+Plan plan_of(const mira_fp8_gemm_args& a) {
+  const int e = a.out_dtype == MIRA_F32, KB = (a.k + 127) / 128, cus = device_cu_count();
+  const float active = (float)(a.n_groups < a.m ? a.n_groups : a.m);
+  const float arrive = (active * a.n * a.k + (float)a.m * a.k + (float)a.m * a.n * (e ? 4.f : 2.f)) / kBytesPerUs;
+  Plan best{0, 0};
+  float least = 0.f;
+  for (int i = 0; i < kShapeCount; ++i) {
+    const Shape& s = kShapes[i];
+    const long tiles = tiles_of(a, s);
+    for (int parts = 1; parts <= kMaxParts && parts <= KB; ++parts) {
+      const int per = (KB + parts - 1) / parts;
+      if ((KB + per - 1) / per != parts) continue;  // no empty part
+      if (tiles * parts > kMaxTiles) break;
+      const long all = tiles * parts, full = all / (cus * s.per_cu), rest = all % (cus * s.per_cu);
+      float us = full * (per * s.all[e] + kTileUs) +
+                 (rest ? per * (rest > cus ? s.all[e] : s.one[e]) + kTileUs : 0.f);
+      us = us > arrive ? us + 0.2f * arrive : arrive + 0.2f * us;  // the two overlap, not wholly
+      if (parts > 1) us += kJoinUs + (float)parts * a.m * a.n * 8.f / kJoinBytesPerUs;
+      if (best.S == 0 || us < least) {
+        least = us;
+        best = Plan{i, parts};
+      }
+    }
+  }
+  return best;
+}
+
+template <int NT, int MT, int WN, int WM, int NS, bool EXACT, typename OutT>
+void launch_tile(const GemmParams& p, const Shape& shape, long tiles, hipStream_t st) {
+  constexpr int BN = 16 * NT * WN;
+  const long grid = (tiles * p.S + 7) / 8 * 8;
+  launch_timed(shape.name, fp8_gemm_tile_kernel<NT, MT, WN, WM, NS, EXACT, OutT>, dim3((uint32_t)grid),
+               dim3(64 * WN * WM), 0, st, p, (p.N + BN - 1) / BN);
+}
+
+template <bool EXACT, typename OutT>
+void launch_shape(const GemmParams& p, int i, long tiles, hipStream_t st) {
+  const Shape& shape = kShapes[i];
+  switch (i) {
+    case 0: launch_tile<8, 4, 2, 4, 2, EXACT, OutT>(p, shape, tiles, st); break;
+    case 1: launch_tile<4, 4, 4, 2, 3, EXACT, OutT>(p, shape, tiles, st); break;
+    case 2: launch_tile<4, 2, 2, 2, 3, EXACT, OutT>(p, shape, tiles, st); break;
+    default: launch_tile<2, 1, 4, 1, 4, EXACT, OutT>(p, shape, tiles, st); break;
+  }
+  if (p.S > 1) {
+    const size_t n = ((size_t)p.M * p.N + 255) / 256;
+    launch_timed("fp8_gemm_join", fp8_gemm_join_kernel<OutT>, dim3((uint32_t)(n < 4096 ? n : 4096)), dim3(256), 0, st, p);
+  }
 }
 
 }  // namespace
 
+bool fp8_gemm_fits(const mira_fp8_gemm_args& a) { return plan_of(a).S > 0; }
+
 size_t fp8_gemm_ws_bytes(const mira_fp8_gemm_args& a) {
-  (void)a;
-  return 0;
+  const Plan plan = plan_of(a);
+  return plan.S > 1 ? (size_t)plan.S * a.m * a.n * 4 : 0;
 }
 
 hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
+  const Plan plan = plan_of(a);
   GemmParams p{};
   p.x = (const uint8_t*)a.x;
   p.xs = a.x_scale;
@@ -487,6 +568,8 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.offsets = a.offsets;
   p.order = a.pair_order;
   p.out = a.out;
+  p.part = plan.S > 1 ? (float*)a.workspace : nullptr;
+  p.S = plan.S;
   p.M = a.m;
   p.N = a.n;
   p.K = a.k;
@@ -502,16 +585,9 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.w_stride = a.w_stride ? a.w_stride : a.n * p.ldw;
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
-  if (p.M > 16 * p.G) {
-    if (a.out_dtype == MIRA_F32) launch_tile<8, 4, 2, 4, true, float>(p, st);
-    else launch_tile<8, 4, 2, 4, false, uint16_t>(p, st);
-    return hipGetLastError();
-  }
-  const dim3 grid((p.N + 15) / 16, p.G);
-  if (a.out_dtype == MIRA_F32)
-    launch_timed("fp8_gemm_rows", fp8_gemm_rows_kernel<float>, grid, dim3(256), 0, st, p);
-  else
-    launch_timed("fp8_gemm_rows", fp8_gemm_rows_kernel<uint16_t>, grid, dim3(256), 0, st, p);
+  const long tiles = tiles_of(a, kShapes[plan.shape]);
+  if (a.out_dtype == MIRA_F32) launch_shape<true, float>(p, plan.shape, tiles, st);
+  else launch_shape<false, uint16_t>(p, plan.shape, tiles, st);
   return hipGetLastError();
 }
 

@@ -268,6 +268,7 @@ hipError_t launch_mixture(const mira_mixture_shape& p, const mira_mixture_weight
 size_t balance_ws_bytes(int E, int G);
 hipError_t launch_balance(const mira_balance_args& a, hipStream_t st);
 hipError_t launch_fp8_quantize(const mira_fp8_quant_args& a, hipStream_t st);
+bool fp8_gemm_fits(const mira_fp8_gemm_args& a);  // one launch holds the tiles
 size_t fp8_gemm_ws_bytes(const mira_fp8_gemm_args& a);
 hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st);
 hipError_t launch_set_slot(int32_t* table, int expert, int slot, hipStream_t st);

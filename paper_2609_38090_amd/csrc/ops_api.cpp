@@ -48,6 +48,8 @@ int check_gemm_sizes(const mira_fp8_gemm_args* a) {
   if (a->n_groups < 1 || a->n_groups > MIRA_MAX_EXPERTS)
     return set_error(MIRA_ERR_SHAPE, "n_groups (%d) must be in [1, %d]", a->n_groups, MIRA_MAX_EXPERTS);
   if (!a->offsets && a->n_groups != 1) return set_error(MIRA_ERR_ARG, "several groups need offsets");
+  if (a->m > 0 && !mira::fp8_gemm_fits(*a))
+    return set_error(MIRA_ERR_SHAPE, "m, n and n_groups (%d, %d, %d) are too large together", a->m, a->n, a->n_groups);
   return MIRA_OK;
 }
 

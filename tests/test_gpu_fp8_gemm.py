@@ -97,6 +97,26 @@ def test_larger(M, N, K, out):
     c.check()
 
 
+# rows, columns, contraction, groups that the dispatch sends to each tile shape
+SHAPES = {"fp8_gemm_256x256": (4100, 8300, 140, 1), "fp8_gemm_256x128": (1900, 4090, 260, 1),
+          "fp8_gemm_128x64": (1500, 2000, 500, 1), "fp8_gemm_128x16": (11, 3000, 700, 1), "fp8_gemm_join": (20, 260, 9000, 1)}
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("tail", [0, 77])
+def test_every_tile_shape(name, out, tail):
+    M, N, K, G = SHAPES[name]
+    c = Case(M, N, K + tail, out, pads=(1, 1, 1, 0, 0))
+    mira.mira_profile_enable(True)
+    mira.mira_profile_read()
+    c.run()
+    ran = mira.mira_profile_read()
+    mira.mira_profile_enable(False)
+    assert name in ran, ran
+    c.check()
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 200, 300), (20, 65, 1000), (150, 300, 257), (600, 530, 400)])
 @pytest.mark.parametrize("pads", [(1, 0, 0, 3, 1), (0, 2, 1, 0, 3), (3, 3, 2, 2, 8)])
 def test_strides(M, N, K, pads):

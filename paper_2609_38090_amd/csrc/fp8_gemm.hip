@@ -254,7 +254,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   // Loads of 8 rows per wave and stage; with fewer than W such groups of token
   // rows, several waves load the same ones to the same place.
   constexpr int GW = BN / 8 / W, GX = BM / 8 / W > 0 ? BM / 8 / W : 1;
-  static_assert(BN % (8 * W) == 0 && (BM % (8 * W) == 0 || W % (BM / 8) == 0) && BN % 128 == 0 && SX < W && 128 % (16 * NT) == 0,
+  static_assert(BN % (8 * W) == 0 && (BM % (8 * W) == 0 || W % (BM / 8) == 0) && (BN % 128 == 0 || 128 % BN == 0) && SX < W && 128 % (16 * NT) == 0,
                 "tile shape");
   static_assert(NS >= 2 && NS <= 4, "a block's scales land before they are read");
   __shared__ __attribute__((aligned(1024))) char lds[NS * kStage + 2 * kScales];
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   // nor the fp32 additions wait for one another; the fences keep this order.
   // LOAD: the loads of stage b + 1, a whole one, are issued between the steps.
   constexpr int kSteps = NT * MT, kBehind = EXACT ? 1 : 2, kLoads = GW + GX;
-  constexpr int kPerStep = (kLoads + kSteps - 2) / (kSteps - 1);  // all issued by step kSteps - 1
+  constexpr int kPerStep = kSteps > 1 ? (kLoads + kSteps - 2) / (kSteps - 1) : kLoads;  // all issued by the last step
   const auto multiply = [&](int b, int buf, int free, auto load) {
     constexpr bool LOAD = load;
     const char* st = lds + buf;
@@ -468,11 +468,12 @@ __global__ __launch_bounds__(256) void fp8_gemm_join_kernel(GemmParams p) {
 // stage with one tile on a CU and (one) with as many as its LDS holds (all),
 // measured over 43 products of 1 to 4096 rows, N 300 to 28672, K 700 to 14336
 // (e.g. 4096 x 28672 x 4096, fp8 cores: 460 us in 256 x 256 tiles, 539 in 256 x
-// 128, 729 in 128 x 64; 64 x 28672 x 4096: 54, 34, 21 and 32 in 128 x 16; 2048 x
-// 4096 x 4096: 57, 39, 53; 16 x 28672 x 4096: 128 x 64 20 us, 128 x 16 19, with fp32
-// output 27 and 20).  Tiles of 128 x 128 were measured too (594, 33, 44) and are
-// best nowhere.  Parts of the contraction fill the chip where the tiles do not:
-// 1 x 4096 x 14336 takes 32 us in one part, 17 in eight.
+// 128, 729 in 128 x 64; 64 x 28672 x 4096: 54, 34, 21; 2048 x 4096 x 4096: 57,
+// 39, 53; 16 x 4096 x 4096: 128 x 64 17 us, 64 x 16 10).  Tiles of 128 x 128 (594, 33,
+// 44) and of 128 x 16 (1 x 28672 x 4096: 28.7, 64 x 16 27.3) were measured too.
+// Parts of the contraction fill the chip where the tiles do not: 1 x 4096 x 14336
+// takes 28 us in one part, 15 in parts (their second launch is why short
+// contractions stay whole: 16 x 4096 x 4096 10 us, 13 in parts).
 struct Shape {
   const char* name;  // in the kernel timing
   int bn, bm, per_cu;
@@ -482,10 +483,10 @@ constexpr Shape kShapes[] = {
     {"fp8_gemm_256x256", 256, 256, 1, {2.0f, 3.3f}, {2.0f, 3.3f}},
     {"fp8_gemm_256x128", 256, 128, 1, {1.1f, 1.85f}, {1.1f, 1.85f}},
     {"fp8_gemm_128x64", 128, 64, 2, {0.5f, 0.72f}, {0.8f, 1.15f}},
-    {"fp8_gemm_128x16", 128, 16, 2, {0.28f, 0.36f}, {0.42f, 0.52f}},
+    {"fp8_gemm_64x16", 64, 16, 3, {0.25f, 0.3f}, {0.4f, 0.5f}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
-constexpr float kTileUs = 2.5f, kJoinUs = 4.5f, kJoinBytesPerUs = 4e6f, kBytesPerUs = 5.5e6f;
+constexpr float kTileUs = 2.5f, kJoinUs = 7.f, kJoinBytesPerUs = 4e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
 constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
 
@@ -541,7 +542,7 @@ void launch_shape(const GemmParams& p, int i, long tiles, hipStream_t st) {
     case 0: launch_tile<8, 4, 2, 4, 2, EXACT, OutT>(p, shape, tiles, st); break;
     case 1: launch_tile<4, 4, 4, 2, 3, EXACT, OutT>(p, shape, tiles, st); break;
     case 2: launch_tile<4, 2, 2, 2, 3, EXACT, OutT>(p, shape, tiles, st); break;
-    default: launch_tile<2, 1, 4, 1, 4, EXACT, OutT>(p, shape, tiles, st); break;
+    default: launch_tile<1, 1, 4, 1, 4, EXACT, OutT>(p, shape, tiles, st); break;
   }
   if (p.S > 1) {
     const size_t n = ((size_t)p.M * p.N + 255) / 256;

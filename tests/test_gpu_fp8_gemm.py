@@ -99,7 +99,7 @@ def test_larger(M, N, K, out):
 
 # rows, columns, contraction, groups that the dispatch sends to each tile shape
 SHAPES = {"fp8_gemm_256x256": (4100, 8300, 140, 1), "fp8_gemm_256x128": (1900, 4090, 260, 1),
-          "fp8_gemm_128x64": (1500, 2000, 500, 1), "fp8_gemm_128x16": (11, 3000, 700, 1), "fp8_gemm_join": (20, 260, 9000, 1)}
+          "fp8_gemm_128x64": (1500, 2000, 500, 1), "fp8_gemm_64x16": (11, 3000, 700, 1), "fp8_gemm_join": (20, 260, 9000, 1)}
 
 
 @pytest.mark.parametrize("name", list(SHAPES))

@@ -12,8 +12,11 @@
 // walks the groups that it meets.  Over the chunks in order, (chunk, group)
 // pairs that meet only ever step one of the two up, so chunk + group numbers
 // the partial sums without gaps to search: kMaxChunks + G slots hold any
-// layout of groups, and the finishing kernel adds a group's slots in order.
-// Calls of few logits run one workgroup per group in a single launch.
+// layout of groups.  A group's slots are added in order to its means and loss: for
+// one group by the last chunk to end, for several in a launch that follows (37
+// groups of 30011 rows: 26 us so, 32 with the chunks counting their groups' ends;
+// one group of 2048 x 64: 17 us with the launch, 12 without).  Calls of few logits
+// run one workgroup per group in a single launch.
 #include "device_util.h"
 #include "mira_internal.h"
 
@@ -23,7 +26,9 @@ namespace {
 
 constexpr int kMaxChunks = 256;   // one 1024-thread workgroup per CU
 constexpr int kBigThreads = 1024;
-constexpr int kSmallThreads = 256;
+// Selections that one workgroup per group counts (four times as many where groups
+// share them); more are counted by chunks, after a launch that zeroes the counts.
+constexpr size_t kFewPairs = 65536;
 
 struct BalanceParams {
   const void* logits;
@@ -34,6 +39,7 @@ struct BalanceParams {
   void* dlogits;           // may be null
   int32_t* counts;         // output or workspace
   int32_t* kept;           // [G] rows kept (with a mask)
+  int32_t* ended;          // chunks that have ended (one group)
   float* mean;             // may be null
   float* loss;             // may be null
   float* partial;          // [chunks + G][E]
@@ -60,8 +66,14 @@ __device__ __forceinline__ float lanes_reduce(float v) {
   if constexpr (L >= 4) v = Op::of(v, dpp<0x4E>(v));    // quad_perm 2,3,0,1
   if constexpr (L >= 8) v = Op::of(v, dpp<0x141>(v));   // mirror in 8
   if constexpr (L >= 16) v = Op::of(v, dpp<0x140>(v));  // mirror in 16
-  if constexpr (L >= 32) v = Op::of(v, __shfl_xor(v, 16, 64));
-  if constexpr (L >= 64) v = Op::of(v, __shfl_xor(v, 32, 64));
+  if constexpr (L >= 32) {  // both halves of the 32 swapped: one result is the lane's own value
+    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = Op::of(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
+  if constexpr (L >= 64) {
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = Op::of(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
   return v;
 }
 
@@ -76,8 +88,10 @@ __device__ __forceinline__ float exp_neg(float x) {
   return fmaf(e, r * 0.693147182464599609375f, e);
 }
 
-// The four logits of a row that a lane holds: VEC: 4l .. 4l+3 (E a multiple of
-// 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.
+// The logits of a row that a lane holds, up to four: VEC: 4l .. 4l+3 (E a multiple
+// of 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.  At most
+// kFewExperts experts take the largest power of two of lanes that they fill.
+constexpr int kFewExperts = 8;
 template <int L, bool VEC>
 __device__ __forceinline__ int expert_of(int l, int i) {
   return VEC ? 4 * l + i : l + L * i;
@@ -131,23 +145,25 @@ __device__ __forceinline__ Segment group_rows(const BalanceParams& q, int g) {
   const int lo = min(max(q.offsets[g], 0), q.T);
   return Segment{lo, min(max(q.offsets[g + 1], lo), q.T)};
 }
-// Last group g with offsets[g] <= row (the group that holds it if any does); -1 if none.
-__device__ __forceinline__ int group_of(const BalanceParams& q, int row) {
-  if (!q.offsets) return 0;
-  int lo = 0, hi = q.G + 1;  // first index with offsets[i] > row
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (q.offsets[mid] > row) hi = mid; else lo = mid + 1;
-  }
-  return lo - 1;
+__device__ __forceinline__ float count_scale(const BalanceParams& q, int n) {
+  return n > 0 ? (float)q.E * (1.f / ((float)q.k * (float)n)) : 0.f;
+}
+__device__ __forceinline__ float group_grad(const BalanceParams& q, int g) { return q.grad_loss ? q.grad_loss[g] : 1.f; }
+__device__ __forceinline__ float grad_scale(const BalanceParams& q, float grad, int n) {
+  return n > 0 ? grad * q.coef / (float)n : 0.f;
 }
 
 // Softmax, gradient and sums of p of rows lo, lo + step, .. < hi for one lane
 // group of L lanes (lane l of it); acc holds the lane's sums of p.  U rows are
 // in flight at once.
-template <int L, bool VEC, int U, typename T>
+// FEW (at most kFewExperts): expf and the formula's own operations, each rounded
+// once and none contracted.  With as many selected as there are experts the
+// gradient is zero but for its roundings; these are then those of the formula
+// evaluated step by step, not of a rearrangement.
+template <int L, bool VEC, bool FEW, int U, typename T>
 __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi, int step, int l,
-                                          const float f[4], float gscale, float acc[4]) {
+                                          const int counts[4], int n, float grad, float acc[4]) {
+  constexpr int NV = FEW ? 2 : 4;  // values that a lane may hold
   const T* x = (const T*)q.logits;
   T* d = (T*)q.dlogits;
   for (int r0 = lo; r0 < hi; r0 += U * step) {
@@ -162,29 +178,61 @@ __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi
         if (q.mask) keep[u] = q.mask[r] != 0;
       }
     }
+    // (here, so that the first rows do not wait for the counts to arrive)
+    const float gscale = grad_scale(q, grad, n), cs = count_scale(q, n);
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)counts[i] * cs;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = r0 + u * step;
       if (r >= hi) break;
-      float m = lanes_reduce<L, MaxOp>(fmaxf(fmaxf(v[u][0], v[u][1]), fmaxf(v[u][2], v[u][3])));
+      float m = v[u][0];
+#pragma unroll
+      for (int i = 1; i < NV; ++i) m = fmaxf(m, v[u][i]);
+      m = lanes_reduce<L, MaxOp>(m);
       m = m == -INFINITY ? 0.f : m;
-      float s = 0.f, w = 0.f;
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (FEW) {
+#pragma clang fp contract(off)
+        float s = 0.f, w = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[u][i] = exp_neg(v[u][i] - m);
-        s += v[u][i];
-        w = fmaf(f[i], v[u][i], w);
-      }
-      s = lanes_reduce<L, AddOp>(s);
-      w = lanes_reduce<L, AddOp>(w);
-      const float inv = s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
-      w *= inv;
-      float o[4];
+        for (int i = 0; i < NV; ++i) {
+          v[u][i] = expf(v[u][i] - m);
+          s = s + v[u][i];
+        }
+        s = lanes_reduce<L, AddOp>(s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = v[u][i] * inv;
-        acc[i] += keep[u] ? p : 0.f;
-        o[i] = keep[u] ? gscale * p * (f[i] - w) : 0.f;
+        for (int i = 0; i < NV; ++i) {
+          v[u][i] = s == 0.f ? 0.f : v[u][i] / s;
+          const float fp = f[i] * v[u][i];
+          w = w + fp;
+        }
+        w = lanes_reduce<L, AddOp>(w);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          acc[i] += keep[u] ? v[u][i] : 0.f;
+          const float gp = gscale * v[u][i];
+          o[i] = keep[u] ? gp * (f[i] - w) : 0.f;
+        }
+      } else {
+        float s = 0.f, w = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          v[u][i] = exp_neg(v[u][i] - m);
+          s += v[u][i];
+          w = fmaf(f[i], v[u][i], w);
+        }
+        s = lanes_reduce<L, AddOp>(s);
+        w = lanes_reduce<L, AddOp>(w);
+        const float inv = s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
+        w *= inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const float p = v[u][i] * inv;
+          acc[i] += keep[u] ? p : 0.f;
+          o[i] = keep[u] ? gscale * p * (f[i] - w) : 0.f;
+        }
       }
       if (d) store_row<L, VEC>(d + (size_t)r * q.ld_d, l, q.E, o);
     }
@@ -209,9 +257,18 @@ __device__ __forceinline__ void reduce_groups(float acc[4], int E, float (*wave_
 template <int THREADS>
 __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int hi, int* hist, int* kept) {
   const uint32_t end = (uint32_t)hi * q.k;  // T * k is at most 2^30
-  for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += THREADS) {
-    const int e = q.idx[i];
-    if ((uint32_t)e < (uint32_t)q.E && (!q.mask || q.mask[i / q.k])) atomicAdd(hist + e, 1);
+  for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += 4 * THREADS) {  // four loads in flight
+    int e[4];
+    bool keep[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t at = min(i + j * THREADS, end - 1);
+      e[j] = q.idx[at];
+      keep[j] = !q.mask || q.mask[at / q.k] != 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j * THREADS < end && (uint32_t)e[j] < (uint32_t)q.E && keep[j]) atomicAdd(hist + e[j], 1);
   }
   if (q.mask) {
     int n = 0;
@@ -220,42 +277,36 @@ __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int 
   }
 }
 
-__device__ __forceinline__ float count_scale(const BalanceParams& q, int n) {
-  return n > 0 ? (float)q.E / ((float)q.k * (float)n) : 0.f;
-}
-__device__ __forceinline__ float grad_scale(const BalanceParams& q, int g, int n) {
-  return n > 0 ? (q.grad_loss ? q.grad_loss[g] : 1.f) * q.coef / (float)n : 0.f;
-}
-
 // One workgroup per group: counts, rows, means and loss.
-template <int L, bool VEC, typename T>
-__global__ __launch_bounds__(kSmallThreads) void balance_group_kernel(BalanceParams q) {
+template <int L, bool VEC, bool FEW, int THREADS, typename T>
+__global__ __launch_bounds__(THREADS) void balance_group_kernel(BalanceParams q) {
   __shared__ int hist[MIRA_MAX_EXPERTS];
   __shared__ int kept;
-  __shared__ float wave_sums[kSmallThreads / 64][MIRA_MAX_EXPERTS];
-  __shared__ float part[kSmallThreads / 64];
+  __shared__ float wave_sums[THREADS / 64][MIRA_MAX_EXPERTS];
+  __shared__ float part[THREADS / 64];
   const int g = blockIdx.x, t = threadIdx.x, l = t % L;
   const Segment s = group_rows(q, g);
-  for (int e = t; e < q.E; e += kSmallThreads) hist[e] = 0;
+  for (int e = t; e < q.E; e += THREADS) hist[e] = 0;
   if (t == 0) kept = 0;
   __syncthreads();
-  count_pairs<kSmallThreads>(q, s.lo, s.hi, hist, &kept);
+  count_pairs<THREADS>(q, s.lo, s.hi, hist, &kept);
   __syncthreads();
   const int n = q.mask ? kept : s.hi - s.lo;
   const float cs = count_scale(q, n);
-  float f[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
+  int counts[4];
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int e = expert_of<L, VEC>(l, i);
-    f[i] = e < q.E ? (float)hist[e] * cs : 0.f;
+    counts[i] = e < q.E ? hist[e] : 0;
   }
-  rows_pass<L, VEC, 2, T>(q, s.lo + t / L, s.hi, kSmallThreads / L, l, f, grad_scale(q, g, n), acc);
-  reduce_groups<L, VEC, kSmallThreads>(acc, q.E, wave_sums);
+  rows_pass<L, VEC, FEW, 2, T>(q, s.lo + t / L, s.hi, THREADS / L, l, counts, n, group_grad(q, g), acc);
+  reduce_groups<L, VEC, THREADS>(acc, q.E, wave_sums);
   __syncthreads();
   float term = 0.f;
-  for (int e = t; e < q.E; e += kSmallThreads) {
+  for (int e = t; e < q.E; e += THREADS) {
     float sum = 0.f;
-    for (int w = 0; w < kSmallThreads / 64; ++w) sum += wave_sums[w][e];
+    for (int w = 0; w < THREADS / 64; ++w) sum += wave_sums[w][e];
     const float mean = n > 0 ? sum / (float)n : 0.f;
     if (q.mean) q.mean[(size_t)g * q.E + e] = mean;
     q.counts[(size_t)g * q.E + e] = hist[e];
@@ -266,39 +317,166 @@ __global__ __launch_bounds__(kSmallThreads) void balance_group_kernel(BalancePar
   __syncthreads();
   if (t == 0 && q.loss) {
     float sum = 0.f;
-    for (int w = 0; w < kSmallThreads / 64; ++w) sum += part[w];
+    for (int w = 0; w < THREADS / 64; ++w) sum += part[w];
     q.loss[g] = q.coef * sum;
   }
 }
 
-// ---- many logits: zero, count, rows, finish ---------------------------------
+// ---- many logits ----------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void balance_zero_kernel(int32_t* counts, size_t n, int32_t* kept, int G) {
+__global__ __launch_bounds__(256) void balance_zero_kernel(int32_t* counts, size_t n, int32_t* kept, int32_t* ended, int G) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ended = 0;
   const size_t i0 = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
   for (size_t i = i0; i < n; i += step) counts[i] = 0;
   for (size_t i = i0; i < (size_t)G; i += step) kept[i] = 0;
 }
 
-// Walks the groups that rows [lo, hi) meet: f(g, first row, end row).
+// Few pairs: one workgroup per group counts them, no zeros and no second pass.
+__global__ __launch_bounds__(kBigThreads) void balance_count_group_kernel(BalanceParams q) {
+  __shared__ int hist[MIRA_MAX_EXPERTS];
+  __shared__ int kept;
+  const int g = blockIdx.x;
+  const Segment s = group_rows(q, g);
+  for (int e = threadIdx.x; e < q.E; e += kBigThreads) hist[e] = 0;
+  if (threadIdx.x == 0) kept = 0;
+  __syncthreads();
+  count_pairs<kBigThreads>(q, s.lo, s.hi, hist, &kept);
+  __syncthreads();
+  for (int e = threadIdx.x; e < q.E; e += kBigThreads) q.counts[(size_t)g * q.E + e] = hist[e];
+  if (threadIdx.x == 0) {
+    q.kept[g] = kept;
+    if (g == 0) *q.ended = 0;
+  }
+}
+
+// Walks the groups that rows [lo, hi) meet, upwards: f(g, the group's rows, first
+// row, end row).  The whole workgroup looks at all offsets at once for the group
+// that holds a row; a search would wait for memory at every step.
 template <typename F>
 __device__ __forceinline__ void for_groups(const BalanceParams& q, int lo, int hi, F&& f) {
-  int g = max(group_of(q, lo), 0);
-  while (g < q.G) {
-    const Segment s = group_rows(q, g);
-    if (s.lo >= hi) break;
-    const int a = max(s.lo, lo), b = min(s.hi, hi);
-    if (a < b) f(g, a, b);
-    if (s.hi >= hi) break;
-    // the next group that holds a row (empty ones are passed over); always upwards
-    g = max(g + 1, group_of(q, s.hi));
+  if (!q.offsets) {
+    if (lo < hi) f(0, Segment{0, q.T}, lo, hi);
+    return;
   }
+  __shared__ int found[3];
+  int row = lo, above = -1;
+  while (true) {
+    __syncthreads();
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    row = max(row, min(max(q.offsets[0], 0), q.T));
+    for (int i = threadIdx.x; i < q.G; i += blockDim.x) {
+      const Segment s = group_rows(q, i);
+      if (s.lo <= row && row < s.hi) {  // one group, where the offsets ascend
+        found[0] = i;
+        found[1] = s.lo;
+        found[2] = s.hi;
+      }
+    }
+    __syncthreads();
+    const int g = found[0];
+    const Segment s{found[1], found[2]};
+    // (none: past the last group; not above the last one: offsets that do not ascend)
+    if (row >= hi || g <= above || s.lo > row || s.hi <= row) return;
+    f(g, s, row, min(s.hi, hi));
+    above = g;
+    row = s.hi;
+    if (row >= hi) return;
+  }
+}
+
+// Means and loss of a group from its chunks' sums: thread (e, part) adds every
+// parts-th slot in order, then the parts are added in order.  The sums come from
+// workgroups on other XCDs: both sides use agent-scope accesses, which pass the
+// XCDs' own L2, and the writers wait for theirs to arrive before they count their
+// chunk as ended.  (Agent-scope fences instead write all of an L2 back, the
+// gradient's lines with it: 131072 x 256 took 137 us so, 75 us like this.)
+__device__ __forceinline__ void finish_group(const BalanceParams& q, int g, const Segment& s, int n, float* sums) {
+  int width = 1;
+  while (width < q.E) width *= 2;
+  const int t = threadIdx.x, e = t % width, part = t / width, parts = kBigThreads / width;
+  float sum = 0.f;
+  if (e < q.E && s.lo < s.hi) {
+    const int c0 = s.lo / q.chunk_rows, c1 = (s.hi - 1) / q.chunk_rows;
+    for (int c = c0 + part; c <= c1; c += 32 * parts) {  // 32 loads in flight, added in order
+      float v[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        v[i] = __hip_atomic_load(q.partial + (size_t)(min(c + i * parts, c1) + g) * q.E + e, __ATOMIC_RELAXED,
+                                 __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) sum += c + i * parts <= c1 ? v[i] : 0.f;
+    }
+  }
+  __syncthreads();
+  sums[t] = sum;
+  __syncthreads();
+  float term = 0.f;
+  if (part == 0 && e < q.E) {
+    for (int i = 1; i < parts; ++i) sum += sums[i * width + e];
+    const float mean = n > 0 ? sum / (float)n : 0.f;
+    if (q.mean) q.mean[(size_t)g * q.E + e] = mean;
+    term = (float)q.counts[(size_t)g * q.E + e] * count_scale(q, n) * mean;
+  }
+  __syncthreads();
+  term = wave_sum(term);
+  if ((t & 63) == 0) sums[t >> 6] = term;
+  __syncthreads();
+  if (t == 0 && q.loss) {
+    float total = 0.f;
+    for (int w = 0; w < kBigThreads / 64; ++w) total += sums[w];
+    q.loss[g] = q.coef * total;
+  }
+}
+
+template <int L, bool VEC, bool FEW, typename T>
+__global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams q) {
+  __shared__ float wave_sums[kBigThreads / 64][MIRA_MAX_EXPERTS];
+  __shared__ int last;
+  const int t = threadIdx.x, l = t % L;
+  const int lo = blockIdx.x * q.chunk_rows, hi = min(lo + q.chunk_rows, q.T);
+  for_groups(q, lo, hi, [&](int g, Segment s, int a, int b) {
+    int counts[4];
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    const int n = q.mask ? q.kept[g] : s.hi - s.lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = expert_of<L, VEC>(l, i);
+      counts[i] = q.counts[(size_t)g * q.E + min(e, q.E - 1)];
+    }
+    rows_pass<L, VEC, FEW, 2, T>(q, a + t / L, b, kBigThreads / L, l, counts, n, group_grad(q, g), acc);
+    if (!q.mean && !q.loss) return;
+    __syncthreads();
+    reduce_groups<L, VEC, kBigThreads>(acc, q.E, wave_sums);
+    __syncthreads();
+    for (int e = t; e < q.E; e += kBigThreads) {
+      float sum = 0.f;
+      for (int w = 0; w < kBigThreads / 64; ++w) sum += wave_sums[w][e];
+      __hip_atomic_store(q.partial + (size_t)(blockIdx.x + g) * q.E + e, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  });
+  if (q.offsets || (!q.mean && !q.loss)) return;
+  // One group: the last chunk to end finishes it.  (The sums have arrived when the
+  // counter of stores in flight is zero.)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (t == 0)
+    last = __hip_atomic_fetch_add(q.ended, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (last) finish_group(q, 0, Segment{0, q.T}, q.mask ? q.kept[0] : q.T, &wave_sums[0][0]);
+}
+
+__global__ __launch_bounds__(kBigThreads) void balance_finish_kernel(BalanceParams q) {
+  __shared__ float sums[kBigThreads];
+  const Segment s = group_rows(q, blockIdx.x);
+  finish_group(q, blockIdx.x, s, q.mask ? q.kept[blockIdx.x] : s.hi - s.lo, sums);
 }
 
 __global__ __launch_bounds__(kBigThreads) void balance_count_kernel(BalanceParams q) {
   __shared__ int hist[MIRA_MAX_EXPERTS];
   __shared__ int kept;
   const int lo = blockIdx.x * q.chunk_rows, hi = min(lo + q.chunk_rows, q.T);
-  for_groups(q, lo, hi, [&](int g, int a, int b) {
+  for_groups(q, lo, hi, [&](int g, Segment, int a, int b) {
     for (int e = threadIdx.x; e < q.E; e += kBigThreads) hist[e] = 0;
     if (threadIdx.x == 0) kept = 0;
     __syncthreads();
@@ -312,96 +490,65 @@ __global__ __launch_bounds__(kBigThreads) void balance_count_kernel(BalanceParam
   });
 }
 
-template <int L, bool VEC, typename T>
-__global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams q) {
-  __shared__ float wave_sums[kBigThreads / 64][MIRA_MAX_EXPERTS];
-  const int t = threadIdx.x, l = t % L;
-  const int lo = blockIdx.x * q.chunk_rows, hi = min(lo + q.chunk_rows, q.T);
-  for_groups(q, lo, hi, [&](int g, int a, int b) {
-    const Segment s = group_rows(q, g);
-    const int n = q.mask ? q.kept[g] : s.hi - s.lo;
-    const float cs = count_scale(q, n);
-    float f[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = expert_of<L, VEC>(l, i);
-      f[i] = e < q.E ? (float)q.counts[(size_t)g * q.E + e] * cs : 0.f;
-    }
-    rows_pass<L, VEC, 4, T>(q, a + t / L, b, kBigThreads / L, l, f, grad_scale(q, g, n), acc);
-    reduce_groups<L, VEC, kBigThreads>(acc, q.E, wave_sums);
-    __syncthreads();
-    for (int e = t; e < q.E; e += kBigThreads) {
-      float sum = 0.f;
-      for (int w = 0; w < kBigThreads / 64; ++w) sum += wave_sums[w][e];
-      q.partial[(size_t)(blockIdx.x + g) * q.E + e] = sum;
-    }
-    __syncthreads();
-  });
-}
-
-// Means and loss of a group from its chunks' sums: thread (e, part) adds every
-// parts-th slot in order, then the parts are added in order.
-__global__ __launch_bounds__(kBigThreads) void balance_finish_kernel(BalanceParams q, int width) {
-  __shared__ float sums[kBigThreads];
-  __shared__ float part_loss[kBigThreads / 64];
-  const int g = blockIdx.x, t = threadIdx.x, e = t % width, part = t / width, parts = kBigThreads / width;
-  const Segment s = group_rows(q, g);
-  const int n = q.mask ? q.kept[g] : s.hi - s.lo;
-  float sum = 0.f;
-  if (e < q.E && s.lo < s.hi) {
-    const int c1 = (s.hi - 1) / q.chunk_rows;
-    for (int c = s.lo / q.chunk_rows + part; c <= c1; c += parts) sum += q.partial[(size_t)(c + g) * q.E + e];
-  }
-  sums[t] = sum;
-  __syncthreads();
-  float term = 0.f;
-  if (part == 0 && e < q.E) {
-    for (int i = 1; i < parts; ++i) sum += sums[i * width + e];
-    const float mean = n > 0 ? sum / (float)n : 0.f;
-    if (q.mean) q.mean[(size_t)g * q.E + e] = mean;
-    term = (float)q.counts[(size_t)g * q.E + e] * count_scale(q, n) * mean;
-  }
-  term = wave_sum(term);
-  if ((t & 63) == 0) part_loss[t >> 6] = term;
-  __syncthreads();
-  if (t == 0 && q.loss) {
-    float total = 0.f;
-    for (int w = 0; w < kBigThreads / 64; ++w) total += part_loss[w];
-    q.loss[g] = q.coef * total;
-  }
-}
-
 struct BalanceLayout {
-  size_t counts, kept, partial, total;
+  size_t counts, kept, ended, partial, total;
 };
 BalanceLayout balance_layout(int E, int G) {
   BalanceLayout w;
   w.counts = 0;
   w.kept = align_up((size_t)G * E * 4, 256);
-  w.partial = w.kept + align_up((size_t)G * 4, 256);
+  w.ended = w.kept + align_up((size_t)G * 4, 256);
+  w.partial = w.ended + 256;
   w.total = w.partial + align_up((size_t)(kMaxChunks + G) * E * 4, 256);
   return w;
 }
 
-template <int L, bool VEC, typename T>
+template <int L, bool VEC, bool FEW, typename T>
 void launch_rows(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
-  if (small)
-    launch_timed("balance_group", balance_group_kernel<L, VEC, T>, dim3(q.G), dim3(kSmallThreads), 0, st, q);
+  // a group of more than one pass of 256 threads gets a larger workgroup
+  if (small && (size_t)q.T * L <= (size_t)q.G * 256)
+    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, 256, T>, dim3(q.G), dim3(256), 0, st, q);
+  else if (small)
+    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, kBigThreads, T>, dim3(q.G), dim3(kBigThreads), 0, st, q);
   else
-    launch_timed("balance_rows", balance_rows_kernel<L, VEC, T>, dim3(chunks), dim3(kBigThreads), 0, st, q);
+    launch_timed("balance_rows", balance_rows_kernel<L, VEC, FEW, T>, dim3(chunks), dim3(kBigThreads), 0, st, q);
 }
 
-template <bool VEC, typename T>
-void launch_lanes(const BalanceParams& q, int lanes, bool small, int chunks, hipStream_t st) {
-  switch (lanes) {
-    case 1: return launch_rows<1, VEC, T>(q, small, chunks, st);
-    case 2: return launch_rows<2, VEC, T>(q, small, chunks, st);
-    case 4: return launch_rows<4, VEC, T>(q, small, chunks, st);
-    case 8: return launch_rows<8, VEC, T>(q, small, chunks, st);
-    case 16: return launch_rows<16, VEC, T>(q, small, chunks, st);
-    case 32: return launch_rows<32, VEC, T>(q, small, chunks, st);
-    default: return launch_rows<64, VEC, T>(q, small, chunks, st);
+// Lanes of a row: the largest power of two up to E for few experts, else the
+// smallest of four values a lane.
+int row_lanes(int E) {
+  int lanes = 1;
+  if (E <= kFewExperts)
+    while (lanes * 2 <= E) lanes *= 2;
+  else
+    while (lanes * 4 < E) lanes *= 2;
+  return lanes;
+}
+
+template <typename T>
+void launch_few(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
+  switch (row_lanes(q.E)) {
+    case 1: return launch_rows<1, false, true, T>(q, small, chunks, st);
+    case 2: return launch_rows<2, false, true, T>(q, small, chunks, st);
+    case 4: return launch_rows<4, false, true, T>(q, small, chunks, st);
+    default: return launch_rows<8, false, true, T>(q, small, chunks, st);
   }
+}
+template <bool VEC, typename T>
+void launch_many(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
+  switch (row_lanes(q.E)) {
+    case 4: return launch_rows<4, VEC, false, T>(q, small, chunks, st);
+    case 8: return launch_rows<8, VEC, false, T>(q, small, chunks, st);
+    case 16: return launch_rows<16, VEC, false, T>(q, small, chunks, st);
+    case 32: return launch_rows<32, VEC, false, T>(q, small, chunks, st);
+    default: return launch_rows<64, VEC, false, T>(q, small, chunks, st);
+  }
+}
+template <typename T>
+void launch_typed(const BalanceParams& q, bool vec, bool small, int chunks, hipStream_t st) {
+  if (q.E <= kFewExperts) launch_few<T>(q, small, chunks, st);
+  else if (vec) launch_many<true, T>(q, small, chunks, st);
+  else launch_many<false, T>(q, small, chunks, st);
 }
 
 }  // namespace
@@ -422,6 +569,7 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
   q.kept = (int32_t*)(ws + w.kept);
   q.mean = a.mean_prob;
   q.loss = a.loss;
+  q.ended = (int32_t*)(ws + w.ended);
   q.partial = (float*)(ws + w.partial);
   q.ld_x = a.ld_logits ? a.ld_logits : a.n_experts;
   q.ld_d = a.ld_dlogits ? a.ld_dlogits : a.n_experts;
@@ -430,8 +578,7 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
   q.k = a.top_k;
   q.G = a.n_groups;
   q.coef = a.coef;
-  int lanes = 1;
-  while (lanes * 4 < q.E) lanes *= 2;
+  const int lanes = row_lanes(q.E);
   const size_t esz = a.logits_dtype == MIRA_F32 ? 4 : 2;
   const bool vec = q.E % 4 == 0 && q.ld_x % 4 == 0 && (uintptr_t)q.logits % (4 * esz) == 0 &&
                    (!q.dlogits || (q.ld_d % 4 == 0 && (uintptr_t)q.dlogits % (4 * esz) == 0));
@@ -442,23 +589,19 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
     const int rows = kBigThreads / lanes;
     q.chunk_rows = (int)align_up((size_t)(q.T + kMaxChunks - 1) / kMaxChunks, rows);
     chunks = (q.T + q.chunk_rows - 1) / q.chunk_rows;
-    const size_t n = (size_t)q.G * q.E;
-    const int zb = (int)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024);
-    launch_timed("balance_zero", balance_zero_kernel, dim3(zb), dim3(256), 0, st, q.counts, n, q.kept, q.G);
-    launch_timed("balance_count", balance_count_kernel, dim3(chunks), dim3(kBigThreads), 0, st, q);
+    if ((size_t)q.T * q.k <= (q.G > 1 ? 4 : 1) * kFewPairs) {
+      launch_timed("balance_count", balance_count_group_kernel, dim3(q.G), dim3(kBigThreads), 0, st, q);
+    } else {
+      const size_t n = (size_t)q.G * q.E;
+      const int zb = (int)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024);
+      launch_timed("balance_zero", balance_zero_kernel, dim3(zb), dim3(256), 0, st, q.counts, n, q.kept, q.ended, q.G);
+      launch_timed("balance_count", balance_count_kernel, dim3(chunks), dim3(kBigThreads), 0, st, q);
+    }
   }
-  if (a.logits_dtype == MIRA_F32) {
-    if (vec) launch_lanes<true, float>(q, lanes, small, chunks, st);
-    else launch_lanes<false, float>(q, lanes, small, chunks, st);
-  } else {
-    if (vec) launch_lanes<true, uint16_t>(q, lanes, small, chunks, st);
-    else launch_lanes<false, uint16_t>(q, lanes, small, chunks, st);
-  }
-  if (!small) {
-    int width = 1;
-    while (width < q.E) width *= 2;
-    launch_timed("balance_finish", balance_finish_kernel, dim3(q.G), dim3(kBigThreads), 0, st, q, width);
-  }
+  if (a.logits_dtype == MIRA_F32) launch_typed<float>(q, vec, small, chunks, st);
+  else launch_typed<uint16_t>(q, vec, small, chunks, st);
+  if (!small && q.offsets && (q.mean || q.loss))
+    launch_timed("balance_finish", balance_finish_kernel, dim3(q.G), dim3(kBigThreads), 0, st, q);
   return hipGetLastError();
 }
 

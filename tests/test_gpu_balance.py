@@ -258,3 +258,22 @@ def test_offsets_that_do_not_ascend_stay_inside():
             c = Case(T, 8, 2, 3, tweak=tweak)
             c.run()
             assert (c.out["dlogits"].shape[0] == T)
+
+
+@pytest.mark.parametrize("E", [2, 3, 5, 8])
+@pytest.mark.parametrize("T,dt", [(37, "f32"), (20000, "f32"), (20000, "bf16")])
+def test_all_experts_selected(E, T, dt):
+    """Every expert selected by every token: f is 1 throughout and the gradient is
+    zero but for roundings, which are those of the formula evaluated step by step
+    in fp32 (elementwise, by torch)."""
+    c = Case(T, E, E, 1, dt)
+    got = c.run()["dlogits"][:T, :E]
+    x = c.logits[:T, :E].float()
+    e = torch.exp(x - x.amax(1, keepdim=True))
+    p = e / e.sum(1, keepdim=True)
+    n = torch.full((1,), float(T), device="cuda")
+    f = torch.full((E,), float(T), device="cuda") * ((E * n) .reciprocal() * E)
+    d = (c.dev["gl"] * c.coef / n) * p * (f - (f * p).sum(1, keepdim=True))
+    # nothing larger than the roundings of w = sum f p (E + 3 of them) times the scale
+    assert float(got.double().abs().max()) <= (E + 3) * 2 * U32 * float(c.gl[0]) * c.coef / T
+    assert torch.equal(got, d.to(got.dtype))

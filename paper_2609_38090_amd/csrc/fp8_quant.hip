@@ -56,12 +56,35 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.f + e) * u;
 }
 
-__device__ __forceinline__ void load8_act(const float* p, float v[8]) {
-  load4_act(p, v);
-  load4_act(p + 4, v + 4);
+// Vectors at the alignment of their elements: global loads take any, so rows of
+// every length and start load 16 bytes at a time.
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef int v2i_any __attribute__((ext_vector_type(2), aligned(2)));
+
+__device__ __forceinline__ void load_n(const float* p, float (&v)[4]) {
+  const v4f q = *(const v4f_any*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = q[i];
 }
-__device__ __forceinline__ void load8_act(const uint16_t* p, float v[8]) {
-  const v4i q = ld16(p);
+__device__ __forceinline__ void load_n(const uint16_t* p, float (&v)[4]) {
+  const v2i_any q = *(const v2i_any*)p;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] = __uint_as_float((uint32_t)q[i] << 16);
+    v[2 * i + 1] = __uint_as_float((uint32_t)q[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load_n(const float* p, float (&v)[8]) {
+  const v4f a = *(const v4f_any*)p, b = *(const v4f_any*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
+}
+__device__ __forceinline__ void load_n(const uint16_t* p, float (&v)[8]) {
+  const v4i q = *(const v4i_any*)p;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = __uint_as_float((uint32_t)q[i] << 16);
@@ -69,20 +92,19 @@ __device__ __forceinline__ void load8_act(const uint16_t* p, float v[8]) {
   }
 }
 
-// Eight values of row `row` from column c on; those from cols on are 0.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int cols, float v[8]) {
-  if (VEC && c + 8 <= cols) {
-    load8_act(row + c, v);
+// N values of a row from column c on; those from cols on are 0.
+template <int N, typename T>
+__device__ __forceinline__ void load_cols(const T* row, int c, int cols, float (&v)[N]) {
+  if (c + N <= cols) {
+    load_n(row + c, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? load_act(row, c + i) : 0.f;
+    for (int i = 0; i < N; ++i) v[i] = c + i < cols ? load_act(row, c + i) : 0.f;
   }
 }
 
-// 1 x 128 blocks: 16 lanes hold a block, eight values each.  VEC: rows of x (and
-// up's part of them) start aligned to 16 bytes.
-template <bool SWIGLU, bool VEC, typename T>
+// 1 x 128 blocks: 16 lanes hold a block, eight values each.
+template <bool SWIGLU, typename T>
 __global__ __launch_bounds__(256) void fp8_quant_rows_kernel(QuantParams p, int nb) {
   const size_t block = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   const size_t total = (size_t)p.rows * nb;
@@ -91,10 +113,10 @@ __global__ __launch_bounds__(256) void fp8_quant_rows_kernel(QuantParams p, int 
   const int b = (int)(block - r * nb), c = b * 128 + (threadIdx.x & 15) * 8;
   const T* row = (const T*)p.x + r * p.ldx;
   float v[8];
-  load8<VEC>(row, c, p.cols, v);
+  load_cols(row, c, p.cols, v);
   if constexpr (SWIGLU) {
     float u[8];
-    load8<VEC>(row + p.cols, c, p.cols, u);
+    load_cols(row + p.cols, c, p.cols, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = swiglu(v[i], u[i]);
   }
@@ -117,7 +139,7 @@ __global__ __launch_bounds__(256) void fp8_quant_rows_kernel(QuantParams p, int 
 // thread t columns 4 (t % 32) .. +3 of rows 4 (t / 32 + 8 j) .. +3, j < 4.  The
 // transposed copy turns each 4 x 4 square of bytes with byte permutes and
 // goes through LDS to rows of 16 bytes.
-template <bool VEC, typename T>
+template <typename T>
 __global__ __launch_bounds__(256) void fp8_quant_blocks_kernel(QuantParams p, int nb) {
   __shared__ float wave_m[4];
   __shared__ uint32_t turned[128][33];  // [column][row / 4], padded against bank conflicts
@@ -132,13 +154,7 @@ __global__ __launch_bounds__(256) void fp8_quant_blocks_kernel(QuantParams p, in
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = br * 128 + (rg + 8 * j) * 4 + i;
-      if (r < p.rows && VEC && c + 4 <= p.cols) {
-        load4_act(x + (size_t)r * p.ldx + c, v[j][i]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[j][i][e] = r < p.rows && c + e < p.cols ? load_act(x, (size_t)r * p.ldx + c + e) : 0.f;
-      }
+      load_cols(x + (size_t)min(r, p.rows - 1) * p.ldx, r < p.rows ? c : p.cols, p.cols, v[j][i]);
     }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -193,23 +209,17 @@ __global__ __launch_bounds__(256) void fp8_quant_blocks_kernel(QuantParams p, in
 
 template <typename T>
 void launch_quant(const mira_fp8_quant_args& a, const QuantParams& p, hipStream_t st) {
-  constexpr size_t kEach = 16 / sizeof(T);
-  const bool vec = p.ldx % kEach == 0 && (uintptr_t)p.x % 16 == 0 && (!(a.flags & MIRA_FP8_SWIGLU) || p.cols % kEach == 0);
   const int nb = (p.cols + 127) / 128;
   if (a.block_rows == 128) {
     const dim3 grid((uint32_t)nb * ((p.rows + 127) / 128));
-    if (vec) launch_timed("fp8_quant_blocks", fp8_quant_blocks_kernel<true, T>, grid, dim3(256), 0, st, p, nb);
-    else launch_timed("fp8_quant_blocks", fp8_quant_blocks_kernel<false, T>, grid, dim3(256), 0, st, p, nb);
+    launch_timed("fp8_quant_blocks", fp8_quant_blocks_kernel<T>, grid, dim3(256), 0, st, p, nb);
     return;
   }
   const dim3 grid((uint32_t)(((size_t)p.rows * nb + 15) / 16));
-  if (a.flags & MIRA_FP8_SWIGLU) {
-    if (vec) launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<true, true, T>, grid, dim3(256), 0, st, p, nb);
-    else launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<true, false, T>, grid, dim3(256), 0, st, p, nb);
-  } else {
-    if (vec) launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<false, true, T>, grid, dim3(256), 0, st, p, nb);
-    else launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<false, false, T>, grid, dim3(256), 0, st, p, nb);
-  }
+  if (a.flags & MIRA_FP8_SWIGLU)
+    launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<true, T>, grid, dim3(256), 0, st, p, nb);
+  else
+    launch_timed("fp8_quant_rows", fp8_quant_rows_kernel<false, T>, grid, dim3(256), 0, st, p, nb);
 }
 
 }  // namespace

@@ -118,6 +118,9 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(N) : "memory");
 }
 
+// All LDS reads have returned, in every wave.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 struct Tile {
   int g, m0, m1, nt, part;  // group, rows [m0, m1), tile of weight rows, part of the contraction
 };
@@ -431,7 +434,46 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     step();
   }
 
+  // A lane holds four columns of a row: stored from here, a wave's stores are pieces
+  // of 32 bytes (bf16).  Through LDS, which the stages no longer need, they are whole
+  // rows of the wave's tile, 16 bytes a lane (chunk c of row r at c ^ (r % chunks)).
   OutT* out = (OutT*)p.out;
+  constexpr int kRowBytes = NT * 32, kChunks = kRowBytes / 16;
+  static_assert(W * MT * 16 * kRowBytes <= NS * kStage, "the tile's rows fit the ring");
+  if (sizeof(OutT) == 2 && !p.part && p.ldo % 8 == 0 && ((uintptr_t)out & 15) == 0) {
+    lds_barrier();  // every wave has read its last stage
+    char* mine = lds + wave * (MT * 16 * kRowBytes);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const int m = t.m0 + wm * (MT * 16) + j * 16 + r16;
+      const bool none = p.order && m < t.m1 && source_row(p, m) < 0;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        uint16_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_out(h + e, none ? 0.f : acc[i][j][e]);
+        *(uint2*)(mine + (j * 16 + r16) * kRowBytes + (((i * 2 + (kg >> 1)) ^ (r16 & (kChunks - 1))) << 4) + (kg & 1) * 8) =
+            uint2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < (MT * 16 * kChunks + 63) / 64; ++q) {
+      const int at = q * 64 + lane, row = at / kChunks, c = at % kChunks;
+      if (row >= MT * 16) continue;
+      const int m = t.m0 + wm * (MT * 16) + row, n = n0 + wn * (NT * 16) + c * 8;
+      const v4i v = *(const v4i*)(mine + row * kRowBytes + ((c ^ (row & (kChunks - 1))) << 4));
+      if (m >= t.m1 || n >= p.N) continue;
+      uint16_t* o = (uint16_t*)out + (size_t)m * p.ldo + n;
+      if (n + 8 <= p.N) {
+        *(v4i*)o = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < p.N) o[e] = (uint16_t)((uint32_t)v[e >> 1] >> (16 * (e & 1)));
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
     const int m = t.m0 + wm * (MT * 16) + j * 16 + r16;

@@ -359,25 +359,31 @@ __device__ __forceinline__ void for_groups(const BalanceParams& q, int lo, int h
     return;
   }
   __shared__ int found[3];
-  int row = lo, above = -1;
+  int row = lo, above = -1, g = -1;
+  Segment s{0, 0};
   while (true) {
-    __syncthreads();
-    if (threadIdx.x == 0) found[0] = -1;
-    __syncthreads();
-    row = max(row, min(max(q.offsets[0], 0), q.T));
-    for (int i = threadIdx.x; i < q.G; i += blockDim.x) {
-      const Segment s = group_rows(q, i);
-      if (s.lo <= row && row < s.hi) {  // one group, where the offsets ascend
-        found[0] = i;
-        found[1] = s.lo;
-        found[2] = s.hi;
+    if (g >= 0 && g + 1 < q.G) s = group_rows(q, g + 1);  // mostly the next one
+    if (g >= 0 && g + 1 < q.G && s.lo <= row && row < s.hi) {
+      ++g;
+    } else {
+      __syncthreads();
+      if (threadIdx.x == 0) found[0] = -1;
+      __syncthreads();
+      row = max(row, min(max(q.offsets[0], 0), q.T));
+      for (int i = threadIdx.x; i < q.G; i += blockDim.x) {
+        const Segment at = group_rows(q, i);
+        if (at.lo <= row && row < at.hi) {  // one group, where the offsets ascend
+          found[0] = i;
+          found[1] = at.lo;
+          found[2] = at.hi;
+        }
       }
+      __syncthreads();
+      g = found[0];
+      s = Segment{found[1], found[2]};
+      // (none: past the last group; not above the last one: offsets that do not ascend)
+      if (row >= hi || g <= above || s.lo > row || s.hi <= row) return;
     }
-    __syncthreads();
-    const int g = found[0];
-    const Segment s{found[1], found[2]};
-    // (none: past the last group; not above the last one: offsets that do not ascend)
-    if (row >= hi || g <= above || s.lo > row || s.hi <= row) return;
     f(g, s, row, min(s.hi, hi));
     above = g;
     row = s.hi;
@@ -582,7 +588,11 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
   const size_t esz = a.logits_dtype == MIRA_F32 ? 4 : 2;
   const bool vec = q.E % 4 == 0 && q.ld_x % 4 == 0 && (uintptr_t)q.logits % (4 * esz) == 0 &&
                    (!q.dlogits || (q.ld_d % 4 == 0 && (uintptr_t)q.dlogits % (4 * esz) == 0));
-  const bool small = (size_t)q.T * q.E <= 32768;
+  // One workgroup per group: few logits, or many groups of few logits (1000 rows of
+  // 256 experts in 500 groups: 6.5 us so, 37 by chunks that walk the groups; kept to
+  // 2^20 logits, where one group of nearly all of them costs some 150 us).
+  const size_t logits = (size_t)q.T * q.E;
+  const bool small = logits <= 32768 || (logits <= (size_t)q.G * 8192 && logits <= 1u << 20);
   int chunks = 0;
   if (!small) {
     // whole passes of the workgroup's lane groups, at most kMaxChunks chunks

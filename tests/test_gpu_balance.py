@@ -97,7 +97,8 @@ class Case:
 
 SIZES = [(1, 1, 1, 1), (1, 8, 2, 1), (16, 8, 2, 1), (7, 3, 2, 1), (40, 61, 4, 5), (300, 256, 8, 1), (129, 255, 16, 9),
          (2048, 64, 6, 1), (3001, 60, 4, 37), (5000, 7, 2, 3), (9000, 4, 1, 1), (2500, 128, 8, 700), (1500, 32, 8, 2),
-         (700, 200, 3, 2), (40000, 2, 2, 5), (33000, 1, 1, 1), (1030, 100, 6, 1), (513, 252, 8, 3)]
+         (700, 200, 3, 2), (40000, 2, 2, 5), (33000, 1, 1, 1), (1030, 100, 6, 1), (513, 252, 8, 3),
+         (20000, 64, 2, 300), (4097, 129, 3, 512)]
 
 
 @pytest.mark.parametrize("T,E,k,G", SIZES)
@@ -277,3 +278,32 @@ def test_all_experts_selected(E, T, dt):
     # nothing larger than the roundings of w = sum f p (E + 3 of them) times the scale
     assert float(got.double().abs().max()) <= (E + 3) * 2 * U32 * float(c.gl[0]) * c.coef / T
     assert torch.equal(got, d.to(got.dtype))
+
+
+@pytest.mark.parametrize("T,G", [(3000, 200), (30000, 200)])
+def test_one_group_of_nearly_all_rows(T, G):
+    """Both ways of sharing the work, with runs of empty groups on both sides."""
+    def tweak(c, x, rng):
+        c.off = np.concatenate([np.full(G // 2, 2), np.full(G // 2 - 10, T - 20), np.arange(T - 20, T + 1, 2)]).astype(np.int32)
+        assert len(c.off) == G + 1
+    c = Case(T, 64, 2, G, masked=True, tweak=tweak)
+    c.run()
+    c.check()
+
+
+def test_two_streams_at_once():
+    """Calls on their own workspaces and outputs, in flight together."""
+    cases = [Case(T, 64, 4, G, seed=i) for i, (T, G) in enumerate(((20000, 1), (20000, 300), (300, 5)))]
+    want = [{k: v.clone() for k, v in c.run().items()} for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        for c in cases:
+            for v in c.out.values():
+                v.fill_(3)
+            c.out["dlogits"].fill_(5.0)
+        torch.cuda.synchronize()
+        for c, st in zip(cases, streams):
+            mira.mira_balance_loss(c.args, st)
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert all(torch.equal(c.out[k], w[k]) for k in w)

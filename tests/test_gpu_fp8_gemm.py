@@ -251,3 +251,36 @@ def test_input_gradient_through_the_transposed_copy(M, N, K):
         diff = ((dy * ((x + e) @ w.t())).sum() - (dy * ((x - e) @ w.t())).sum())
         tol = gemm_bound(mag, N, False, want)[i, j] + 4 * N * M * K * 2.0 ** -52 * float((dy.abs() * (x.abs() @ w.abs().t())).max())
         assert abs(float(dx[i, j]) - float(diff)) <= float(tol)
+
+
+def test_two_streams_at_once():
+    """Calls of every tile shape and of parts, each on its own buffers, in flight together."""
+    cases = [Case(M, N, K, out) for M, N, K, out in ((2050, 4096, 300, "bf16"), (40, 300, 9000, "f32"), (600, 1000, 700, "f32"), (3, 5000, 900, "bf16"))]
+    want = [c.run().clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        for c in cases:
+            c.out.fill_(-77.0)
+        torch.cuda.synchronize()
+        for c, st in zip(cases, streams):
+            mira.mira_fp8_gemm(c.args, st)
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert torch.equal(c.out, w)
+
+
+@pytest.mark.parametrize("M,N,K", [(37, 77, 300), (600, 514, 700)])
+@pytest.mark.parametrize("shift", [1, 2, 3, 8])
+def test_out_of_any_alignment(M, N, K, shift):
+    """out starting `shift` elements past an aligned address, rows of odd length."""
+    for out in ("bf16", "f32"):
+        c = Case(M, N, K, out, pads=(0, 0, 0, 0, 3))
+        c.run()
+        want = c.out[:M, :N].clone()
+        flat = torch.full((M * (N + 3) + 16,), -5.0, dtype=c.tdt, device="cuda")
+        c.args.out = flat[shift:]
+        mira.mira_fp8_gemm(c.args)
+        torch.cuda.synchronize()
+        got = flat[shift:shift + M * (N + 3)].view(M, N + 3)
+        assert torch.equal(got[:, :N], want) and (got[:, N:] == -5).all()
+        assert (flat[:shift] == -5).all() and (flat[shift + M * (N + 3):] == -5).all()

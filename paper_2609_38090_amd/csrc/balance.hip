@@ -253,10 +253,14 @@ __device__ __forceinline__ void reduce_groups(float acc[4], int E, float (*wave_
 }
 
 // Counts the pairs of rows [lo, hi) into hist and the kept rows into *kept
-// (both in LDS, zeroed before).
+// (both in LDS, zeroed before).  With few experts the lanes of a wave would queue
+// for the same few counters: each lane counts in registers instead, and a wave
+// adds once per expert (3904 rows of 5: 24 us with a counter per pair, FEWUS so).
 template <int THREADS>
 __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int hi, int* hist, int* kept) {
   const uint32_t end = (uint32_t)hi * q.k;  // T * k is at most 2^30
+  const bool few = q.E <= kFewExperts;
+  int mine[kFewExperts] = {};
   for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += 4 * THREADS) {  // four loads in flight
     int e[4];
     bool keep[4];
@@ -264,11 +268,26 @@ __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int 
     for (int j = 0; j < 4; ++j) {
       const uint32_t at = min(i + j * THREADS, end - 1);
       e[j] = q.idx[at];
-      keep[j] = !q.mask || q.mask[at / q.k] != 0;
+      keep[j] = i + j * THREADS < end && (!q.mask || q.mask[at / q.k] != 0);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (i + j * THREADS < end && (uint32_t)e[j] < (uint32_t)q.E && keep[j]) atomicAdd(hist + e[j], 1);
+    for (int j = 0; j < 4; ++j) {
+      if (few) {
+#pragma unroll
+        for (int x = 0; x < kFewExperts; ++x) mine[x] += keep[j] && e[j] == x;
+      } else if (keep[j] && (uint32_t)e[j] < (uint32_t)q.E) {
+        atomicAdd(hist + e[j], 1);
+      }
+    }
+  }
+  if (few) {
+#pragma unroll
+    for (int x = 0; x < kFewExperts; ++x) {
+      int n = mine[x];
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
+      if ((threadIdx.x & 63) == 0 && x < q.E && n) atomicAdd(hist + x, n);
+    }
   }
   if (q.mask) {
     int n = 0;
@@ -591,7 +610,7 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
   // One workgroup per group: few logits, or many groups of few logits (1000 rows of
   // 256 experts in 500 groups: 6.5 us so, 37 by chunks that walk the groups; kept to
   // 2^20 logits, where one group of nearly all of them costs some 150 us).
-  const size_t logits = (size_t)q.T * q.E;
+  const size_t logits = (size_t)q.T * lanes * 4;  // as the lanes hold them
   const bool small = logits <= 32768 || (logits <= (size_t)q.G * 8192 && logits <= 1u << 20);
   int chunks = 0;
   if (!small) {

@@ -196,16 +196,23 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
   return t.nt >= 0;
 }
 
+// Vectors at the alignment of out's elements: global stores take any, so rows of
+// every length and start are stored 8 or 16 bytes at a time.
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// Four consecutive columns, n of them (at least one) inside the row.
 template <typename OutT>
 __device__ __forceinline__ void store_out4(OutT* p, v4f v, int n) {
-  if (n >= 4 && ((uintptr_t)p & (4 * sizeof(OutT) - 1)) == 0) {
+  if (n >= 4) {
     if constexpr (sizeof(OutT) == 4) {
-      *(v4f*)p = v;
+      *(v4f_any*)p = v;
     } else {
       uint16_t h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) store_out(h + i, v[i]);
-      *(uint2*)p = uint2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
+      *(v2u_any*)p = v2u_any{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
     }
   } else {
 #pragma unroll
@@ -440,7 +447,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   OutT* out = (OutT*)p.out;
   constexpr int kRowBytes = NT * 32, kChunks = kRowBytes / 16;
   static_assert(W * MT * 16 * kRowBytes <= NS * kStage, "the tile's rows fit the ring");
-  if (sizeof(OutT) == 2 && !p.part && p.ldo % 8 == 0 && ((uintptr_t)out & 15) == 0) {
+  if (sizeof(OutT) == 2 && !p.part) {
     lds_barrier();  // every wave has read its last stage
     char* mine = lds + wave * (MT * 16 * kRowBytes);
 #pragma unroll
@@ -465,7 +472,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
       if (m >= t.m1 || n >= p.N) continue;
       uint16_t* o = (uint16_t*)out + (size_t)m * p.ldo + n;
       if (n + 8 <= p.N) {
-        *(v4i*)o = v;
+        *(v4i_any*)o = v;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)

@@ -46,6 +46,7 @@ struct BalanceParams {
   size_t ld_x, ld_d;
   int T, E, k, G, chunk_rows;
   float coef;
+  uint64_t inv_k;  // 2^34 / k rounded up: i / k = i * inv_k >> 34 for i < 2^30, k <= 16
 };
 
 // Reductions over groups of L = 1, 2, .. 64 consecutive lanes.  After each step all
@@ -195,25 +196,18 @@ __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi
       float o[4] = {0.f, 0.f, 0.f, 0.f};
       if constexpr (FEW) {
 #pragma clang fp contract(off)
-        float s = 0.f, w = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          v[u][i] = expf(v[u][i] - m);
-          s = s + v[u][i];
-        }
-        s = lanes_reduce<L, AddOp>(s);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          v[u][i] = s == 0.f ? 0.f : v[u][i] / s;
-          const float fp = f[i] * v[u][i];
-          w = w + fp;
-        }
-        w = lanes_reduce<L, AddOp>(w);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          acc[i] += keep[u] ? v[u][i] : 0.f;
-          const float gp = gscale * v[u][i];
-          o[i] = keep[u] ? gp * (f[i] - w) : 0.f;
+        const bool two = q.E > L;  // the lanes' second values exist (E is no power of two)
+        float e0 = expf(v[u][0] - m), e1 = two ? expf(v[u][1] - m) : 0.f;
+        const float s = lanes_reduce<L, AddOp>(e0 + e1);
+        e0 = s == 0.f ? 0.f : e0 / s;
+        if (two) e1 = s == 0.f ? 0.f : e1 / s;
+        const float f0 = f[0] * e0, f1 = f[1] * e1;
+        const float w = lanes_reduce<L, AddOp>(f0 + f1);
+        acc[0] += keep[u] ? e0 : 0.f;
+        o[0] = keep[u] ? (gscale * e0) * (f[0] - w) : 0.f;
+        if (two) {
+          acc[1] += keep[u] ? e1 : 0.f;
+          o[1] = keep[u] ? (gscale * e1) * (f[1] - w) : 0.f;
         }
       } else {
         float s = 0.f, w = 0.f;
@@ -252,43 +246,58 @@ __device__ __forceinline__ void reduce_groups(float acc[4], int E, float (*wave_
   }
 }
 
+// Adds a wave's counts of up to kFewExperts experts, a byte each per lane, to hist.
+__device__ __forceinline__ void add_bytes(uint64_t c, int E, int* hist) {
+  const uint32_t lo = (uint32_t)c, hi = (uint32_t)(c >> 32);
+  // two 16-bit sums each: 64 lanes of at most 255 stay below 2^16
+  uint32_t v[4] = {lo & 0x00FF00FFu, lo >> 8 & 0x00FF00FFu, hi & 0x00FF00FFu, hi >> 8 & 0x00FF00FFu};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int x = 0; x < kFewExperts; ++x) {
+      const int n = v[(x >> 2) * 2 + (x & 1)] >> ((x & 2) * 8) & 0xFFFF;
+      if (x < E && n) atomicAdd(hist + x, n);
+    }
+  }
+}
+
 // Counts the pairs of rows [lo, hi) into hist and the kept rows into *kept
 // (both in LDS, zeroed before).  With few experts the lanes of a wave would queue
-// for the same few counters: each lane counts in registers instead, and a wave
-// adds once per expert (3904 rows of 5: 24 us with a counter per pair, FEWUS so).
+// for the same few counters: each lane counts in the bytes of a register instead,
+// and a wave adds those up (3904 rows of 5 of 5, masked: 24 us the call with a
+// counter per pair, 20 us so).
 template <int THREADS>
 __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int hi, int* hist, int* kept) {
   const uint32_t end = (uint32_t)hi * q.k;  // T * k is at most 2^30
   const bool few = q.E <= kFewExperts;
-  int mine[kFewExperts] = {};
-  for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += 4 * THREADS) {  // four loads in flight
-    int e[4];
-    bool keep[4];
+  uint64_t bytes = 0;
+  int n_bytes = 0;
+  constexpr int kFlight = 4;  // loads in flight; whole waves stay in the loop
+  for (uint32_t i0 = (uint32_t)lo * q.k; i0 < end; i0 += kFlight * THREADS) {
+    const uint32_t i = i0 + threadIdx.x;
+    int e[kFlight];
+    bool keep[kFlight];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kFlight; ++j) {
       const uint32_t at = min(i + j * THREADS, end - 1);
       e[j] = q.idx[at];
-      keep[j] = i + j * THREADS < end && (!q.mask || q.mask[at / q.k] != 0);
+      keep[j] = i + j * THREADS < end && (!q.mask || q.mask[(uint32_t)((uint64_t)at * q.inv_k >> 34)] != 0);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (few) {
-#pragma unroll
-        for (int x = 0; x < kFewExperts; ++x) mine[x] += keep[j] && e[j] == x;
-      } else if (keep[j] && (uint32_t)e[j] < (uint32_t)q.E) {
-        atomicAdd(hist + e[j], 1);
-      }
+    for (int j = 0; j < kFlight; ++j) {
+      const bool in = keep[j] && (uint32_t)e[j] < (uint32_t)q.E;
+      if (few) bytes += (uint64_t)in << ((e[j] & 7) * 8);
+      else if (in) atomicAdd(hist + e[j], 1);
     }
-  }
-  if (few) {
-#pragma unroll
-    for (int x = 0; x < kFewExperts; ++x) {
-      int n = mine[x];
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
-      if ((threadIdx.x & 63) == 0 && x < q.E && n) atomicAdd(hist + x, n);
+    if (few && (n_bytes += kFlight) + kFlight > 255) {
+      add_bytes(bytes, q.E, hist);
+      bytes = n_bytes = 0;
     }
   }
+  if (few) add_bytes(bytes, q.E, hist);
   if (q.mask) {
     int n = 0;
     for (int r = lo + threadIdx.x; r < hi; r += THREADS) n += q.mask[r] != 0;
@@ -319,7 +328,7 @@ __global__ __launch_bounds__(THREADS) void balance_group_kernel(BalanceParams q)
     const int e = expert_of<L, VEC>(l, i);
     counts[i] = e < q.E ? hist[e] : 0;
   }
-  rows_pass<L, VEC, FEW, 2, T>(q, s.lo + t / L, s.hi, THREADS / L, l, counts, n, group_grad(q, g), acc);
+  rows_pass<L, VEC, FEW, FEW ? 4 : 2, T>(q, s.lo + t / L, s.hi, THREADS / L, l, counts, n, group_grad(q, g), acc);
   reduce_groups<L, VEC, THREADS>(acc, q.E, wave_sums);
   __syncthreads();
   float term = 0.f;
@@ -469,7 +478,7 @@ __global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams
       const int e = expert_of<L, VEC>(l, i);
       counts[i] = q.counts[(size_t)g * q.E + min(e, q.E - 1)];
     }
-    rows_pass<L, VEC, FEW, 2, T>(q, a + t / L, b, kBigThreads / L, l, counts, n, group_grad(q, g), acc);
+    rows_pass<L, VEC, FEW, FEW ? 4 : 2, T>(q, a + t / L, b, kBigThreads / L, l, counts, n, group_grad(q, g), acc);
     if (!q.mean && !q.loss) return;
     __syncthreads();
     reduce_groups<L, VEC, kBigThreads>(acc, q.E, wave_sums);
@@ -603,6 +612,7 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
   q.k = a.top_k;
   q.G = a.n_groups;
   q.coef = a.coef;
+  q.inv_k = ((1ull << 34) + a.top_k - 1) / a.top_k;
   const int lanes = row_lanes(q.E);
   const size_t esz = a.logits_dtype == MIRA_F32 ? 4 : 2;
   const bool vec = q.E % 4 == 0 && q.ld_x % 4 == 0 && (uintptr_t)q.logits % (4 * esz) == 0 &&

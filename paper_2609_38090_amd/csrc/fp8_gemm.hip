@@ -54,13 +54,15 @@ __device__ __forceinline__ Rows rows_of(const GemmParams& p, int g) {
   return Rows{lo, min(max(p.offsets[g + 1], lo), p.M)};
 }
 
-// Source row of output row i; -1 for a row of zeros.
-__device__ __forceinline__ int source_row(const GemmParams& p, int i) {
-  if (!p.order) return i;
-  const int pair = p.order[i];
+// Source row of a pair, and of output row i; -1 for a row of zeros.
+__device__ __forceinline__ int source_of_pair(const GemmParams& p, int pair) {
   if (pair < 0) return -1;
   const int routed = p.x_rows * p.top_k;
   return pair < routed ? pair / p.top_k : (pair - routed) % p.x_rows;
+}
+__device__ __forceinline__ int source_row(const GemmParams& p, int i) {
+  if (!p.order) return i;
+  return source_of_pair(p, p.order[i]);
 }
 
 __device__ __forceinline__ v8i join(v4i a, v4i b) {
@@ -497,6 +499,116 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   }
 }
 
+// ---- few rows --------------------------------------------------------------------
+//
+// Up to 16 rows are bound by the weights' bytes and by how soon they are asked for.
+// A workgroup owns 16 weight rows and one tile of 16 token rows; its four waves
+// take the blocks of the contraction in turn, straight from memory to registers: no
+// LDS and no barrier until their sums are joined, so that each has D blocks on the
+// way whatever the others do, and N / 16 workgroups fill the chip where tiles of 64
+// weight rows do not.  Its price is that every 16 weight rows read the token rows
+// anew (few_rows() below keeps that small).  GROUPED: a workgroup first waits for
+// its group's bounds and its pairs, so the weights are asked for before the tokens;
+// D = 2 leaves room for more workgroups to wait at once (2 x 14336 x 4096 of 8
+// experts: 26.3 us, 29.4 as the other; 1 x 4096 x 14336 without groups: 16.0 us
+// this way, 13.8 with D = 4).
+template <bool GROUPED, bool EXACT, typename OutT>
+__global__ __launch_bounds__(256) void fp8_gemm_few_kernel(GemmParams p, int nT) {
+  constexpr int WV = 4, D = GROUPED ? 2 : 4;
+  __shared__ v4f sums[WV][64];
+  __shared__ int tile_s[5];
+  Tile t;
+  if (!find_tile<16>(p, nT, tile_s, t)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, kg = lane >> 4, n0 = t.nt * 16;
+  const int k16 = (p.K + 15) & ~15;
+  const int first = wave, n = (p.KB - first + WV - 1) / WV;  // blocks first, first + WV, ..
+  const uint8_t* w = p.w + (size_t)t.g * p.w_stride + (size_t)min(n0 + r16, p.N - 1) * p.ldw;
+  const float* ws = p.ws + (size_t)t.g * p.ws_stride + (size_t)(n0 >> 7) * p.ld_ws;
+  struct Block {
+    v4i w[2], x[2];
+    float xs, ws;
+  };
+  // Bytes of half h of block b that this lane holds; past the end those of the row's
+  // start, which meet zeros of x.
+  const auto inside = [&](int b, int h) { return b * 128 + h * 64 + kg * 16 < k16; };
+  const auto from = [&](int b, int h) { return inside(b, h) ? b * 128 + h * 64 + kg * 16 : 0; };
+  const auto load_w = [&](Block& s, int b) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) s.w[h] = *(const v4i*)(w + from(b, h));
+  };
+  Block ring[D];
+  const int m = t.m0 + r16;
+  int src = min(m, t.m1 - 1);
+  bool none = false;
+  if constexpr (GROUPED) {
+    const int pair = p.order ? p.order[src] : src;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      if (d < n) load_w(ring[d], first + d * WV);
+    __builtin_amdgcn_sched_barrier(0);
+    src = p.order ? source_of_pair(p, pair) : pair;
+    none = src < 0;
+    src = max(src, 0);
+  } else {
+    src = max(source_row(p, src), 0);
+    none = p.order && source_row(p, min(m, t.m1 - 1)) < 0;
+  }
+  const uint8_t* x = p.x + (size_t)src * p.ldx;
+  const float* xs = p.xs + (size_t)src * p.ld_xs;
+  const auto load_x = [&](Block& s, int b) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) s.x[h] = *(const v4i*)(x + from(b, h));
+    s.xs = xs[b];
+    s.ws = ws[b];
+  };
+  v4f acc = {0.f, 0.f, 0.f, 0.f};
+  const auto use = [&](const Block& s, int b) {
+    Frag<EXACT> fw, fx;
+    fw.set(join(s.w[0], s.w[1]));
+    fx.set(join(inside(b, 0) ? s.x[0] : zero16(), inside(b, 1) ? s.x[1] : zero16()));
+    const v4f d = Frag<EXACT>::mul(fw, fx);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(d[e], s.xs * s.ws, acc[e]);
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (d < n) {
+      if constexpr (!GROUPED) load_w(ring[d], first + d * WV);
+      load_x(ring[d], first + d * WV);
+    }
+  int i = 0;
+  for (; i + 2 * D <= n; i += D) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int b = first + (i + d) * WV;
+      use(ring[d], b);
+      load_w(ring[d], b + D * WV);
+      load_x(ring[d], b + D * WV);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  for (; i < n; i += D) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int b = first + (i + d) * WV;
+      if (i + d < n) use(ring[d], b);
+      if (i + d + D < n) {
+        load_w(ring[d], b + D * WV);
+        load_x(ring[d], b + D * WV);
+      }
+    }
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  const int c = n0 + 4 * kg;
+  if (wave != 0 || m >= t.m1 || c >= p.N) return;
+#pragma unroll
+  for (int q = 1; q < WV; ++q) acc += sums[q][lane];
+  store_out4((OutT*)p.out + (size_t)m * p.ldo + c, none ? v4f{0.f, 0.f, 0.f, 0.f} : acc, p.N - c);
+}
+
 // Adds the S parts of the contraction in order.
 template <typename OutT>
 __global__ __launch_bounds__(256) void fp8_gemm_join_kernel(GemmParams p) {
@@ -536,12 +648,13 @@ constexpr Shape kShapes[] = {
     {"fp8_gemm_64x16", 64, 16, 3, {0.25f, 0.3f}, {0.4f, 0.5f}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
+constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}};
 constexpr float kTileUs = 2.5f, kJoinUs = 7.f, kJoinBytesPerUs = 4e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
 constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
 
 struct Plan {
-  int shape, S;  // S = 0: no shape fits one launch
+  int shape, S;  // shape kShapeCount: few rows; S = 0: no shape fits one launch
 };
 
 long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
@@ -550,7 +663,23 @@ long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
   return mT * ((a.n + s.bn - 1) / s.bn);
 }
 
+// Whether the kernel for few rows takes a call (us, it against the tiles, weights
+// not in a cache).  Token rows read anew by every 16 weight rows: 4 x 28672 x 4096
+// 25.4 against 26.6, 8 rows 29.7 against 27.5, 16 rows 36 against 28; one or two
+// rows always (1 x 28672 x 4096 23.1 against 26.6, 1 x 128256 x 4096 88 against 97).
+// A wave's way through the contraction: 1 x 4096 x 14336 13.8 against 17.9, 16 x
+// 4096 x 4096 7.5 against 10.4, but 16 x 1024 x 14336 17.9 against 11.6.  Many small
+// tiles, each with its start: 6 x 2816 x 2048 in 6 of 64 experts (1056 tiles) 12.0
+// against 12.3, 16 rows in 12 to 16 of them 16.0 against 13.8.
+bool few_rows(const mira_fp8_gemm_args& a) {
+  const double work = (double)a.m * a.n * a.k;
+  const long tiles = tiles_of(a, kFew);
+  return a.m <= 16 && (a.m <= 2 || work <= 1 << 28) && (long)a.k * (a.m > 4 ? a.m : 4) <= 1 << 16 &&
+         (a.k >= 4096 || tiles <= (long)device_cu_count() * kFew.per_cu) && tiles <= kMaxTiles;
+}
+
 Plan plan_of(const mira_fp8_gemm_args& a) {
+  if (few_rows(a)) return Plan{kShapeCount, 1};
   const int e = a.out_dtype == MIRA_F32, KB = (a.k + 127) / 128, cus = device_cu_count();
   const float active = (float)(a.n_groups < a.m ? a.n_groups : a.m);
   const float arrive = (active * a.n * a.k + (float)a.m * a.k + (float)a.m * a.n * (e ? 4.f : 2.f)) / kBytesPerUs;
@@ -586,7 +715,16 @@ void launch_tile(const GemmParams& p, const Shape& shape, long tiles, hipStream_
 }
 
 template <bool EXACT, typename OutT>
+void launch_few(const GemmParams& p, long tiles, hipStream_t st) {
+  const dim3 grid((uint32_t)((tiles + 7) / 8 * 8));
+  const int nT = (p.N + kFew.bn - 1) / kFew.bn;
+  if (p.offsets) launch_timed(kFew.name, fp8_gemm_few_kernel<true, EXACT, OutT>, grid, dim3(256), 0, st, p, nT);
+  else launch_timed(kFew.name, fp8_gemm_few_kernel<false, EXACT, OutT>, grid, dim3(256), 0, st, p, nT);
+}
+
+template <bool EXACT, typename OutT>
 void launch_shape(const GemmParams& p, int i, long tiles, hipStream_t st) {
+  if (i == kShapeCount) return launch_few<EXACT, OutT>(p, tiles, st);
   const Shape& shape = kShapes[i];
   switch (i) {
     case 0: launch_tile<8, 4, 2, 4, 2, EXACT, OutT>(p, shape, tiles, st); break;
@@ -636,7 +774,7 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.w_stride = a.w_stride ? a.w_stride : a.n * p.ldw;
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
-  const long tiles = tiles_of(a, kShapes[plan.shape]);
+  const long tiles = tiles_of(a, plan.shape == kShapeCount ? kFew : kShapes[plan.shape]);
   if (a.out_dtype == MIRA_F32) launch_shape<true, float>(p, plan.shape, tiles, st);
   else launch_shape<false, uint16_t>(p, plan.shape, tiles, st);
   return hipGetLastError();

@@ -99,7 +99,8 @@ def test_larger(M, N, K, out):
 
 # rows, columns, contraction, groups that the dispatch sends to each tile shape
 SHAPES = {"fp8_gemm_256x256": (4100, 8300, 140, 1), "fp8_gemm_256x128": (1900, 4090, 260, 1),
-          "fp8_gemm_128x64": (1500, 2000, 500, 1), "fp8_gemm_64x16": (11, 3000, 700, 1), "fp8_gemm_join": (20, 260, 9000, 1)}
+          "fp8_gemm_128x64": (1500, 2000, 500, 1), "fp8_gemm_64x16": (19, 3000, 700, 1), "fp8_gemm_join": (20, 260, 9000, 1),
+          "fp8_gemm_few": (11, 3000, 700, 1)}
 
 
 @pytest.mark.parametrize("name", list(SHAPES))
@@ -114,6 +115,48 @@ def test_every_tile_shape(name, out, tail):
     ran = mira.mira_profile_read()
     mira.mira_profile_enable(False)
     assert name in ran, ran
+    c.check()
+
+
+def _ran(c):
+    mira.mira_profile_enable(True)
+    mira.mira_profile_read()
+    c.run()
+    ran = mira.mira_profile_read()
+    mira.mira_profile_enable(False)
+    return set(ran)
+
+
+# blocks of the contraction: fewer than a workgroup's four waves, a wave's ring not
+# full, full, turned over once and more, with an end inside a block
+@pytest.mark.parametrize("K", [1, 128, 400, 512, 1030, 2048, 2049, 4000, 4096, 4100, 8100])
+@pytest.mark.parametrize("M,sizes,lo,tail,top_k,shared", [(1, None, 0, 0, 0, 0), (2, None, 0, 0, 0, 0), (8, None, 0, 0, 0, 0), (16, None, 0, 0, 0, 0),
+                                                          (7, [0, 3, 0, 1, 2], 0, 1, 0, 0), (16, [16], 0, 0, 0, 0),
+                                                          (6, [1, 1, 0, 3, 0, 0, 1], 0, 0, 2, 0), (8, [2, 0, 4], 1, 1, 3, 1)])
+def test_few_rows(M, sizes, lo, tail, top_k, shared, K):
+    c = Case(M, 83, K, "f32" if K % 3 else "bf16", G=len(sizes) if sizes else 1, sizes=sizes, lo=lo, tail=tail, top_k=top_k,
+             T=3 if top_k else 0, shared=shared, pads=(1, 1, 1, 2, 3))
+    if top_k:
+        c.order[M // 2] = -1
+    assert ("fp8_gemm_few" in _ran(c)) == (K * max(M, 4) <= 1 << 16)
+    c.check()
+
+
+def test_few_rows_nan():
+    # codes of NaN at the start of a row meet only their own column and row
+    c = Case(5, 40, 130, "bf16")
+    c.w[0, 3, 0], c.w[0, 20, 129], c.x[2, 0] = 0x7F, 0xFF, 0x7F
+    assert _ran(c) == {"fp8_gemm_few"}
+    c.check()
+
+
+# either side of each bound of the dispatch
+@pytest.mark.parametrize("M,N,K,few", [(16, 4096, 4096, True), (16, 4112, 4096, False), (17, 64, 256, False), (2, 33000, 4200, True),
+                                       (3, 33000, 4200, False), (1, 20, 16384, True), (1, 20, 16400, False), (16, 48, 4128, False),
+                                       (1, 16 * 1280, 256, True)])
+def test_few_rows_bounds(M, N, K, few):
+    c = Case(M, N, K, "bf16")
+    assert ("fp8_gemm_few" in _ran(c)) == few
     c.check()
 
 

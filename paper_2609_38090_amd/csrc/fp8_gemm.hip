@@ -633,9 +633,10 @@ __global__ __launch_bounds__(256) void fp8_gemm_join_kernel(GemmParams p) {
 // 128, 729 in 128 x 64; 64 x 28672 x 4096: 54, 34, 21; 2048 x 4096 x 4096: 57,
 // 39, 53; 16 x 4096 x 4096: 128 x 64 17 us, 64 x 16 10).  Tiles of 128 x 128 (594, 33,
 // 44) and of 128 x 16 (1 x 28672 x 4096: 28.7, 64 x 16 27.3) were measured too.
-// Parts of the contraction fill the chip where the tiles do not: 1 x 4096 x 14336
-// takes 28 us in one part, 15 in parts (their second launch is why short
-// contractions stay whole: 16 x 4096 x 4096 10 us, 13 in parts).
+// Parts of the contraction fill the chip where the tiles do not: 16 x 4096 x 14336
+// takes 34 us in one part, 17 to 19 in parts, 512 rows of it 59 and 48 (their second
+// launch is why short contractions stay whole: 17 x 4096 x 4096 10.4 us, 11.5 in
+// parts).
 struct Shape {
   const char* name;  // in the kernel timing
   int bn, bm, per_cu;
@@ -649,7 +650,7 @@ constexpr Shape kShapes[] = {
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}};
-constexpr float kTileUs = 2.5f, kJoinUs = 7.f, kJoinBytesPerUs = 4e6f, kBytesPerUs = 5.5e6f;
+constexpr float kTileUs = 2.5f, kJoinUs = 8.f, kJoinBytesPerUs = 7e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
 constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
 

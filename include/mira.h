@@ -12,7 +12,10 @@
  * STAGE regions of the expert cache (section IV-C); slots are filled from
  * pinned host memory by asynchronous copies (sections IV-E, IV-F).  Predictor
  * heads score the experts of layer l+2 (section IV-E): a two-layer MLP and the
- * paper's MixtureHead.
+ * paper's MixtureHead.  Beside the step stand the operators that a program needs
+ * to train or tune such a layer and to run its dense matrices in 8 bits: the
+ * router's balance loss with its gradient, and e4m3 matrices with block scales:
+ * their quantizer and their product, plain or grouped over experts.
  *
  * Conventions for every entry point:
  *  - Return 0 (MIRA_OK) on success or a negative mira_status.  A failing call
@@ -27,7 +30,8 @@
  *    valid once the stream reaches the call.  Only the host path of
  *    mira_pack_experts runs synchronously.  Calls on distinct workspaces may
  *    run concurrently.
- *  - mira_moe_forward, mira_moe_route and mira_moe_experts only launch
+ *  - mira_moe_forward, mira_moe_route, mira_moe_experts, mira_balance_loss,
+ *    mira_fp8_quantize and mira_fp8_gemm only launch
  *    kernels (no allocation, copy, memset or host synchronisation), so they
  *    can be captured into a HIP graph and replayed; a replay recomputes
  *    everything from the buffers the captured call was given.
@@ -374,7 +378,7 @@ typedef struct mira_balance_args {
   int32_t n_tokens;        /* T >= 0 */
   int32_t n_experts;       /* E: 1..MIRA_MAX_EXPERTS */
   int32_t top_k;           /* k: 1..MIRA_MAX_TOPK */
-  int32_t n_groups;        /* G >= 1; 1 with offsets NULL */
+  int32_t n_groups;        /* G: 1..2^21; 1 with offsets NULL */
   float coef;              /* finite */
   uint64_t ld_logits;      /* elements between rows of logits, >= E; 0 = E */
   uint64_t ld_dlogits;     /* elements between rows of dlogits, >= E; 0 = E */
@@ -387,8 +391,8 @@ typedef struct mira_balance_args {
 } mira_balance_args;
 
 /* Bytes of workspace for calls with up to max_tokens tokens and max_groups
- * groups.  Returns 0 for a negative max_tokens, max_groups < 1 or n_experts
- * outside 1..MIRA_MAX_EXPERTS. */
+ * groups.  Returns 0 for a negative max_tokens, max_groups outside 1..2^21 or
+ * n_experts outside 1..MIRA_MAX_EXPERTS. */
 size_t mira_balance_workspace_bytes(int32_t max_tokens, int32_t n_experts, int32_t max_groups);
 
 /* The loss, its counts and its gradient in one call: any of the four outputs
@@ -448,8 +452,14 @@ int mira_fp8_quantize(const mira_fp8_quant_args* a, hipStream_t stream);
  * writes it (expert_offsets are the offsets then), the token of pair p =
  * pair_order[i]: p / top_k for p < x_rows * top_k, (p - x_rows * top_k) mod
  * x_rows for shared pairs; a negative p gives a row of zeros.
- * Each block's products are summed by the fp8 matrix cores, the blocks in
- * fp32; out is rounded once.  Deterministic.  NaN operands give NaN. */
+ * With out MIRA_F32 the products are summed in fp32 (e4m3 values are exact in
+ * bf16, whose matrix instructions keep 32 bits).  With out MIRA_BF16 a block's
+ * products are summed by the fp8 matrix instructions, at twice the rate: of each
+ * eight consecutive k they drop the bits below 2^-13 of the largest product, which
+ * puts a block's sum off by some 1.5e-5 of its 2-norm (a hundredth of out's own
+ * rounding) and by at most 2^-10 of the sum of its products' magnitudes.  The
+ * blocks are summed in fp32 either way and out is rounded once.  Repeated calls
+ * give the same bits.  NaN operands give NaN.  out overlaps no input. */
 typedef struct mira_fp8_gemm_args {
   int32_t m;           /* rows of out, >= 0 */
   int32_t n;           /* columns of out = rows of each w, >= 1 */

@@ -21,6 +21,9 @@ uint64_t pad16(uint64_t n) { return (n + 15) / 16 * 16; }
 // Strides may not take any buffer past 2^60 bytes, so that no offset overflows.
 constexpr uint64_t kMaxLd = 1ull << 28;
 
+// Groups of a balance loss: a workgroup of 1024 threads each, fewer than 2^32 in a launch.
+constexpr int32_t kMaxGroups = 1 << 21;
+
 int check_ld(const char* name, uint64_t ld, uint64_t least, uint64_t mult) {
   if (ld == 0) return MIRA_OK;
   if (ld < least)
@@ -58,7 +61,7 @@ int check_gemm_sizes(const mira_fp8_gemm_args* a) {
 extern "C" {
 
 size_t mira_balance_workspace_bytes(int32_t max_tokens, int32_t n_experts, int32_t max_groups) {
-  if (max_tokens < 0 || n_experts < 1 || n_experts > MIRA_MAX_EXPERTS || max_groups < 1) return 0;
+  if (max_tokens < 0 || n_experts < 1 || n_experts > MIRA_MAX_EXPERTS || max_groups < 1 || max_groups > kMaxGroups) return 0;
   return mira::balance_ws_bytes(n_experts, max_groups);
 }
 
@@ -71,8 +74,8 @@ int mira_balance_loss(const mira_balance_args* a, hipStream_t stream) {
     return set_error(MIRA_ERR_SHAPE, "top_k (%d) must be in [1, %d]", a->top_k, MIRA_MAX_TOPK);
   if (a->n_tokens < 0 || (int64_t)a->n_tokens * a->top_k > (int64_t)1 << 30)
     return set_error(MIRA_ERR_SHAPE, "n_tokens (%d) must be in [0, 2^30 / top_k]", a->n_tokens);
-  if (a->n_groups < 1 || a->n_groups > 1 << 22)
-    return set_error(MIRA_ERR_SHAPE, "n_groups (%d) must be in [1, 2^22]", a->n_groups);
+  if (a->n_groups < 1 || a->n_groups > kMaxGroups)
+    return set_error(MIRA_ERR_SHAPE, "n_groups (%d) must be in [1, 2^21]", a->n_groups);
   if (!a->offsets && a->n_groups != 1) return set_error(MIRA_ERR_ARG, "several groups need offsets");
   if (!std::isfinite(a->coef)) return set_error(MIRA_ERR_ARG, "coef must be finite");
   int rc = check_ld("ld_logits", a->ld_logits, a->n_experts, 1);

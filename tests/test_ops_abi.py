@@ -25,7 +25,7 @@ def _balance(**kw):
 @pytest.mark.parametrize("bad,code", [
     (dict(logits_dtype=5), ARG), (dict(n_experts=0), SHAPE), (dict(n_experts=257), SHAPE), (dict(top_k=0), SHAPE),
     (dict(top_k=17), SHAPE), (dict(n_tokens=-1), SHAPE), (dict(n_tokens=2 ** 30), SHAPE), (dict(n_groups=0), SHAPE),
-    (dict(offsets=None), ARG), (dict(coef=float("nan")), ARG), (dict(coef=float("inf")), ARG),
+    (dict(n_groups=2 ** 21 + 1), SHAPE), (dict(offsets=None), ARG), (dict(coef=float("nan")), ARG), (dict(coef=float("inf")), ARG),
     (dict(ld_logits=7), SHAPE), (dict(ld_dlogits=7), SHAPE), (dict(logits=None), ARG), (dict(topk_idx=None), ARG),
     (dict(logits=0x1002), ALIGN), (dict(loss=0x4001), ALIGN), (dict(workspace=None), ARG),
     (dict(workspace=0x10010), ALIGN), (dict(workspace_bytes=16), WORKSPACE),
@@ -38,7 +38,7 @@ def test_balance_refuses(bad, code):
 def test_balance_workspace():
     sizes = [mira.mira_balance_workspace_bytes(100, 64, g) for g in (1, 2, 100, 5000)]
     assert sizes == sorted(sizes) and all(s % 256 == 0 for s in sizes)
-    for bad in ((-1, 8, 1), (4, 0, 1), (4, 257, 1), (4, 8, 0)):
+    for bad in ((-1, 8, 1), (4, 0, 1), (4, 257, 1), (4, 8, 0), (4, 8, 2 ** 21 + 1)):
         with pytest.raises(mira.MiraError):
             mira.mira_balance_workspace_bytes(*bad)
 

@@ -26,9 +26,14 @@ namespace {
 
 constexpr int kMaxChunks = 256;   // one 1024-thread workgroup per CU
 constexpr int kBigThreads = 1024;
-// Selections that one workgroup per group counts (four times as many where groups
-// share them); more are counted by chunks, after a launch that zeroes the counts.
-constexpr size_t kFewPairs = 65536;
+// Selections that one workgroup per group counts; more are counted by chunks, after
+// a launch that zeroes the counts (us, per group against chunks: one group of 32768
+// 15.9 and 17.1, of 49152 17.8 and 17.3; 37 groups of 3244 26.5 and 29.3, 16 of 8192
+// 31.5 and 27.9, 4 of 65536 31 and 22).  Beyond 2^18 of them one group may hold so
+// many that its workgroup is what the call waits for: 40 to 90 us at 2^18.
+constexpr bool few_pairs(size_t pairs, size_t groups) {
+  return pairs <= 32768 || (pairs <= groups * 4096 && pairs <= 1u << 18);
+}
 
 struct BalanceParams {
   const void* logits;
@@ -628,7 +633,7 @@ hipError_t launch_balance(const mira_balance_args& a, hipStream_t st) {
     const int rows = kBigThreads / lanes;
     q.chunk_rows = (int)align_up((size_t)(q.T + kMaxChunks - 1) / kMaxChunks, rows);
     chunks = (q.T + q.chunk_rows - 1) / q.chunk_rows;
-    if ((size_t)q.T * q.k <= (q.G > 1 ? 4 : 1) * kFewPairs) {
+    if (few_pairs((size_t)q.T * q.k, q.G)) {
       launch_timed("balance_count", balance_count_group_kernel, dim3(q.G), dim3(kBigThreads), 0, st, q);
     } else {
       const size_t n = (size_t)q.G * q.E;

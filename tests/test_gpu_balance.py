@@ -307,3 +307,21 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         for c, w in zip(cases, want):
             assert all(torch.equal(c.out[k], w[k]) for k in w)
+
+
+# either side of each bound of the dispatch: one workgroup per group for all; counts by
+# group; counts by chunks from zeros
+@pytest.mark.parametrize("T,E,k,G,ran", [
+    (512, 64, 4, 1, {"group"}), (513, 64, 4, 1, {"count", "rows"}), (16384, 64, 2, 1, {"count", "rows"}),
+    (16385, 64, 2, 1, {"zero", "count", "rows"}), (2048, 64, 4, 16, {"group"}), (2049, 64, 4, 16, {"count", "rows", "finish"}),
+    (21845, 64, 3, 16, {"count", "rows", "finish"}), (21846, 64, 3, 16, {"zero", "count", "rows", "finish"}),
+    (32768, 32, 8, 64, {"count", "rows", "finish"}), (32769, 32, 8, 64, {"zero", "count", "rows", "finish"})])
+def test_dispatch_bounds(T, E, k, G, ran):
+    c = Case(T, E, k, G, masked=G > 1)
+    mira.mira_profile_enable(True)
+    mira.mira_profile_read()
+    c.run()
+    names = set(mira.mira_profile_read())
+    mira.mira_profile_enable(False)
+    assert names == {"balance_" + n for n in ran}
+    c.check()

@@ -1,7 +1,9 @@
 // Quantizing to e4m3 with one fp32 scale per block of 1 x 128 or 128 x 128:
 //   a = max(max |x|, eps), scale = fl32(a / 448), q = e4m3(fl32(x * fl32(448 / a))).
 // Memory bound: every value is read once, kept in registers while its block's
-// maximum is found, and written as one byte.  A value is multiplied by the
+// maximum is found, and written as one byte (a copy on this GPU runs at 5.1 TB/s:
+// SwiGLU of 4096 x 2 x 14336 bf16, 296 MB, 57 us, 5.2 TB/s; 14336 x 4096 fp32 to both
+// copies, 353 MB, 69 us, 5.1 TB/s; 8 x 4096, 5.2 us, is a launch).  A value is multiplied by the
 // block's inverse instead of divided by its scale: one correctly rounded
 // division per block instead of one per value (about ten instructions each).
 #include "device_util.h"
@@ -103,7 +105,8 @@ __device__ __forceinline__ void load_cols(const T* row, int c, int cols, float (
   }
 }
 
-// 1 x 128 blocks: 16 lanes hold a block, eight values each.
+// 1 x 128 blocks: 16 lanes hold a block, eight values each, so that a lane's load is
+// 16 bytes of bf16 and its store 8, and the maximum is four exchanges of registers.
 template <bool SWIGLU, typename T>
 __global__ __launch_bounds__(256) void fp8_quant_rows_kernel(QuantParams p, int nb) {
   const size_t block = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);

@@ -140,12 +140,12 @@ struct Tile {
   int g, m0, m1, nt, part;  // group, rows [m0, m1), tile of weight rows, part of the contraction
 };
 
-// Tiles are numbered so that the workgroups of one XCD (ids equal modulo 8) take
-// consecutive ones, and consecutive tiles run down kTileRun row tiles that share
+// Tiles are numbered so that the workgroups of one XCD (ids equal modulo 8, i the
+// id's place among them) take consecutive ones, and consecutive tiles run down kTileRun row tiles that share
 // their weights before the next weight rows.
 constexpr int kTileRun = 8;
-__device__ __forceinline__ bool tile_number(int mT, int nT, int S, int& mt, int& nt, int& part) {
-  const int each = mT * nT, total = each * S, per = (total + 7) >> 3, i = blockIdx.x >> 3;
+__device__ __forceinline__ bool tile_number(int i, int mT, int nT, int S, int& mt, int& nt, int& part) {
+  const int each = mT * nT, total = each * S, per = (total + 7) >> 3;
   int id = (blockIdx.x & 7) * per + i;
   if (i >= per || id >= total) return false;
   part = id / each;
@@ -162,7 +162,7 @@ template <int BM>
 __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shared, Tile& t) {
   if (!p.offsets) {
     int mt;
-    if (!tile_number((p.M + BM - 1) / BM, nT, p.S, mt, t.nt, t.part)) return false;
+    if (!tile_number(blockIdx.x >> 3, (p.M + BM - 1) / BM, nT, p.S, mt, t.nt, t.part)) return false;
     t.g = 0;
     t.m0 = mt * BM;
     t.m1 = min(t.m0 + BM, p.M);
@@ -186,7 +186,7 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
     }
     const int mT = min(__shfl(end, 63, 64), p.M / BM + min(p.G, p.M));  // (more only where offsets overlap)
     int mt = 0, nt = 0, part = 0;
-    const bool any = tile_number(mT, nT, p.S, mt, nt, part);
+    const bool any = tile_number(blockIdx.x >> 3, mT, nT, p.S, mt, nt, part);
     if (l == 0) {
       shared[0] = any ? nt : -1;
       shared[4] = part;
@@ -208,6 +208,64 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
   t.m0 = __builtin_amdgcn_readfirstlane(shared[2]);
   t.m1 = min(t.m0 + BM, __builtin_amdgcn_readfirstlane(shared[3]));
   t.part = __builtin_amdgcn_readfirstlane(shared[4]);
+  return t.nt >= 0;
+}
+
+// The same with tiles of two heights: BM rows, and for a group's last BM / 2 rows or
+// fewer half as many.  The tall ones, which take longer, come first on every XCD.
+template <int BM>
+__device__ __forceinline__ bool find_mixed_tile(const GemmParams& p, int nT, int* shared, Tile& t, bool& tall) {
+  if (threadIdx.x < 64) {
+    const int l = threadIdx.x;
+    Rows r[4];
+    int n[2][4], sum[2] = {0, 0}, end[2];  // [0] tall, [1] half
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[i] = 4 * l + i < p.G ? rows_of(p, 4 * l + i) : Rows{0, 0};
+      const int rows = r[i].hi - r[i].lo, rest = rows % BM;
+      n[0][i] = rows / BM + (rest > BM / 2);
+      n[1][i] = rest > 0 && rest <= BM / 2;
+      sum[0] += n[0][i];
+      sum[1] += n[1][i];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      end[h] = sum[h];
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(end[h], o, 64);
+        if (l >= o) end[h] += v;
+      }
+    }
+    const int groups = min(p.G, p.M);  // (more tiles only where offsets overlap)
+    const int mT0 = min(__shfl(end[0], 63, 64), p.M / BM + groups), mT1 = min(__shfl(end[1], 63, 64), groups);
+    const int i = blockIdx.x >> 3, per0 = (mT0 * nT + 7) >> 3;
+    const int h = i < per0 ? 0 : 1;
+    int mt = 0, nt = 0, part = 0;
+    const bool any = tile_number(h ? i - per0 : i, h ? mT1 : mT0, nT, 1, mt, nt, part);
+    if (l == 0) {
+      shared[0] = any ? nt : -1;
+      shared[4] = h;
+    }
+    int at = h ? end[1] - sum[1] : end[0] - sum[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = h ? n[1][i] : n[0][i];
+      if (any && mt >= at && mt < at + c) {
+        shared[1] = 4 * l + i;
+        shared[2] = r[i].lo + (h ? (r[i].hi - r[i].lo) / BM : mt - at) * BM;
+        shared[3] = r[i].hi;
+      }
+      at += c;
+    }
+  }
+  __syncthreads();
+  t.nt = __builtin_amdgcn_readfirstlane(shared[0]);
+  t.g = __builtin_amdgcn_readfirstlane(shared[1]);
+  t.m0 = __builtin_amdgcn_readfirstlane(shared[2]);
+  tall = __builtin_amdgcn_readfirstlane(shared[4]) == 0;
+  t.m1 = min(t.m0 + BM, __builtin_amdgcn_readfirstlane(shared[3]));
+  t.part = 0;
   return t.nt >= 0;
 }
 
@@ -271,11 +329,23 @@ struct Frag<true> {
   }
 };
 
-template <int NT, int MT, int WN, int WM, int NS, bool EXACT, typename OutT>
-__global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams p, int nT) {
+// LDS of a tile: the ring of stages, and the scales of twice four stages.
+template <int NT, int MT, int WN, int WM, int NS>
+constexpr int tile_lds() {
+  return NS * (16 * NT * WN + 16 * MT * WM) * 128 + 2 * ((16 * MT * WM + 63) / 64 + 1) * 1024;
+}
+
+// (a variable, so that both tiles of a kernel may share it: through a pointer or a
+// reference the largest tile needs registers that it does not have)
+template <int BYTES>
+__shared__ __attribute__((aligned(1024))) char tile_memory[BYTES];
+
+template <int NT, int MT, int WN, int WM, int NS, bool EXACT, typename OutT, int LDS = tile_lds<NT, MT, WN, WM, NS>()>
+__device__ __forceinline__ void tile_body(const GemmParams& p, Tile t) {
   constexpr int BN = 16 * NT * WN, BM = 16 * MT * WM, W = WN * WM;
   constexpr int SX = (BM + 63) / 64;  // waves that load token scales; the next one loads the weights'
   constexpr int kW = BN * 128, kX = BM * 128, kStage = kW + kX, kScales = (SX + 1) * 1024;
+  static_assert(NS * kStage + 2 * kScales <= LDS, "the tile's LDS");
   // Loads of 8 rows per wave and stage; with fewer than W such groups of token
   // rows, several waves load the same ones to the same place.
   constexpr int GW = BN / 8 / W, GX = BM / 8 / W > 0 ? BM / 8 / W : 1;
@@ -283,10 +353,6 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
                 "tile shape");
   // (scales are asked for four stages, and so at least NS - 2 stages' loads, ahead)
   static_assert(NS >= 2 && NS <= 6, "a block's scales land before they are read");
-  __shared__ __attribute__((aligned(1024))) char lds[NS * kStage + 2 * kScales];
-  __shared__ int tile_s[5];
-  Tile t;
-  if (!find_tile<BM>(p, nT, tile_s, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, kg = lane >> 4, wn = wave % WN, wm = wave / WN;
   const int n0 = t.nt * BN;
@@ -323,7 +389,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     gs = p.xs + (size_t)max(source_row(p, min(t.m0 + wave * 64 + lane, t.m1 - 1)), 0) * p.ld_xs;
   else if (wave == SX)
     gs = ws + (size_t)min((n0 >> 7) + (lane & ((BN + 127) / 128 - 1)), (p.N - 1) >> 7) * p.ld_ws;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(tile_memory<LDS>));
   const int k16 = (p.K + 15) & ~15;
   // Load d of the wave's GW + GX of a whole stage.
   const auto load_one = [&](auto d, const uint8_t* wb, uint32_t at) {
@@ -341,7 +407,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
     if (p.KB >= 4) {
       dma16(gs + min(b0 + 4 * q, p.KB - 4), lds0 + at);
     } else {
-      for (int i = 0; i < p.KB; ++i) *(float*)(lds + at + lane * 16 + i * 4) = gs[i];
+      for (int i = 0; i < p.KB; ++i) *(float*)(tile_memory<LDS> + at + lane * 16 + i * 4) = gs[i];
     }
   };
   // Any stage at once; where the contraction ends inside it, the chunks behind its end are zeros.
@@ -355,13 +421,13 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
       for (int j = 0; j < GW; ++j) {
         const int grp = wave * GW + j;
         if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gw[j], wb, at + grp * 1024);
-        else *(v4i*)(lds + buf + grp * 1024 + lane * 16) = zero16();
+        else *(v4i*)(tile_memory<LDS> + buf + grp * 1024 + lane * 16) = zero16();
       }
 #pragma unroll
       for (int j = 0; j < GX; ++j) {
         const int grp = (wave * GX + j) % (BM / 8);
         if (b * 128 + chunk[grp & 1] * 16 < k16) dma16(gx[j], at + kW + grp * 1024);
-        else *(v4i*)(lds + buf + kW + grp * 1024 + lane * 16) = zero16();
+        else *(v4i*)(tile_memory<LDS> + buf + kW + grp * 1024 + lane * 16) = zero16();
       }
     }
     w += 128;
@@ -384,13 +450,13 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   constexpr int kPerStep = kSteps > 1 ? (kLoads + kSteps - 2) / (kSteps - 1) : kLoads;  // all issued by the last step
   const auto multiply = [&](int b, int buf, int free, auto load) {
     constexpr bool LOAD = load;
-    const char* st = lds + buf;
+    const char* st = tile_memory<LDS> + buf;
     const uint32_t next = lds0 + free;
     const uint8_t* wb = uniform(w);
     const char* sx = st + kW + wm * (MT * 2048);
     const char* sw = st + wn * (NT * 2048);
     const int q = (b - b0) >> 2;
-    const float* sc = (const float*)(lds + NS * kStage + (q & 1) * kScales) + (b - max(min(b0 + 4 * q, p.KB - 4), 0));
+    const float* sc = (const float*)(tile_memory<LDS> + NS * kStage + (q & 1) * kScales) + (b - max(min(b0 + 4 * q, p.KB - 4), 0));
     v4f d[kBehind + 1];
     Frag<EXACT> a[2], x[MT];
     float s[MT];
@@ -464,7 +530,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   static_assert(W * MT * 16 * kRowBytes <= NS * kStage, "the tile's rows fit the ring");
   if (sizeof(OutT) == 2 && !p.part) {
     lds_barrier();  // every wave has read its last stage
-    char* mine = lds + wave * (MT * 16 * kRowBytes);
+    char* mine = tile_memory<LDS> + wave * (MT * 16 * kRowBytes);
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       const int m = t.m0 + wm * (MT * 16) + j * 16 + r16;
@@ -510,6 +576,32 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
       else store_out4(out + (size_t)m * p.ldo + n, v, p.N - n);
     }
   }
+}
+
+template <int NT, int MT, int WN, int WM, int NS, bool EXACT, typename OutT>
+__global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams p, int nT) {
+  __shared__ int tile_s[5];
+  Tile t;
+  if (!find_tile<16 * MT * WM>(p, nT, tile_s, t)) return;
+  tile_body<NT, MT, WN, WM, NS, EXACT, OutT>(p, t);
+}
+
+// Groups in tiles of 256 weight rows by 256 or 128 token rows: a tile of 256 costs 1.5
+// times one of 128, and a group's end leaves half of its last one empty on average.
+// us, so and in tiles of 128: 12288 rows spread evenly over 64 experts of 2816 x 2048
+// 142 and 159 (in tiles of 256 140), unevenly 168 and 164 (188), 12288 unevenly over
+// 64 of 2048 x 1408 92 and 102, 8192 over 32 of 4096 x 1024 93 and 100.  The tall
+// ones first: mixed evenly over the launch 101 and 99 for the last two.  Only with bf16
+// out: with the widening as well the two bodies spill registers.
+__global__ __launch_bounds__(512) void fp8_gemm_mixed_kernel(GemmParams p, int nT) {
+  constexpr int tall_lds = tile_lds<8, 4, 2, 4, 2>(), half_lds = tile_lds<4, 4, 4, 2, 3>();
+  constexpr int most = tall_lds > half_lds ? tall_lds : half_lds;
+  __shared__ int tile_s[5];
+  Tile t;
+  bool tall;
+  if (!find_mixed_tile<256>(p, nT, tile_s, t, tall)) return;
+  if (tall) tile_body<8, 4, 2, 4, 2, false, uint16_t, most>(p, t);
+  else tile_body<4, 4, 4, 2, 3, false, uint16_t, most>(p, t);
 }
 
 // ---- few rows --------------------------------------------------------------------
@@ -662,14 +754,16 @@ constexpr Shape kShapes[] = {
     {"fp8_gemm_64x16", 64, 16, 3, {0.25f, 0.3f}, {0.4f, 0.5f}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
-constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}};
+constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}}, kMixed = {"fp8_gemm_mixed", 256, 256, 1, {}, {}};
+enum : int { kFewRows = kShapeCount, kMixedTiles };
 constexpr float kTileUs = 2.5f, kJoinUs = 8.f, kJoinBytesPerUs = 7e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
 constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
 
 struct Plan {
-  int shape, S;  // shape kShapeCount: few rows; S = 0: no shape fits one launch
+  int shape, S;  // S = 0: no shape fits one launch
 };
+const Shape& shape_of(int i) { return i == kFewRows ? kFew : i == kMixedTiles ? kMixed : kShapes[i]; }
 
 long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
   // with offsets an upper bound: every group may end inside a tile
@@ -693,12 +787,21 @@ bool few_rows(const mira_fp8_gemm_args& a) {
 }
 
 Plan plan_of(const mira_fp8_gemm_args& a) {
-  if (few_rows(a)) return Plan{kShapeCount, 1};
+  if (few_rows(a)) return Plan{kFewRows, 1};
   const int e = a.out_dtype == MIRA_F32, KB = (a.k + 127) / 128, cus = device_cu_count();
   const float active = (float)(a.n_groups < a.m ? a.n_groups : a.m);
   const float arrive = (active * a.n * a.k + (float)a.m * a.k + (float)a.m * a.n * (e ? 4.f : 2.f)) / kBytesPerUs;
+  const auto overlap = [&](float us) { return us > arrive ? us + 0.2f * arrive : arrive + 0.2f * us; };  // not wholly
   Plan best{0, 0};
   float least = 0.f;
+  if (a.offsets && !e && tiles_of(a, kMixed) <= kMaxTiles) {
+    // the rows' whole tiles, a half tile for each group, and a part of one until the last ends
+    const Shape &tall = kShapes[0], &half = kShapes[1];
+    const float us[2] = {KB * tall.one[e] + kTileUs, KB * half.one[e] + kTileUs};
+    const float wide = (float)((a.n + tall.bn - 1) / tall.bn) / cus;
+    least = overlap(fmaxf((a.m / tall.bm * us[0] + active * us[1]) * wide + 0.25f * us[0], us[0]));
+    best = Plan{kMixedTiles, 1};
+  }
   for (int i = 0; i < kShapeCount; ++i) {
     const Shape& s = kShapes[i];
     const long tiles = tiles_of(a, s);
@@ -709,7 +812,7 @@ Plan plan_of(const mira_fp8_gemm_args& a) {
       const long all = tiles * parts, full = all / (cus * s.per_cu), rest = all % (cus * s.per_cu);
       float us = full * (per * s.all[e] + kTileUs) +
                  (rest ? per * (rest > cus ? s.all[e] : s.one[e]) + kTileUs : 0.f);
-      us = us > arrive ? us + 0.2f * arrive : arrive + 0.2f * us;  // the two overlap, not wholly
+      us = overlap(us);
       if (parts > 1) us += kJoinUs + (float)parts * a.m * a.n * 8.f / kJoinBytesPerUs;
       if (best.S == 0 || us < least) {
         least = us;
@@ -736,9 +839,16 @@ void launch_few(const GemmParams& p, long tiles, hipStream_t st) {
   else launch_timed(kFew.name, fp8_gemm_few_kernel<false, EXACT, OutT>, grid, dim3(256), 0, st, p, nT);
 }
 
+void launch_mixed(const GemmParams& p, long tiles, hipStream_t st) {
+  // each XCD's share of the tall and of the half tiles is rounded up
+  const dim3 grid((uint32_t)((tiles + 7) / 8 * 8 + 8));
+  launch_timed(kMixed.name, fp8_gemm_mixed_kernel, grid, dim3(512), 0, st, p, (p.N + kMixed.bn - 1) / kMixed.bn);
+}
+
 template <bool EXACT, typename OutT>
 void launch_shape(const GemmParams& p, int i, long tiles, hipStream_t st) {
-  if (i == kShapeCount) return launch_few<EXACT, OutT>(p, tiles, st);
+  if (i == kFewRows) return launch_few<EXACT, OutT>(p, tiles, st);
+  if (i == kMixedTiles) return launch_mixed(p, tiles, st);
   const Shape& shape = kShapes[i];
   switch (i) {
     case 0: launch_tile<8, 4, 2, 4, 2, EXACT, OutT>(p, shape, tiles, st); break;
@@ -788,7 +898,7 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.w_stride = a.w_stride ? a.w_stride : a.n * p.ldw;
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
-  const long tiles = tiles_of(a, plan.shape == kShapeCount ? kFew : kShapes[plan.shape]);
+  const long tiles = tiles_of(a, shape_of(plan.shape));
   if (a.out_dtype == MIRA_F32) launch_shape<true, float>(p, plan.shape, tiles, st);
   else launch_shape<false, uint16_t>(p, plan.shape, tiles, st);
   return hipGetLastError();

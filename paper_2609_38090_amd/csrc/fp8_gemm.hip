@@ -211,50 +211,60 @@ __device__ __forceinline__ bool find_tile(const GemmParams& p, int nT, int* shar
   return t.nt >= 0;
 }
 
-// The same with tiles of two heights: BM rows, and for a group's last BM / 2 rows or
-// fewer half as many.  The tall ones, which take longer, come first on every XCD.
+// The same with tiles of three heights: BM rows, and for a group's last rows BM, BM / 2
+// or BM / 4 (height 0, 1, 2).  The taller ones, which take longer, come first on
+// every XCD.
 template <int BM>
-__device__ __forceinline__ bool find_mixed_tile(const GemmParams& p, int nT, int* shared, Tile& t, bool& tall) {
+__device__ __forceinline__ bool find_mixed_tile(const GemmParams& p, int nT, int* shared, Tile& t, int& height) {
   if (threadIdx.x < 64) {
     const int l = threadIdx.x;
     Rows r[4];
-    int n[2][4], sum[2] = {0, 0}, end[2];  // [0] tall, [1] half
+    int n[3][4], sum[3] = {0, 0, 0}, end[3], mT[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       r[i] = 4 * l + i < p.G ? rows_of(p, 4 * l + i) : Rows{0, 0};
       const int rows = r[i].hi - r[i].lo, rest = rows % BM;
       n[0][i] = rows / BM + (rest > BM / 2);
-      n[1][i] = rest > 0 && rest <= BM / 2;
-      sum[0] += n[0][i];
-      sum[1] += n[1][i];
-    }
+      n[1][i] = rest > BM / 4 && rest <= BM / 2;
+      n[2][i] = rest > 0 && rest <= BM / 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 3; ++h) sum[h] += n[h][i];
+    }
+    const int groups = min(p.G, p.M);
+#pragma unroll
+    for (int h = 0; h < 3; ++h) {
       end[h] = sum[h];
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int v = __shfl_up(end[h], o, 64);
         if (l >= o) end[h] += v;
       }
+      mT[h] = min(__shfl(end[h], 63, 64), (h ? 0 : p.M / BM) + groups);  // (more only where offsets overlap)
     }
-    const int groups = min(p.G, p.M);  // (more tiles only where offsets overlap)
-    const int mT0 = min(__shfl(end[0], 63, 64), p.M / BM + groups), mT1 = min(__shfl(end[1], 63, 64), groups);
-    const int i = blockIdx.x >> 3, per0 = (mT0 * nT + 7) >> 3;
-    const int h = i < per0 ? 0 : 1;
+    int i = blockIdx.x >> 3, h = 0, at = end[0] - sum[0], all = mT[0];
+#pragma unroll
+    for (int j = 1; j < 3; ++j) {
+      const int per = (all * nT + 7) >> 3;
+      if (h == j - 1 && i >= per) {
+        i -= per;
+        h = j;
+        at = end[j] - sum[j];
+        all = mT[j];
+      }
+    }
     int mt = 0, nt = 0, part = 0;
-    const bool any = tile_number(h ? i - per0 : i, h ? mT1 : mT0, nT, 1, mt, nt, part);
+    const bool any = tile_number(i, all, nT, 1, mt, nt, part);
     if (l == 0) {
       shared[0] = any ? nt : -1;
       shared[4] = h;
     }
-    int at = h ? end[1] - sum[1] : end[0] - sum[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = h ? n[1][i] : n[0][i];
+    for (int j = 0; j < 4; ++j) {
+      const int c = h == 0 ? n[0][j] : h == 1 ? n[1][j] : n[2][j];
       if (any && mt >= at && mt < at + c) {
-        shared[1] = 4 * l + i;
-        shared[2] = r[i].lo + (h ? (r[i].hi - r[i].lo) / BM : mt - at) * BM;
-        shared[3] = r[i].hi;
+        shared[1] = 4 * l + j;
+        shared[2] = r[j].lo + (h ? (r[j].hi - r[j].lo) / BM : mt - at) * BM;
+        shared[3] = r[j].hi;
       }
       at += c;
     }
@@ -263,7 +273,7 @@ __device__ __forceinline__ bool find_mixed_tile(const GemmParams& p, int nT, int
   t.nt = __builtin_amdgcn_readfirstlane(shared[0]);
   t.g = __builtin_amdgcn_readfirstlane(shared[1]);
   t.m0 = __builtin_amdgcn_readfirstlane(shared[2]);
-  tall = __builtin_amdgcn_readfirstlane(shared[4]) == 0;
+  height = __builtin_amdgcn_readfirstlane(shared[4]);
   t.m1 = min(t.m0 + BM, __builtin_amdgcn_readfirstlane(shared[3]));
   t.part = 0;
   return t.nt >= 0;
@@ -598,10 +608,11 @@ __global__ __launch_bounds__(512) void fp8_gemm_mixed_kernel(GemmParams p, int n
   constexpr int most = tall_lds > half_lds ? tall_lds : half_lds;
   __shared__ int tile_s[5];
   Tile t;
-  bool tall;
-  if (!find_mixed_tile<256>(p, nT, tile_s, t, tall)) return;
-  if (tall) tile_body<8, 4, 2, 4, 2, false, uint16_t, most>(p, t);
-  else tile_body<4, 4, 4, 2, 3, false, uint16_t, most>(p, t);
+  int height;
+  if (!find_mixed_tile<256>(p, nT, tile_s, t, height)) return;
+  if (height == 0) tile_body<8, 4, 2, 4, 2, false, uint16_t, most>(p, t);
+  else if (height == 1) tile_body<4, 4, 4, 2, 3, false, uint16_t, most>(p, t);
+  else tile_body<4, 2, 4, 2, 3, false, uint16_t, most>(p, t);
 }
 
 // ---- few rows --------------------------------------------------------------------
@@ -840,8 +851,8 @@ void launch_few(const GemmParams& p, long tiles, hipStream_t st) {
 }
 
 void launch_mixed(const GemmParams& p, long tiles, hipStream_t st) {
-  // each XCD's share of the tall and of the half tiles is rounded up
-  const dim3 grid((uint32_t)((tiles + 7) / 8 * 8 + 8));
+  // each XCD's share of each height is rounded up
+  const dim3 grid((uint32_t)((tiles + 7) / 8 * 8 + 16));
   launch_timed(kMixed.name, fp8_gemm_mixed_kernel, grid, dim3(512), 0, st, p, (p.N + kMixed.bn - 1) / kMixed.bn);
 }
 

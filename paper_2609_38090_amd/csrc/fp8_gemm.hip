@@ -596,13 +596,14 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
   tile_body<NT, MT, WN, WM, NS, EXACT, OutT>(p, t);
 }
 
-// Groups in tiles of 256 weight rows by 256 or 128 token rows: a tile of 256 costs 1.5
-// times one of 128, and a group's end leaves half of its last one empty on average.
-// us, so and in tiles of 128: 12288 rows spread evenly over 64 experts of 2816 x 2048
-// 142 and 159 (in tiles of 256 140), unevenly 168 and 164 (188), 12288 unevenly over
-// 64 of 2048 x 1408 92 and 102, 8192 over 32 of 4096 x 1024 93 and 100.  The tall
-// ones first: mixed evenly over the launch 101 and 99 for the last two.  Only with bf16
-// out: with the widening as well the two bodies spill registers.
+// Groups in tiles of 256 weight rows by 256, 128 or 64 token rows: the lower ones cost
+// 0.65 and 0.45 of a whole one, which a group's end half fills on average.  us, so and
+// in tiles of one height, the best of them: 12288 rows unevenly over 64 experts of
+// 2816 x 2048 158 and 164 (128 rows; 188 of 256), evenly 142 and 140 (256; 160 of 128),
+// unevenly over 64 of 2048 x 1408 85 and 102, 8192 over 32 of 4096 x 1024 90 and
+// 100, 4096 over 64 of 2816 x 2048 98 and 109 (64 rows).  Tall ones first: with whole
+// and half tiles in turn throughout the launch 101 and 99 for the third and fourth,
+// 92 and 93 so.  Only with bf16 out: with the widening the bodies spill registers.
 __global__ __launch_bounds__(512) void fp8_gemm_mixed_kernel(GemmParams p, int nT) {
   constexpr int tall_lds = tile_lds<8, 4, 2, 4, 2>(), half_lds = tile_lds<4, 4, 4, 2, 3>();
   constexpr int most = tall_lds > half_lds ? tall_lds : half_lds;
@@ -806,11 +807,11 @@ Plan plan_of(const mira_fp8_gemm_args& a) {
   Plan best{0, 0};
   float least = 0.f;
   if (a.offsets && !e && tiles_of(a, kMixed) <= kMaxTiles) {
-    // the rows' whole tiles, a half tile for each group, and a part of one until the last ends
-    const Shape &tall = kShapes[0], &half = kShapes[1];
-    const float us[2] = {KB * tall.one[e] + kTileUs, KB * half.one[e] + kTileUs};
-    const float wide = (float)((a.n + tall.bn - 1) / tall.bn) / cus;
-    least = overlap(fmaxf((a.m / tall.bm * us[0] + active * us[1]) * wide + 0.25f * us[0], us[0]));
+    // the rows' whole tiles, a lower one for each group (0.8 us a stage, between a half
+    // and a quarter tile), and a part of one until the last ends
+    const float whole = KB * kShapes[0].one[e] + kTileUs, low = KB * 0.8f + kTileUs;
+    const float wide = (float)((a.n + kMixed.bn - 1) / kMixed.bn) / cus;
+    least = overlap(fmaxf((a.m / kMixed.bm * whole + active * low) * wide + 0.25f * whole, whole));
     best = Plan{kMixedTiles, 1};
   }
   for (int i = 0; i < kShapeCount; ++i) {

@@ -94,10 +94,10 @@ __device__ __forceinline__ void store_out<uint16_t>(uint16_t* p, float v) {
 // fp32 out (four bf16 instructions and the widening for each fp8 one) it takes 750
 // us, 1.28 PFLOP/s.  A tile's start and end, 5 us and 2 more with groups, are not
 // hidden (one workgroup fills a CU's LDS): 12288 rows over 64 experts, 2816 x 2048,
-// 164 us for 510 MB and 141 GFLOP.  Measured and slower: a persistent walk with the
+// 158 us for 141 GFLOP.  Measured and slower: a persistent walk with the
 // next tile's loads before the stores (482 us against 481), prefetching into L2 (512
-// to 524 against 487), deeper rings, 128 x 128 tiles two to a CU (594; 181 against 164
-// over the experts).
+// to 524 against 487; 176 to 193 against 168 over the experts), deeper rings, 128 x 128
+// tiles two to a CU (594; 181 against 164 over the experts).
 
 // One direct-to-LDS load of a wave: lane l's bytes go to LDS address m0 + 16 l.  The
 // compiler does not see these loads; every wait for them is the explicit one at

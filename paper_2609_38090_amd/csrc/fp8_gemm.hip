@@ -603,17 +603,25 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_gemm_tile_kernel(GemmParams 
 // unevenly over 64 of 2048 x 1408 85 and 102, 8192 over 32 of 4096 x 1024 90 and
 // 100, 4096 over 64 of 2816 x 2048 98 and 109 (64 rows).  Tall ones first: with whole
 // and half tiles in turn throughout the launch 101 and 99 for the third and fourth,
-// 92 and 93 so.  Only with bf16 out: with the widening the bodies spill registers.
+// 92 and 93 so.  With fp32 out the heights are 128, 64 and 32, since with the widening a
+// kernel of the taller ones spills registers: the first, second and third 232 and 246, 224
+// and 235, 126 and 140; 1024 over 64 of 2816 x 2048 76 and 86.
+template <bool EXACT, typename OutT>
 __global__ __launch_bounds__(512) void fp8_gemm_mixed_kernel(GemmParams p, int nT) {
-  constexpr int tall_lds = tile_lds<8, 4, 2, 4, 2>(), half_lds = tile_lds<4, 4, 4, 2, 3>();
-  constexpr int most = tall_lds > half_lds ? tall_lds : half_lds;
   __shared__ int tile_s[5];
   Tile t;
   int height;
-  if (!find_mixed_tile<256>(p, nT, tile_s, t, height)) return;
-  if (height == 0) tile_body<8, 4, 2, 4, 2, false, uint16_t, most>(p, t);
-  else if (height == 1) tile_body<4, 4, 4, 2, 3, false, uint16_t, most>(p, t);
-  else tile_body<4, 2, 4, 2, 3, false, uint16_t, most>(p, t);
+  if (!find_mixed_tile<EXACT ? 128 : 256>(p, nT, tile_s, t, height)) return;
+  constexpr int most = tile_lds<4, 4, 4, 2, 3>();
+  if constexpr (EXACT) {
+    if (height == 0) tile_body<4, 4, 4, 2, 3, true, OutT, most>(p, t);
+    else if (height == 1) tile_body<4, 2, 4, 2, 3, true, OutT, most>(p, t);
+    else tile_body<4, 1, 4, 2, 3, true, OutT, most>(p, t);
+  } else {
+    if (height == 0) tile_body<8, 4, 2, 4, 2, false, OutT, most>(p, t);
+    else if (height == 1) tile_body<4, 4, 4, 2, 3, false, OutT, most>(p, t);
+    else tile_body<4, 2, 4, 2, 3, false, OutT, most>(p, t);
+  }
 }
 
 // ---- few rows --------------------------------------------------------------------
@@ -766,7 +774,9 @@ constexpr Shape kShapes[] = {
     {"fp8_gemm_64x16", 64, 16, 3, {0.25f, 0.3f}, {0.4f, 0.5f}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
-constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}}, kMixed = {"fp8_gemm_mixed", 256, 256, 1, {}, {}};
+constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}}, kMixed[] = {
+    {"fp8_gemm_mixed", 256, 256, 1, {}, {}}, {"fp8_gemm_mixed", 256, 128, 1, {}, {}}};  // bf16, fp32 out
+
 enum : int { kFewRows = kShapeCount, kMixedTiles };
 constexpr float kTileUs = 2.5f, kJoinUs = 8.f, kJoinBytesPerUs = 7e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
@@ -775,7 +785,7 @@ constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
 struct Plan {
   int shape, S;  // S = 0: no shape fits one launch
 };
-const Shape& shape_of(int i) { return i == kFewRows ? kFew : i == kMixedTiles ? kMixed : kShapes[i]; }
+const Shape& shape_of(int i, int e) { return i == kFewRows ? kFew : i == kMixedTiles ? kMixed[e] : kShapes[i]; }
 
 long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
   // with offsets an upper bound: every group may end inside a tile
@@ -806,12 +816,12 @@ Plan plan_of(const mira_fp8_gemm_args& a) {
   const auto overlap = [&](float us) { return us > arrive ? us + 0.2f * arrive : arrive + 0.2f * us; };  // not wholly
   Plan best{0, 0};
   float least = 0.f;
-  if (a.offsets && !e && tiles_of(a, kMixed) <= kMaxTiles) {
-    // the rows' whole tiles, a lower one for each group (0.8 us a stage, between a half
-    // and a quarter tile), and a part of one until the last ends
-    const float whole = KB * kShapes[0].one[e] + kTileUs, low = KB * 0.8f + kTileUs;
-    const float wide = (float)((a.n + kMixed.bn - 1) / kMixed.bn) / cus;
-    least = overlap(fmaxf((a.m / kMixed.bm * whole + active * low) * wide + 0.25f * whole, whole));
+  if (a.offsets && tiles_of(a, kMixed[e]) <= kMaxTiles) {
+    // the rows' whole tiles, a lower one for each group (us a stage, between a half and
+    // a quarter tile), and a part of one until the last ends
+    const float whole = KB * kShapes[e].one[e] + kTileUs, low = KB * (e ? 0.9f : 0.8f) + kTileUs;
+    const float wide = (float)((a.n + kMixed[e].bn - 1) / kMixed[e].bn) / cus;
+    least = overlap(fmaxf((a.m / kMixed[e].bm * whole + active * low) * wide + (e ? 0.5f : 0.25f) * whole, whole));
     best = Plan{kMixedTiles, 1};
   }
   for (int i = 0; i < kShapeCount; ++i) {
@@ -851,16 +861,18 @@ void launch_few(const GemmParams& p, long tiles, hipStream_t st) {
   else launch_timed(kFew.name, fp8_gemm_few_kernel<false, EXACT, OutT>, grid, dim3(256), 0, st, p, nT);
 }
 
+template <bool EXACT, typename OutT>
 void launch_mixed(const GemmParams& p, long tiles, hipStream_t st) {
+  const Shape& shape = kMixed[EXACT];
   // each XCD's share of each height is rounded up
   const dim3 grid((uint32_t)((tiles + 7) / 8 * 8 + 16));
-  launch_timed(kMixed.name, fp8_gemm_mixed_kernel, grid, dim3(512), 0, st, p, (p.N + kMixed.bn - 1) / kMixed.bn);
+  launch_timed(shape.name, fp8_gemm_mixed_kernel<EXACT, OutT>, grid, dim3(512), 0, st, p, (p.N + shape.bn - 1) / shape.bn);
 }
 
 template <bool EXACT, typename OutT>
 void launch_shape(const GemmParams& p, int i, long tiles, hipStream_t st) {
   if (i == kFewRows) return launch_few<EXACT, OutT>(p, tiles, st);
-  if (i == kMixedTiles) return launch_mixed(p, tiles, st);
+  if (i == kMixedTiles) return launch_mixed<EXACT, OutT>(p, tiles, st);
   const Shape& shape = kShapes[i];
   switch (i) {
     case 0: launch_tile<8, 4, 2, 4, 2, EXACT, OutT>(p, shape, tiles, st); break;
@@ -910,7 +922,7 @@ hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st) {
   p.w_stride = a.w_stride ? a.w_stride : a.n * p.ldw;
   p.ws_stride = a.ws_stride ? a.ws_stride : nb * p.ld_ws;
   p.ldo = a.ldo ? a.ldo : a.n;
-  const long tiles = tiles_of(a, shape_of(plan.shape));
+  const long tiles = tiles_of(a, shape_of(plan.shape, a.out_dtype == MIRA_F32));
   if (a.out_dtype == MIRA_F32) launch_shape<true, float>(p, plan.shape, tiles, st);
   else launch_shape<false, uint16_t>(p, plan.shape, tiles, st);
   return hipGetLastError();

@@ -181,12 +181,14 @@ def test_groups(sizes, lo, tail, N, K, out):
 
 
 # ends on either side of a quarter of a tile, of half and of a whole one; gathered, and rows of no group
-@pytest.mark.parametrize("sizes,lo,tail", [([256, 128, 129, 0, 255, 257, 1, 600], 0, 0), ([127, 128, 129, 383, 384, 385], 3, 5), ([63, 64, 65, 0, 319, 320, 321], 0, 0),
+@pytest.mark.parametrize("sizes,lo,tail", [([256, 128, 129, 0, 255, 257, 1, 600], 0, 0), ([127, 128, 129, 383, 384, 385], 3, 5), ([63, 64, 65, 0, 319, 320, 321], 0, 0), ([31, 32, 33, 95, 96, 97, 700], 0, 0),
                                            ([1, 2, 3, 1, 1500, 0, 0, 1], 0, 0), ([0, 1500, 0], 0, 130)])
 @pytest.mark.parametrize("K,top_k", [(300, 0), (1111, 2), (128, 6)])
-def test_tiles_of_several_heights(sizes, lo, tail, K, top_k):
-    c = Case(sum(sizes) + lo + tail, 12001, K, "bf16", G=len(sizes), sizes=sizes, lo=lo, tail=tail, top_k=top_k, T=311 if top_k else 0)
-    assert _ran(c) == {"fp8_gemm_mixed"}
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_tiles_of_several_heights(sizes, lo, tail, K, top_k, out):
+    c = Case(sum(sizes) + lo + tail, 12001, K, out, G=len(sizes), sizes=sizes, lo=lo, tail=tail, top_k=top_k, T=311 if top_k else 0)
+    ran = _ran(c)
+    assert ran == {"fp8_gemm_mixed"} or (out == "f32" and (K == 128 or len(sizes) == 3))  # (tiles of one height may suit these)
     c.check()
 
 

@@ -488,7 +488,8 @@ typedef struct mira_fp8_gemm_args {
 } mira_fp8_gemm_args;
 
 /* Bytes of workspace of this call (its sizes, types and whether offsets is NULL
- * count, other pointers are not looked at); 0 is possible.  SIZE_MAX for sizes
+ * count, other pointers are not looked at); 0 is possible, and fewer rows may need
+ * more: a program asks for each size that it runs, and takes the largest.  SIZE_MAX for sizes
  * that mira_fp8_gemm refuses. */
 size_t mira_fp8_gemm_workspace_bytes(const mira_fp8_gemm_args* a);
 

@@ -208,6 +208,17 @@ def test_one_group_with_offsets_and_gather(M):
     c.check()
 
 
+@pytest.mark.parametrize("M", [1, 7, 40, 300])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_gather_without_offsets_and_rows_of_zeros(M, out):
+    c = Case(M, 140, 500, out, top_k=3, T=11)
+    c.x[0, 5] = 0x7F  # the row that a row of zeros reads in place of its own
+    c.order[::4] = -1
+    c.run()
+    c.check()
+    assert (c.out[:M:4, :140] == 0).all()
+
+
 @pytest.mark.parametrize("M", [2, 40, 300])
 def test_nan_stays_in_its_row_and_column(M):
     c = Case(M, 160, 300, "f32")
@@ -248,7 +259,8 @@ def test_rows_do_not_depend_on_their_company():
     assert torch.equal(c.run()[:200], a[p.cuda()])
 
 
-@pytest.mark.parametrize("M,N,K,G", [(1, 300, 8192, 1), (40, 300, 600, 1), (600, 300, 600, 1), (64, 100, 256, 8)])
+@pytest.mark.parametrize("M,N,K,G", [(1, 300, 8192, 1), (40, 300, 600, 1), (600, 300, 600, 1), (64, 100, 256, 8), (6, 300, 4100, 3),
+                                     (40, 300, 9000, 1), (800, 6000, 700, 4)])
 def test_other_stream_and_graph(M, N, K, G):
     c = Case(M, N, K, "f32", G=G, sizes=[M // G] * G if G > 1 else None)
     want = c.run().clone()
@@ -264,6 +276,25 @@ def test_other_stream_and_graph(M, N, K, G):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(c.out, want)
+
+
+def test_offsets_that_do_not_ascend_stay_inside_tiles_of_several_heights():
+    for off in ([0, 700, 20, 1500, 300], [-5, 10, 99999, 20, 0], [1500, 0, 0, 0, 0], [0, 1500, 0, 1500, 0], [0, 1500, 1500, 0, 1500]):
+        for out in ("bf16", "f32"):
+            c = Case(1500, 12001, 300, out, G=4, sizes=[375] * 4)
+            c.off = torch.tensor(off, dtype=torch.int32)
+            assert _ran(c) == {"fp8_gemm_mixed"}
+            res = c.out.double().cpu()
+            assert (res[c.M:] == -77).all() and (res[:, c.N:] == -77).all()
+
+
+def test_offsets_that_do_not_ascend_stay_inside_few_rows():
+    for off in ([0, 12, 3, 16], [-5, 10, 99999, 20], [16, 0, 0, 0], [0, 16, 0, 16]):
+        c = Case(16, 83, 300, "bf16", G=3, sizes=[5, 5, 6])
+        c.off = torch.tensor(off, dtype=torch.int32)
+        assert _ran(c) == {"fp8_gemm_few"}
+        res = c.out.double().cpu()
+        assert (res[c.M:] == -77).all() and (res[:, c.N:] == -77).all()
 
 
 def test_offsets_that_do_not_ascend_stay_inside():

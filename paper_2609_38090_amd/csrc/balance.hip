@@ -267,17 +267,20 @@ __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int 
   const uint32_t end = (uint32_t)hi * q.k;  // T * k is at most 2^30
   constexpr int kFlight = 4;
   for (uint32_t i = (uint32_t)lo * q.k + threadIdx.x; i < end; i += kFlight * THREADS) {
-    int e[kFlight];
-    bool keep[kFlight];
+    int e[kFlight], keep[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const uint32_t at = min(i + j * THREADS, end - 1);
-      e[j] = q.idx[at];
-      keep[j] = i + j * THREADS < end && (!q.mask || q.mask[(uint32_t)((uint64_t)at * q.inv_k >> 34)] != 0);
+      e[j] = q.idx[min(i + j * THREADS, end - 1)];
+      keep[j] = 1;
+    }
+    if (q.mask) {  // (no load behind a condition of its own: it would be waited for before the next)
+#pragma unroll
+      for (int j = 0; j < kFlight; ++j)
+        keep[j] = q.mask[(uint32_t)((uint64_t)min(i + j * THREADS, end - 1) * q.inv_k >> 34)];
     }
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
-      if (keep[j] && (uint32_t)e[j] < (uint32_t)q.E) atomicAdd(hist + e[j], 1);
+      if (i + j * THREADS < end && keep[j] && (uint32_t)e[j] < (uint32_t)q.E) atomicAdd(hist + e[j], 1);
   }
   if (q.mask) {
     int n = 0;

@@ -259,7 +259,7 @@ __device__ __forceinline__ void reduce_groups(float acc[4], int E, float (*wave_
 // Counts the pairs of rows [lo, hi) into hist and the kept rows into *kept
 // (both in LDS, zeroed before).  Four loads of each thread are in flight, and a
 // pair's row comes by a product instead of a division (3904 masked rows of 5 of 5
-// experts: 24 us the call without, 18 so).  Counters of few experts are met by many
+// experts: 24 us the call without, 17 so).  Counters of few experts are met by many
 // lanes at once; counts in registers, added up by the waves, were not faster (1024
 // rows of 2 of 8: 9.2 us so, 10.4 in registers).
 template <int THREADS>

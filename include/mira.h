@@ -439,9 +439,10 @@ typedef struct mira_fp8_quant_args {
  * correctly rounded.  Values are expected finite; a NaN becomes e4m3's NaN at
  * its own place (it does not count for the maximum), an infinity gives its
  * block an infinite scale, so the block holds NaN.  silu(g) = g / (1 + exp(-g)) in
- * fp32.  The transposed copy holds the same bytes and scales, for products
- * that contract over the weight's rows (the gradient dX = dY W of a product
- * x W^T is the same product on the transposed copy). */
+ * fp32 (NaN for a gate of -inf); these rules hold for its product with up, which
+ * is an infinity where it passes fp32's range.  The transposed copy holds the same
+ * bytes and scales, for products that contract over the weight's rows (the gradient
+ * dX = dY W of a product x W^T is the same product on the transposed copy). */
 int mira_fp8_quantize(const mira_fp8_quant_args* a, hipStream_t stream);
 
 /* out[i][j] = sum_b xs[r][b] ws[g][j/128][b] sum over k of block b of

@@ -54,7 +54,9 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   const float t = -g * log2e;
   const float r = -fmaf(g, rest, fmaf(g, log2e, t));
   float e = __builtin_amdgcn_exp2f(t);
-  e = t < 127.f ? fmaf(e, r * 0.693147182464599609375f, e) : e;  // (infinite above)
+  // (above, e is near infinity or is it; below, it is nothing beside 1, and r infinite for
+  // gates whose t is)
+  e = fabsf(t) < 127.f ? fmaf(e, r * 0.693147182464599609375f, e) : e;
   return g * __builtin_amdgcn_rcpf(1.f + e) * u;
 }
 

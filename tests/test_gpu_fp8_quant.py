@@ -151,3 +151,40 @@ def test_other_stream_and_graph():
             g.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(u, v) for u, v in zip(want, (q, s, qt, st)))
+
+
+def _swiglu_rows(gates, ups, dt):
+    """One block a row: gate and up at column 5, gates of 0.5 and ups of 1 beside them;
+    the quantized values, the scales and the inputs as held, in 64 bits."""
+    n = len(gates)
+    x = torch.full((n, 256), 0.5)
+    x[:, 128:] = 1.0
+    x[:, 5], x[:, 133] = torch.tensor(gates, dtype=torch.float32), torch.tensor(ups, dtype=torch.float32)
+    x = x.to(torch.float32 if dt == "f32" else torch.bfloat16).cuda()
+    q, s, *_ = _run(x, n, 128, dt, 1, 256, mira.MIRA_FP8_SWIGLU)
+    s = s.cpu().numpy().astype(np.float64)
+    held = x.double().cpu().numpy()
+    return TABLE[q[:n, :128].cpu().numpy()], s[:, 0], held[:, 5], held[:, 133]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_swiglu_of_gates_up_to_the_largest(dt):
+    """g / (1 + exp(-g)) is g where exp(-g) is nothing beside 1, up to the largest gates;
+    an infinity, or a product beyond the range, loses its block; 0 times it only its place."""
+    top = 3.38e38  # below the largest value of both types
+    gates = [88.0, 200.0, 1e30, 2.3e38, 2.4e38, 2.5e38, 3e38, top, -88.0, -1e30, -2.5e38, -top]
+    ups = [0.5, -2.0, 1e-30, 0.5, 1e-3, 0.5, -0.25, 1.0, 1.0, 1.0, 1e3, -0.5]
+    v, s, g, u = _swiglu_rows(gates, ups, dt)
+    rest = 0.5 / (1 + np.exp(-0.5))
+    with np.errstate(over="ignore"):
+        want = g / (1 + np.exp(-g)) * u
+    scale = np.maximum(np.abs(want), rest) / 448
+    # exp within 2 steps, a sum, a quotient, a product, the scale's division: 10 half steps
+    assert (np.abs(s - scale) <= 10 * U32 * scale).all()
+    got = v[:, 5] * s
+    assert (np.abs(got - want) <= (2.0 ** -4 * (1 + 2.0 ** -10) + 12 * U32) * np.abs(want) + 2.0 ** -10 * s).all()
+    inf, nan = float("inf"), float("nan")
+    v, s, g, u = _swiglu_rows([inf, inf, top, 2.0, 2.0, inf, -inf, nan, 1.0], [0.5, -1e-30, 4.0, inf, -inf, 0.0, 1.0, 1.0, nan], dt)
+    assert np.isinf(s[:5]).all() and np.isnan(v[:5, 5]).all()
+    assert (np.abs(s[5:] - rest / 448) <= 10 * U32 * rest / 448).all()
+    assert np.isnan(v[5:, 5]).all() and np.isfinite(np.delete(v[5:], 5, 1)).all()

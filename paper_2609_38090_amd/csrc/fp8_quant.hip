@@ -54,10 +54,11 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   const float t = -g * log2e;
   const float r = -fmaf(g, rest, fmaf(g, log2e, t));
   float e = __builtin_amdgcn_exp2f(t);
-  // (above, e is near infinity or is it; below, it is nothing beside 1, and r infinite for
-  // gates whose t is)
-  e = fabsf(t) < 127.f ? fmaf(e, r * 0.693147182464599609375f, e) : e;
-  return g * __builtin_amdgcn_rcpf(1.f + e) * u;
+  // (above, e is infinite; below, it is nothing beside 1, and r infinite for gates whose t is)
+  e = fabsf(t) < 128.f ? fmaf(e, r * 0.693147182464599609375f, e) : e;
+  // (a quarter of 1 + e: the instruction gives 0 for a reciprocal below 2^-126, where g
+  // times it is still a normal number)
+  return g * (__builtin_amdgcn_rcpf(fmaf(e, 0.25f, 0.25f)) * 0.25f) * u;
 }
 
 // Vectors at the alignment of their elements: global loads take any, so rows of

@@ -188,3 +188,20 @@ def test_swiglu_of_gates_up_to_the_largest(dt):
     assert np.isinf(s[:5]).all() and np.isnan(v[:5, 5]).all()
     assert (np.abs(s[5:] - rest / 448) <= 10 * U32 * rest / 448).all()
     assert np.isnan(v[5:, 5]).all() and np.isfinite(np.delete(v[5:], 5, 1)).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_swiglu_of_gates_whose_exponential_is_near_the_largest(dt):
+    """Down to exp(-g) = 2^128 the quotient is held: it is a normal number though
+    1 / (1 + exp(-g)) alone is not."""
+    gates = [-80.0, -87.0, -87.3, -87.34, -87.5, -88.0, -88.5, -88.7]
+    for up in (1e30, -1e35, 3e38):
+        v, s, g, u = _swiglu_rows(gates, [up] * len(gates), dt)
+        keep = g > -88.72  # (bf16 holds the last one as -88.5)
+        assert keep.all()
+        want = g / (1 + np.exp(-g)) * u
+        scale = np.maximum(np.abs(want), 0.5 / (1 + np.exp(-0.5))) / 448
+        # 10 half steps as above, and the reciprocal's, held to 2^-149 of 2^-128: 2^-21
+        tol = 10 * U32 + 2.0 ** -21
+        assert (np.abs(s - scale) <= tol * scale).all()
+        assert (np.abs(v[:, 5] * s - want) <= (2.0 ** -4 * (1 + 2.0 ** -10) + 2 * tol) * np.abs(want) + 2.0 ** -10 * s).all()

@@ -370,3 +370,63 @@ def test_out_of_any_alignment(M, N, K, shift):
         got = flat[shift:shift + M * (N + 3)].view(M, N + 3)
         assert torch.equal(got[:, :N], want) and (got[:, N:] == -5).all()
         assert (flat[:shift] == -5).all() and (flat[shift + M * (N + 3):] == -5).all()
+
+
+# groups whose contraction is split into parts that a second launch adds (sizes, rows of no
+# group before and behind, columns, contraction): several groups, empty ones, one group of
+# nearly all rows, dense rows and gathered ones, shared pairs, rows of zeros
+@pytest.mark.parametrize("sizes,lo,tail,N,K", [
+    ([5, 0, 3, 7, 0, 0, 1, 9, 2, 0, 4, 3, 0, 1], 3, 4, 417, 9100), ([20, 0, 60, 17], 0, 0, 130, 9000), ([0, 0, 90, 0], 5, 2, 300, 8200),
+    ([70, 130, 0, 200, 31, 65, 100, 0, 64, 84], 0, 0, 381, 4693), ([37], 2, 1, 260, 9001)])
+@pytest.mark.parametrize("top_k,shared", [(0, 0), (2, 1)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_groups_in_parts(sizes, lo, tail, N, K, top_k, shared, out):
+    c = Case(sum(sizes) + lo + tail, N, K, out, G=len(sizes), sizes=sizes, lo=lo, tail=tail, top_k=top_k, T=29 if top_k else 0,
+             shared=shared, pads=(1, 1, 1, 2, 3))
+    if top_k:
+        c.x[0, 5] = 0x7F  # the row that a row of zeros reads in place of its own
+        c.order[::5] = -1
+    assert "fp8_gemm_join" in _ran(c)
+    c.check()
+    if top_k:
+        at = torch.arange(lo, c.M - tail)
+        assert (c.out[at[at % 5 == 0].cuda(), :N] == 0).all()
+
+
+def test_groups_in_parts_captured():
+    c = Case(42, 449, 6136, "f32", G=4, sizes=[20, 0, 3, 15], lo=1, tail=3, top_k=3, T=17, shared=1)
+    c.order[::5] = -1
+    assert "fp8_gemm_join" in _ran(c)
+    c.check()
+    want = c.out.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        mira.mira_fp8_gemm(c.args)
+    for _ in range(4):
+        c.out.fill_(-77.0)
+        c.keep[1].fill_(0xFF)  # the workspace's content does not matter
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want)
+
+
+def test_parts_write_only_their_workspace():
+    """The workspace in the middle of a buffer, and offsets that do not ascend."""
+    for off in (None, [0, 12, 3, 40], [-5, 10, 99999, 20], [40, 0, 0, 0], [0, 40, 0, 40]):
+        c = Case(40, 260, 9000, "f32", G=3 if off else 1, sizes=[13, 13, 14] if off else None)
+        if off:
+            c.off = torch.tensor(off, dtype=torch.int32)
+        assert "fp8_gemm_join" in _ran(c)
+        nb = c.args.workspace_bytes
+        assert nb > 0
+        guard = torch.full((nb + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+        c.args.workspace = guard[4096:]
+        assert c.args.workspace.data_ptr() % 256 == 0
+        mira.mira_fp8_gemm(c.args)
+        torch.cuda.synchronize()
+        assert (guard[:4096] == 0xA5).all() and (guard[4096 + nb:] == 0xA5).all()
+        out = c.out
+        assert (out[c.M:] == -77).all() and (out[:, c.N:] == -77).all()
+        if not off:
+            c.check()

@@ -100,3 +100,15 @@ def test_gemm_workspace():
 def test_empty_calls_are_no_ops():
     mira.mira_fp8_quantize(_quant(rows=0, x=None, q=None, scale=None), stream=1)
     mira.mira_fp8_gemm(_gemm(m=0, x=None, w=None, out=None), stream=1)
+
+
+def test_gemm_workspace_refusals():
+    """A call that splits its contraction refuses a smaller, misaligned or missing workspace,
+    with groups and without."""
+    for kw in (dict(m=20, n=260, k=9000, x_rows=20), dict(m=97, n=130, k=9000, x_rows=97, n_groups=4, offsets=0x9000)):
+        for dt in (mira.MIRA_F32, mira.MIRA_BF16):
+            need = mira.mira_fp8_gemm_workspace_bytes(_gemm(out_dtype=dt, **kw))
+            assert need > 0 and need % (4 * kw["m"] * kw["n"]) == 0
+            for bad, code in ((dict(workspace_bytes=need - 1), WORKSPACE), (dict(workspace_bytes=0), WORKSPACE),
+                              (dict(workspace=0x100010), ALIGN), (dict(workspace=None), ARG)):
+                _refused(mira.mira_fp8_gemm, _gemm(out_dtype=dt, **kw, **bad), code)

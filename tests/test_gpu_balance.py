@@ -325,3 +325,84 @@ def test_dispatch_bounds(T, E, k, G, ran):
     mira.mira_profile_enable(False)
     assert names == {"balance_" + n for n in ran}
     c.check()
+
+
+def _special(T, dt):
+    low = float(torch.finfo(torch.float32 if dt == "f32" else torch.bfloat16).min)
+
+    def tweak(c, x, rng):
+        x[3, 2] = -np.inf
+        x[4, :] = -np.inf
+        x[5, :] = low                 # the type's lowest value throughout
+        x[6, 1:] = low
+        x[7, :] *= 40.0
+        x[8, :], x[9, 1] = np.nan, np.inf   # dropped rows may hold anything
+        x[10, :-1] = -np.inf          # one expert is left
+        c.mask[:12] = 1
+        c.mask[8] = c.mask[9] = 0
+        c.idx[::3, 0] = -1            # not counted
+        c.idx[1::5, 1] = c.E
+        c.idx[2::7, 1] = 2 ** 30
+    return tweak
+
+
+# the special values of the tests above where a router is larger than they have it, each
+# width of its row's lanes
+@pytest.mark.parametrize("E", [9, 16, 17, 61, 64, 100, 256])
+@pytest.mark.parametrize("T", [30, 9000])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_special_logits_of_larger_routers(E, T, dt):
+    c = Case(T, E, 2, 1, dt, masked=True, tweak=_special(T, dt))
+    c.run()
+    loss, counts, mean, d = balance(c.x64, c.idx, np.array([0, T]), c.mask, c.coef, c.gl)
+    n = int((c.mask != 0).sum())
+    assert np.array_equal(c.out["counts"].cpu().numpy(), counts)
+    got = c.out["dlogits"].double().cpu().numpy()[:T]
+    assert (got[[4, 8, 9]] == 0).all() and got[3, 2] == 0 and (got[10, :-1] == 0).all()
+    # probabilities carry the rounding of arguments up to 300 (below, exp is 0): 2 * (300 + 24) half steps
+    tol = 4 * 2 * 324 * U32 * float(c.gl[0]) * c.coef / n * (counts.max() * E / (2 * n))
+    assert (np.abs(got - d) <= tol + (1.01 * U16 * np.abs(d) if dt == "bf16" else 0) + 1e-37).all()
+    assert np.abs(c.out["mean_prob"].cpu().numpy() - mean).max() <= (2 * 324 + 872) * U32
+    assert abs(float(c.out["loss"][0]) - loss[0]) <= (2 * 324 + 872 + 300) * U32 * loss[0]
+
+
+@pytest.mark.parametrize("E", [9, 16, 64, 250])
+@pytest.mark.parametrize("T", [30, 9000])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_nan_stays_in_its_row_and_group_of_larger_routers(E, T, bad):
+    def tweak(c, x, rng):
+        c.off = np.array([0, 10, T], np.int32)
+        x[12, 3] = bad
+    c = Case(T, E, 2, 2, tweak=tweak)
+    c.run()
+    assert torch.isnan(c.out["dlogits"][12]).all()
+    assert torch.isfinite(torch.cat([c.out["dlogits"][:12], c.out["dlogits"][13:]])).all()
+    assert torch.isfinite(c.out["loss"][0]) and torch.isnan(c.out["loss"][1])
+
+
+@pytest.mark.parametrize("off", [[0, 50, 20, 9000], [-5, 100, 99999, 200], [9000, 0, 0, 0], [0, 9000, 0, 9000], [20, 10, 10, 5]])
+@pytest.mark.parametrize("T,E", [(60, 8), (60, 64), (9000, 8), (9000, 64), (30000, 8), (30000, 61)])
+def test_offsets_that_do_not_ascend_write_only_their_buffers(T, E, off):
+    """Every buffer in the middle of a larger one; each way of counting."""
+    def tweak(c, x, rng):
+        c.off = np.array(off, np.int32)
+    c = Case(T, E, 2, 3, masked=True, tweak=tweak)
+    c.run()
+    want = {"small": T == 60, "zero": T == 30000}
+    G, pad = 3, 1024
+    sizes = dict(loss=G, counts=G * E, mean_prob=G * E, dlogits=T * E)
+    flat = {k: torch.full((n + 2 * pad,), 77, dtype=torch.int32 if k == "counts" else torch.float32, device="cuda") for k, n in sizes.items()}
+    for k, v in flat.items():
+        setattr(c.args, k, v[pad:])
+    ws = torch.full((c.args.workspace_bytes + 2 * pad,), 0xA5, dtype=torch.uint8, device="cuda")
+    c.args.workspace = ws[pad:]
+    mira.mira_profile_enable(True)
+    mira.mira_profile_read()
+    mira.mira_balance_loss(c.args)
+    torch.cuda.synchronize()
+    ran = set(mira.mira_profile_read())
+    mira.mira_profile_enable(False)
+    assert ("balance_group" in ran) == want["small"] and ("balance_zero" in ran) == want["zero"], ran
+    for k, v in flat.items():
+        assert (v[:pad] == 77).all() and (v[pad + sizes[k]:] == 77).all(), k
+    assert (ws[:pad] == 0xA5).all() and (ws[pad + c.args.workspace_bytes:] == 0xA5).all()

@@ -100,8 +100,9 @@ __device__ __forceinline__ float exp_neg(float x) {
 }
 
 // The logits of a row that a lane holds, up to four: VEC: 4l .. 4l+3 (E a multiple
-// of 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.  At most
-// kFewExperts experts take the largest power of two of lanes that they fill.
+// of 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.  FEW: the largest power
+// of two of lanes that the experts fill, at most two values a lane; four would leave
+// most lanes of so short a row without any.
 constexpr int kFewExperts = 8;
 template <int L, bool VEC>
 __device__ __forceinline__ int expert_of(int l, int i) {
@@ -167,14 +168,18 @@ __device__ __forceinline__ float grad_scale(const BalanceParams& q, float grad, 
 // Softmax, gradient and sums of p of rows lo, lo + step, .. < hi for one lane
 // group of L lanes (lane l of it); acc holds the lane's sums of p.  U rows are
 // in flight at once.
-// FEW (at most kFewExperts): expf and the formula's own operations, each rounded
-// once and none contracted.  With as many selected as there are experts the
-// gradient is zero but for its roundings; these are then those of the formula
-// evaluated step by step, not of a rearrangement.
-template <int L, bool VEC, bool FEW, int U, typename T>
+// STEP (few experts, all of them selected): expf and the formula's own operations,
+// each rounded once and none contracted.  The gradient is zero then but for its
+// roundings, and these are those of the formula evaluated step by step, not of a
+// rearrangement.  Either way they are fewer than 24 half steps; that costs little where
+// rows are short (131072 of 8: 21.9 us, 20.7 without) and more from 9 experts on (of
+// 16: 25.1 against 20.6, 500 of 16: 9.4 against 5.7), which therefore never take it.
+template <int L, bool VEC, bool FEW, bool STEP, int U, typename T>
 __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi, int step, int l,
                                           const int counts[4], int n, float grad, float acc[4]) {
+  static_assert(FEW || !STEP, "few experts");
   constexpr int NV = FEW ? 2 : 4;  // values that a lane may hold
+  const bool two = !FEW || q.E > L;  // the lanes' second values exist (FEW: E is no power of two)
   const T* x = (const T*)q.logits;
   T* d = (T*)q.dlogits;
   for (int r0 = lo; r0 < hi; r0 += U * step) {
@@ -204,9 +209,8 @@ __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi
       m = lanes_reduce<L, MaxOp>(m);
       m = m == -INFINITY ? 0.f : m;
       float o[4] = {0.f, 0.f, 0.f, 0.f};
-      if constexpr (FEW) {
+      if constexpr (STEP) {
 #pragma clang fp contract(off)
-        const bool two = q.E > L;  // the lanes' second values exist (E is no power of two)
         float e0 = expf(v[u][0] - m), e1 = two ? expf(v[u][1] - m) : 0.f;
         const float s = lanes_reduce<L, AddOp>(e0 + e1);
         e0 = s == 0.f ? 0.f : e0 / s;
@@ -223,6 +227,7 @@ __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi
         float s = 0.f, w = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+          if (i == 1 && !two) break;
           v[u][i] = exp_neg(v[u][i] - m);
           s += v[u][i];
           w = fmaf(f[i], v[u][i], w);
@@ -233,6 +238,7 @@ __device__ __forceinline__ void rows_pass(const BalanceParams& q, int lo, int hi
         w *= inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+          if (i == 1 && !two) break;
           const float p = v[u][i] * inv;
           acc[i] += keep[u] ? p : 0.f;
           o[i] = keep[u] ? gscale * p * (f[i] - w) : 0.f;
@@ -291,7 +297,7 @@ __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int 
 
 // One workgroup per group: counts, rows, means and loss.  Bound by latency: a launch,
 // the counts' loads, then the rows' (16 rows of 8 experts 4.4 us of the call's 5.5).
-template <int L, bool VEC, bool FEW, int THREADS, typename T>
+template <int L, bool VEC, bool FEW, bool STEP, int THREADS, typename T>
 __global__ __launch_bounds__(THREADS) void balance_group_kernel(BalanceParams q) {
   __shared__ int hist[MIRA_MAX_EXPERTS];
   __shared__ int kept;
@@ -313,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void balance_group_kernel(BalanceParams q)
     const int e = expert_of<L, VEC>(l, i);
     counts[i] = e < q.E ? hist[e] : 0;
   }
-  rows_pass<L, VEC, FEW, FEW ? 4 : 2, T>(q, s.lo + t / L, s.hi, THREADS / L, l, counts, n, group_grad(q, g), acc);
+  rows_pass<L, VEC, FEW, STEP, FEW ? 4 : 2, T>(q, s.lo + t / L, s.hi, THREADS / L, l, counts, n, group_grad(q, g), acc);
   reduce_groups<L, VEC, THREADS>(acc, q.E, wave_sums);
   __syncthreads();
   float term = 0.f;
@@ -453,7 +459,7 @@ __device__ __forceinline__ void finish_group(const BalanceParams& q, int g, cons
 // two rows of each lane group in flight measured best (512 threads and 512 chunks 86 us
 // the call against 76; a scalar path for row lengths that are no multiple of four
 // takes 76 where vectors at any alignment took 80).
-template <int L, bool VEC, bool FEW, typename T>
+template <int L, bool VEC, bool FEW, bool STEP, typename T>
 __global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams q) {
   __shared__ float wave_sums[kBigThreads / 64][MIRA_MAX_EXPERTS];
   __shared__ int last;
@@ -468,7 +474,7 @@ __global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams
       const int e = expert_of<L, VEC>(l, i);
       counts[i] = q.counts[(size_t)g * q.E + min(e, q.E - 1)];
     }
-    rows_pass<L, VEC, FEW, FEW ? 4 : 2, T>(q, a + t / L, b, kBigThreads / L, l, counts, n, group_grad(q, g), acc);
+    rows_pass<L, VEC, FEW, STEP, FEW ? 4 : 2, T>(q, a + t / L, b, kBigThreads / L, l, counts, n, group_grad(q, g), acc);
     if (!q.mean && !q.loss) return;
     __syncthreads();
     reduce_groups<L, VEC, kBigThreads>(acc, q.E, wave_sums);
@@ -531,15 +537,15 @@ BalanceLayout balance_layout(int E, int G) {
   return w;
 }
 
-template <int L, bool VEC, bool FEW, typename T>
+template <int L, bool VEC, bool FEW, bool STEP, typename T>
 void launch_rows(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
   // a group of more than one pass of 256 threads gets a larger workgroup
   if (small && (size_t)q.T * L <= (size_t)q.G * 256)
-    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, 256, T>, dim3(q.G), dim3(256), 0, st, q);
+    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, STEP, 256, T>, dim3(q.G), dim3(256), 0, st, q);
   else if (small)
-    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, kBigThreads, T>, dim3(q.G), dim3(kBigThreads), 0, st, q);
+    launch_timed("balance_group", balance_group_kernel<L, VEC, FEW, STEP, kBigThreads, T>, dim3(q.G), dim3(kBigThreads), 0, st, q);
   else
-    launch_timed("balance_rows", balance_rows_kernel<L, VEC, FEW, T>, dim3(chunks), dim3(kBigThreads), 0, st, q);
+    launch_timed("balance_rows", balance_rows_kernel<L, VEC, FEW, STEP, T>, dim3(chunks), dim3(kBigThreads), 0, st, q);
 }
 
 // Lanes of a row: the largest power of two up to E for few experts, else the
@@ -553,28 +559,29 @@ int row_lanes(int E) {
   return lanes;
 }
 
-template <typename T>
+template <bool STEP, typename T>
 void launch_few(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
   switch (row_lanes(q.E)) {
-    case 1: return launch_rows<1, false, true, T>(q, small, chunks, st);
-    case 2: return launch_rows<2, false, true, T>(q, small, chunks, st);
-    case 4: return launch_rows<4, false, true, T>(q, small, chunks, st);
-    default: return launch_rows<8, false, true, T>(q, small, chunks, st);
+    case 1: return launch_rows<1, false, true, true, T>(q, small, chunks, st);  // (its expert is always selected)
+    case 2: return launch_rows<2, false, true, STEP, T>(q, small, chunks, st);
+    case 4: return launch_rows<4, false, true, STEP, T>(q, small, chunks, st);
+    default: return launch_rows<8, false, true, STEP, T>(q, small, chunks, st);
   }
 }
 template <bool VEC, typename T>
 void launch_many(const BalanceParams& q, bool small, int chunks, hipStream_t st) {
   switch (row_lanes(q.E)) {
-    case 4: return launch_rows<4, VEC, false, T>(q, small, chunks, st);
-    case 8: return launch_rows<8, VEC, false, T>(q, small, chunks, st);
-    case 16: return launch_rows<16, VEC, false, T>(q, small, chunks, st);
-    case 32: return launch_rows<32, VEC, false, T>(q, small, chunks, st);
-    default: return launch_rows<64, VEC, false, T>(q, small, chunks, st);
+    case 4: return launch_rows<4, VEC, false, false, T>(q, small, chunks, st);
+    case 8: return launch_rows<8, VEC, false, false, T>(q, small, chunks, st);
+    case 16: return launch_rows<16, VEC, false, false, T>(q, small, chunks, st);
+    case 32: return launch_rows<32, VEC, false, false, T>(q, small, chunks, st);
+    default: return launch_rows<64, VEC, false, false, T>(q, small, chunks, st);
   }
 }
 template <typename T>
 void launch_typed(const BalanceParams& q, bool vec, bool small, int chunks, hipStream_t st) {
-  if (q.E <= kFewExperts) launch_few<T>(q, small, chunks, st);
+  if (q.E <= kFewExperts && q.k >= q.E) launch_few<true, T>(q, small, chunks, st);
+  else if (q.E <= kFewExperts) launch_few<false, T>(q, small, chunks, st);
   else if (vec) launch_many<true, T>(q, small, chunks, st);
   else launch_many<false, T>(q, small, chunks, st);
 }

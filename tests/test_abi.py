@@ -315,3 +315,23 @@ def test_stack_create_rejects_bad_shapes_and_pointers():
     with pytest.raises(mira.MiraError) as e:
         mira.mira_stack_create(cfg, shape, 0x100080, 0x2000, compute=1)
     assert e.value.code == -3  # the slot pool must be 256-byte aligned
+
+
+def test_current_stream_without_torchs_private_functions(monkeypatch):
+    """The current stream's handle comes from a private function of torch where there is
+    one, and from the public Stream object where there is not."""
+    torch = pytest.importorskip("torch")
+    from paper_2609_38090_amd import _binding
+
+    class Stream:
+        cuda_stream = 0x1230
+
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0x4560 + device, raising=False)
+    assert _binding._stream(None) == 0x4561
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        with monkeypatch.context() as m:
+            m.delattr(torch._C, name)
+            assert _binding._stream(None) == 0x1230

@@ -430,3 +430,35 @@ def test_parts_write_only_their_workspace():
         assert (out[c.M:] == -77).all() and (out[:, c.N:] == -77).all()
         if not off:
             c.check()
+
+
+@pytest.mark.parametrize("N,K,sizes", [(96, 160, [3, 0, 1, 12]), (300, 200, [70, 1, 0, 200]), (260, 9000, [5, 0, 9])])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_input_gradient_of_groups_through_the_transposed_copies(N, K, sizes, out):
+    """dX = dY W_g of each group's rows: the grouped product on the experts' transposed
+    copies, against the 64-bit product of the values that the plain copies hold."""
+    G, M = len(sizes), sum(sizes)
+    gen = torch.Generator().manual_seed(N)
+    pad = lambda n: -(-n // 16) * 16  # noqa: E731
+    blk = lambda n: -(-n // 128)  # noqa: E731
+    u8 = lambda *s: torch.empty(*s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    wq, wt, s, st = u8(G, N, pad(K)), u8(G, K, pad(N)), torch.empty(G, blk(N), blk(K), device="cuda"), torch.empty(G, blk(K), blk(N), device="cuda")
+    for g in range(G):
+        mira.mira_fp8_quantize(mira.Fp8QuantArgs(x=torch.randn(N, K, generator=gen).cuda(), x_dtype=mira.MIRA_F32, rows=N, cols=K, block_rows=128,
+                                                 q=wq[g], scale=s[g], qt=wt[g], scale_t=st[g]))
+    dq, ds = u8(M, pad(N)), torch.empty(M, blk(N), device="cuda")
+    mira.mira_fp8_quantize(mira.Fp8QuantArgs(x=torch.randn(M, N, generator=gen).bfloat16().cuda(), rows=M, cols=N, q=dq, scale=ds))
+    off = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int32)
+    tdt, dt = (torch.float32, mira.MIRA_F32) if out == "f32" else (torch.bfloat16, mira.MIRA_BF16)
+    off_dev, dx = off.cuda(), torch.empty(M, K, dtype=tdt, device="cuda")
+    a = mira.Fp8GemmArgs(m=M, n=K, k=N, n_groups=G, out_dtype=dt, x_rows=M, x=dq, x_scale=ds, w=wt, w_scale=st, offsets=off_dev, out=dx)
+    nb = mira.mira_fp8_gemm_workspace_bytes(a)
+    ws = u8(nb)
+    a.workspace, a.workspace_bytes = ws, nb
+    mira.mira_fp8_gemm(a)
+    torch.cuda.synchronize()
+    dy = dequantize(dq, ds, 1, M, N).cpu()
+    for g in range(G):
+        w, at = dequantize(wq[g], s[g], 128, N, K).cpu(), slice(int(off[g]), int(off[g + 1]))
+        want, mag = dy[at] @ w, dy[at].abs() @ w.abs()
+        assert ((dx[at].double().cpu() - want).abs() <= gemm_bound(mag, N, out == "bf16", want)).all()

@@ -9,9 +9,10 @@
 // gradient written once.
 //
 // A long call is bound by memory: 131072 rows of 256 in fp32 with their gradient,
-// 273 MB, 71 us, of which the pass over the logits takes 56 us at 4.8 TB/s (a copy
+// 273 MB, 72 us, of which the pass over the logits takes 57 to 63 at 4.3 to 4.7 TB/s (a copy
 // runs at 5.1).  A short one is bound by its launches and by loads that wait for one
-// another: 16 rows of 8 5.5 us, 2048 of 64 12 us.
+// another: 16 rows of 8 5.9 us, 2048 of 64 12 us.  Where a comment compares two ways,
+// both were timed with the rest of the file as it was then; calls may be faster now.
 //
 // Rows are split into at most kMaxChunks chunks, a workgroup each; a chunk
 // walks the groups that it meets.  Over the chunks in order, (chunk, group)
@@ -19,9 +20,9 @@
 // the partial sums without gaps to search: kMaxChunks + G slots hold any
 // layout of groups.  A group's slots are added in order to its means and loss: for
 // one group by the last chunk to end, for several in a launch that follows (37
-// groups of 30011 rows: 26 us so, 32 with the chunks counting their groups' ends;
-// one group of 2048 x 64: 17 us with the launch, 12 without).  Calls of few logits
-// run one workgroup per group in a single launch.
+// groups of 30011 rows: 26 us so, 24 today, and 32 with the chunks counting their
+// groups' ends; one group of 2048 x 64: 17 us with the launch, 12 without).  Calls of
+// few logits run one workgroup per group in a single launch.
 #include "device_util.h"
 #include "mira_internal.h"
 
@@ -296,7 +297,7 @@ __device__ __forceinline__ void count_pairs(const BalanceParams& q, int lo, int 
 }
 
 // One workgroup per group: counts, rows, means and loss.  Bound by latency: a launch,
-// the counts' loads, then the rows' (16 rows of 8 experts 4.4 us of the call's 5.5).
+// the counts' loads, then the rows' (16 rows of 8 experts 3.1 us of the call's 5.9).
 template <int L, bool VEC, bool FEW, bool STEP, int THREADS, typename T>
 __global__ __launch_bounds__(THREADS) void balance_group_kernel(BalanceParams q) {
   __shared__ int hist[MIRA_MAX_EXPERTS];
@@ -455,9 +456,9 @@ __device__ __forceinline__ void finish_group(const BalanceParams& q, int g, cons
 }
 
 // The one pass over the logits: a chunk of rows each workgroup, L lanes a row.  Bound
-// by memory (131072 x 256 fp32: 56 us, 268 MB at 4.8 TB/s); 1024 threads on each CU and
+// by memory (131072 x 256 fp32: 57 to 63 us, 268 MB at 4.3 to 4.7 TB/s); 1024 threads on each CU and
 // two rows of each lane group in flight measured best (512 threads and 512 chunks 86 us
-// the call against 76; a scalar path for row lengths that are no multiple of four
+// the call against 76 then; a scalar path for row lengths that are no multiple of four
 // takes 76 where vectors at any alignment took 80).
 template <int L, bool VEC, bool FEW, bool STEP, typename T>
 __global__ __launch_bounds__(kBigThreads) void balance_rows_kernel(BalanceParams q) {
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(kBigThreads) void balance_finish_kernel(BalancePara
 }
 
 // Many pairs: each chunk counts its rows' and adds them to zeroed counts (131072 x 8
-// pairs, 4 MB: 7 us, and the launch that zeroes 1 to 4).
+// pairs, 4 MB: 7 us, and the launch that zeroes 1 to 5).
 __global__ __launch_bounds__(kBigThreads) void balance_count_kernel(BalanceParams q) {
   __shared__ int hist[MIRA_MAX_EXPERTS];
   __shared__ int kept;

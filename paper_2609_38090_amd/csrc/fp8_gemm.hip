@@ -86,18 +86,19 @@ __device__ __forceinline__ void store_out<uint16_t>(uint16_t* p, float v) {
 // by direct loads, NS stages in turn: the loads of the next ones are in flight
 // while this one is multiplied.
 //
-// 4096 x 28672 x 4096 (bf16 out, 256 x 256 tiles) takes 450 us, 2.1 PFLOP/s, where a
+// 4096 x 28672 x 4096 (bf16 out, 256 x 256 tiles) takes 452 us, 2.1 PFLOP/s, where a
 // library product with one scale runs at 2.9 (8192^3): its loads alone take 413 us,
-// its products and scales alone 387, and both share one issue of instructions; the
-// matrix cores are busy half of the cycles, at 1.9 GHz.  Each block's sums are scaled
-// by the vector unit, four multiply-adds for each 16 x 16 x 128 instruction.  With
-// fp32 out (four bf16 instructions and the widening for each fp8 one) it takes 750
-// us, 1.28 PFLOP/s.  A tile's start and end, 5 us and 2 more with groups, are not
-// hidden (one workgroup fills a CU's LDS): 12288 rows over 64 experts, 2816 x 2048,
-// 158 us for 141 GFLOP.  Measured and slower: a persistent walk with the
-// next tile's loads before the stores (482 us against 481), prefetching into L2 (512
-// to 524 against 487; 176 to 193 against 168 over the experts), deeper rings, 128 x 128
-// tiles two to a CU (594; 181 against 164 over the experts).
+// its products and scales alone 387 (of 461 in the same run), and both share one issue
+// of instructions; the matrix cores are busy half of the cycles, at 1.9 GHz.  Each
+// block's sums are scaled by the vector unit, four multiply-adds for each 16 x 16 x 128
+// instruction.  With fp32 out (four bf16 instructions and the widening for each fp8
+// one) it takes 750 to 770 us, 1.25 to 1.28 PFLOP/s.  A tile's start and end, 5 us and 2
+// more with groups, are not hidden (one workgroup fills a CU's LDS): 12288 rows over 64
+// experts, 2816 x 2048, 153 to 161 us for 141 GFLOP.  Measured and slower, each pair in
+// a run of its own: a persistent walk with the next tile's loads before the stores (482
+// us against 481), prefetching into L2 (512 to 524 against 487; 176 to 193 against 168
+// over the experts), deeper rings, 128 x 128 tiles two to a CU (594 against 460; 181
+// against 164 over the experts).
 
 // One direct-to-LDS load of a wave: lane l's bytes go to LDS address m0 + 16 l.  The
 // compiler does not see these loads; every wait for them is the explicit one at
@@ -753,7 +754,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_join_kernel(GemmParams p) {
 // Time of a call = rounds of tiles over the chip * (stages * time of a stage + a
 // tile's start and end), beside what its operands take to arrive.  us per
 // stage with one tile on a CU and (one) with as many as its LDS holds (all),
-// measured over 43 products of 1 to 4096 rows, N 300 to 28672, K 700 to 14336
+// measured in one run over 43 products of 1 to 4096 rows, N 300 to 28672, K 700 to 14336
 // (e.g. 4096 x 28672 x 4096, fp8 cores: 460 us in 256 x 256 tiles, 539 in 256 x
 // 128, 729 in 128 x 64; 64 x 28672 x 4096: 54, 34, 21; 2048 x 4096 x 4096: 57,
 // 39, 53; 16 x 4096 x 4096: 128 x 64 17 us, 64 x 16 10).  Tiles of 128 x 128 (594, 33,
@@ -778,6 +779,8 @@ constexpr Shape kFew = {"fp8_gemm_few", 16, 16, 5, {}, {}}, kMixed[] = {
     {"fp8_gemm_mixed", 256, 256, 1, {}, {}}, {"fp8_gemm_mixed", 256, 128, 1, {}, {}}};  // bf16, fp32 out
 
 enum : int { kFewRows = kShapeCount, kMixedTiles };
+// kTileUs: a tile's start and end.  The join's two are a line through the calls above (its
+// parts come from caches: more bytes a us than memory gives).
 constexpr float kTileUs = 2.5f, kJoinUs = 8.f, kJoinBytesPerUs = 7e6f, kBytesPerUs = 5.5e6f;
 constexpr int kMaxParts = 32;
 constexpr long kMaxTiles = 1l << 22;  // 512 threads each: below 2^32
@@ -798,7 +801,8 @@ long tiles_of(const mira_fp8_gemm_args& a, const Shape& s) {
 // 25.4 against 26.6, 8 rows 29.7 against 27.5, 16 rows 36 against 28; one or two
 // rows always (1 x 28672 x 4096 23.1 against 26.6, 1 x 128256 x 4096 88 against 97).
 // A wave's way through the contraction: 1 x 4096 x 14336 13.8 against 17.9, 16 x
-// 4096 x 4096 7.5 against 10.4, but 16 x 1024 x 14336 17.9 against 11.6.  Many small
+// 4096 x 4096 7.5 against 10.4, but 16 x 1024 x 14336 17.9 against 11.6; up to four rows
+// go in parts beyond 16384 (1 x 4096 x 28672 27.3, 25.6 by this kernel).  Many small
 // tiles, each with its start: 6 x 2816 x 2048 in 6 of 64 experts (1056 tiles) 12.0
 // against 12.3, 16 rows in 12 to 16 of them 16.0 against 13.8.
 bool few_rows(const mira_fp8_gemm_args& a) {

@@ -2,8 +2,8 @@
 //   a = max(max |x|, eps), scale = fl32(a / 448), q = e4m3(fl32(x * fl32(448 / a))).
 // Memory bound: every value is read once, kept in registers while its block's
 // maximum is found, and written as one byte (a copy on this GPU runs at 5.1 TB/s:
-// SwiGLU of 4096 x 2 x 14336 bf16, 296 MB, 57 us, 5.2 TB/s; 14336 x 4096 fp32 to both
-// copies, 353 MB, 69 us, 5.1 TB/s; 8 x 4096, 5.2 us, is a launch).  A value is multiplied by the
+// SwiGLU of 4096 x 2 x 14336 bf16, 296 MB, 56 us, 5.2 TB/s; 14336 x 4096 fp32 to both
+// copies, 353 MB, 70 us, 5.1 TB/s; 8 x 4096, 5.4 us, is a launch).  A value is multiplied by the
 // block's inverse instead of divided by its scale: one correctly rounded
 // division per block instead of one per value (about ten instructions each).
 #include "device_util.h"

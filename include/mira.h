@@ -14,8 +14,11 @@
  * heads score the experts of layer l+2 (section IV-E): a two-layer MLP and the
  * paper's MixtureHead.  Beside the step stand the operators that a program needs
  * to train or tune such a layer and to run its dense matrices in 8 bits: the
- * router's balance loss with its gradient, and e4m3 matrices with block scales:
- * their quantizer and their product, plain or grouped over experts.
+ * router's balance loss with its gradient, e4m3 matrices with block scales (their
+ * quantizer and their product, plain or grouped over experts), and what lies between
+ * the products, forward and backward: the root-mean-square norm before the layer, the
+ * selection of experts from given logits, SwiGLU's gradient, and the combine of the
+ * experts' rows.
  *
  * Conventions for every entry point:
  *  - Return 0 (MIRA_OK) on success or a negative mira_status.  A failing call
@@ -31,7 +34,9 @@
  *    mira_pack_experts runs synchronously.  Calls on distinct workspaces may
  *    run concurrently.
  *  - mira_moe_forward, mira_moe_route, mira_moe_experts, mira_balance_loss,
- *    mira_fp8_quantize and mira_fp8_gemm only launch
+ *    mira_fp8_quantize, mira_fp8_gemm, mira_rmsnorm, mira_rmsnorm_grad,
+ *    mira_route_select, mira_route_select_grad, mira_pair_positions,
+ *    mira_combine, mira_combine_grad and mira_swiglu_grad only launch
  *    kernels (no allocation, copy, memset or host synchronisation), so they
  *    can be captured into a HIP graph and replayed; a replay recomputes
  *    everything from the buffers the captured call was given.
@@ -496,6 +501,267 @@ size_t mira_fp8_gemm_workspace_bytes(const mira_fp8_gemm_args* a);
 
 /* Only launches kernels (a HIP graph may capture it). */
 int mira_fp8_gemm(const mira_fp8_gemm_args* a, hipStream_t stream);
+
+/* ---- root-mean-square norm -------------------------------------------------
+ * Before an expert layer: the residual's addition, the norm, and its result for
+ * the router (y) and as e4m3 with a scale per block of 1 x 128 for the products
+ * (q, scale), in one pass over the rows:
+ *   h = x + residual, rounded to x_dtype (sum; without residual h = x),
+ *   y = h w / sqrt(mean of h^2 + eps),
+ * fp32 arithmetic, y rounded once.  The norm is of h as it is held, so a call with
+ * residual gives the bits of an addition and a call on its result.  q and scale
+ * are those of mira_fp8_quantize (block_rows 1, eps q_eps) on y in fp32.  Rows whose
+ * sum of squares passes fp32's range are scaled first.  A NaN in a row of h gives a row of
+ * NaN; an infinity gives NaN in its place and zeros beside it. */
+typedef struct mira_rmsnorm_args {
+  const void* x;        /* [rows][cols] x_dtype */
+  const void* residual; /* optional [rows][cols] x_dtype */
+  const void* weight;   /* [cols] w_dtype */
+  int32_t x_dtype;      /* mira_dtype of x, residual and sum */
+  int32_t w_dtype;
+  int32_t y_dtype;
+  int32_t rows;         /* >= 0 */
+  int32_t cols;         /* 1..2^24 */
+  float eps;            /* 1e-30..1e30 */
+  float q_eps;          /* smallest block maximum of q: 1e-30..1e30, e.g. 1e-8 */
+  int32_t reserved;     /* must be 0 */
+  uint64_t ldx;         /* elements between rows; 0 = cols (here and below) */
+  uint64_t ld_res;
+  void* sum;            /* optional [rows][cols] x_dtype; may be x or residual itself (same ld) */
+  uint64_t ld_sum;
+  void* y;              /* optional [rows][cols] y_dtype */
+  uint64_t ldy;
+  void* q;              /* optional [rows][ldq] e4m3 bytes, 16-byte aligned */
+  uint64_t ldq;         /* bytes: a multiple of 16; 0 = cols rounded up to one */
+  float* scale;         /* with q, and only with it: [rows][ceil(cols/128)] */
+  uint64_t ld_scale;    /* 0 = dense */
+} mira_rmsnorm_args;
+
+/* At least one of sum, y and q is given.  y, q and scale overlap no input. */
+int mira_rmsnorm(const mira_rmsnorm_args* a, hipStream_t stream);
+
+/* Its gradient, for dy arriving at y and dsum at sum: with r = 1 / sqrt(mean of
+ * h^2 + eps),
+ *   dx      = dsum + r (dy w - h r^2 mean(h dy w))   (of x, and of residual),
+ *   dweight = sum over rows of dy h r,
+ * fp32 arithmetic, sums in a fixed order.  A forward call whose result was quantized
+ * takes the gradient that arrives at the product's operand as dy.  Without rows
+ * dweight is 0.  Rows whose sum of squares passes fp32's range are scaled first, as in
+ * the forward call. */
+typedef struct mira_rmsnorm_grad_args {
+  const void* dy;     /* [rows][cols] y_dtype */
+  const void* dsum;   /* optional [rows][cols] x_dtype */
+  const void* h;      /* [rows][cols] x_dtype: sum of the forward call, or its x without residual */
+  const void* weight; /* [cols] w_dtype */
+  int32_t x_dtype;    /* of h, dsum and dx */
+  int32_t w_dtype;
+  int32_t y_dtype;    /* of dy */
+  int32_t rows;       /* >= 0 */
+  int32_t cols;       /* 1..2^24 */
+  float eps;          /* as in the forward call */
+  uint64_t ld_dy;     /* elements between rows; 0 = cols (here and below) */
+  uint64_t ld_dsum;
+  uint64_t ld_h;
+  void* dx;           /* optional [rows][cols] x_dtype; may be dsum itself (same ld), overlaps no other input */
+  uint64_t ld_dx;
+  float* dweight;     /* optional [cols] */
+  void* workspace;    /* mira_rmsnorm_grad_workspace_bytes bytes, 256-byte aligned; NULL without dweight */
+  uint64_t workspace_bytes;
+} mira_rmsnorm_grad_args;
+
+/* Bytes of workspace for calls with up to max_rows rows and dweight.  Returns 0
+ * for a negative max_rows or cols outside 1..2^24. */
+size_t mira_rmsnorm_grad_workspace_bytes(int32_t max_rows, int32_t cols);
+
+/* At least one of dx and dweight is given. */
+int mira_rmsnorm_grad(const mira_rmsnorm_grad_args* a, hipStream_t stream);
+
+/* ---- selection of experts from logits --------------------------------------
+ * The forms of routing that mira_moe_route, whose scores are a softmax, does not
+ * have: sigmoid scores, a bias for balance that counts in the selection alone,
+ * groups of experts, renormalised and scaled weights, padding; from given
+ * logits.  Per row t, s = softmax over the row or, with MIRA_ROUTE_SIGMOID, the
+ * sigmoid of each logit, and c_e = s_e + bias_e (without bias the logits' order,
+ * which is that of s):
+ *   1. with n_groups > 1: a group is n_experts / n_groups consecutive experts, its
+ *      score the sum of its group_best largest c; the top_groups groups of the
+ *      largest scores stay;
+ *   2. the top_k experts of the largest c in them are selected, best first;
+ *   3. weight = scale s_e, with MIRA_ROUTE_RENORM scale s_e / (sum of the selected
+ *      s + 1e-20).
+ * Ties go to the lower index in both steps.  The selection is that of 64-bit
+ * scores (where scores in fp32 do not tell two candidates apart they are computed
+ * anew in 64 bits); weights are fp32 arithmetic.
+ * An expert whose logit is -inf is never selected; where fewer than top_k remain,
+ * the rest of the row's topk_idx is -1 with weight 0, and so is all of a row that
+ * the mask drops, whatever its logits.  A row with a NaN logit, or for softmax
+ * +inf, has NaN weights, and its selected experts are some in 0..E-1, each once,
+ * none of them with a NaN logit.
+ * The pairs of tokens and experts are ordered as mira_moe_route orders them: pair
+ * t*k+j, and T*k + s*T + t for shared expert s, grouped by expert, increasing
+ * inside a group.  Entries of -1 and shared pairs of masked rows are in no group:
+ * expert_offsets end before them, pair_order is -1 from there on.  pair_pos is the
+ * inverse: the position of each pair, or -1.
+ * Calls give the same bits whenever repeated. */
+#define MIRA_ROUTE_SIGMOID 0x1u
+#define MIRA_ROUTE_RENORM 0x2u
+
+typedef struct mira_route_select_args {
+  const void* logits;   /* [T][E] logits_dtype */
+  const float* bias;    /* optional [E], finite */
+  const uint8_t* mask;  /* optional [T]: 0 drops a row */
+  int32_t logits_dtype; /* mira_dtype */
+  int32_t n_tokens;     /* T: 0..2^28, and T * (k + S) <= 2^30 */
+  int32_t n_experts;    /* E: E + S in 1..MIRA_MAX_EXPERTS */
+  int32_t top_k;        /* k: 1..min(MIRA_MAX_TOPK, top_groups * E / n_groups) */
+  int32_t n_shared;     /* S >= 0: shared experts, which every kept row has */
+  int32_t n_groups;     /* divides E; 1 = no groups */
+  int32_t top_groups;   /* 1..n_groups */
+  int32_t group_best;   /* 1 or 2, at most E / n_groups */
+  uint32_t flags;       /* MIRA_ROUTE_* */
+  float scale;          /* finite */
+  uint64_t ld_logits;   /* elements between rows of logits, >= E; 0 = E */
+  int32_t* topk_idx;    /* [T][k] */
+  float* topk_weight;   /* optional [T][k] */
+  int32_t* expert_counts;  /* optional [E+S] */
+  int32_t* expert_offsets; /* optional [E+S+1] */
+  int32_t* pair_order;     /* optional [T*k + S*T] */
+  int32_t* pair_pos;       /* optional [T*k + S*T] */
+  void* workspace;      /* mira_route_select_workspace_bytes bytes, 256-byte aligned */
+  uint64_t workspace_bytes;
+} mira_route_select_args;
+
+/* Bytes of workspace for calls with up to max_tokens tokens.  Returns 0 for sizes that
+ * mira_route_select refuses. */
+size_t mira_route_select_workspace_bytes(int32_t max_tokens, int32_t n_experts, int32_t top_k, int32_t n_shared);
+
+int mira_route_select(const mira_route_select_args* a, hipStream_t stream);
+
+/* The gradient of the weights, with the selection held constant: for dweight
+ * arriving at topk_weight,
+ *   dlogits[t][e] = add[t][e] + sum over j of dweight[t][j] d weight[t][j] / d logits[t][e].
+ * Entries of topk_idx outside 0..E-1 count for nothing; a row without others has
+ * gradient 0 (plus add) whatever its logits.  So do experts whose logit is -inf.  In a row
+ * with other entries a NaN logit, or for softmax +inf, makes the gradients NaN that depend on
+ * it: of all experts for softmax, for sigmoid of that expert if it is selected, and with it
+ * of the row's other selected ones where weights are renormalised.  fp32 arithmetic, rounded
+ * once. */
+typedef struct mira_route_select_grad_args {
+  const void* logits;      /* [T][E] logits_dtype */
+  const int32_t* topk_idx; /* [T][k] */
+  const float* dweight;    /* [T][k]; read only where topk_idx selects an expert */
+  const void* add;         /* optional [T][E] logits_dtype: another gradient of the logits
+                              (the balance loss's), added; may be dlogits itself (same ld) */
+  int32_t logits_dtype;    /* mira_dtype of logits, add and dlogits */
+  int32_t n_tokens;        /* as in the forward call, here and below */
+  int32_t n_experts;       /* 1..MIRA_MAX_EXPERTS */
+  int32_t top_k;           /* 1..MIRA_MAX_TOPK */
+  uint32_t flags;
+  float scale;
+  uint64_t ld_logits;      /* 0 = E (here and below) */
+  uint64_t ld_add;
+  uint64_t ld_dlogits;
+  void* dlogits;           /* [T][E] logits_dtype; may be logits itself (same ld) */
+} mira_route_select_grad_args;
+
+int mira_route_select_grad(const mira_route_select_grad_args* a, hipStream_t stream);
+
+/* pair_pos, the inverse of a pair_order of m entries over n_pairs pairs (as
+ * mira_moe_route writes it): pair_pos[pair_order[i]] = i, -1 for pairs that do not occur.
+ * Entries outside 0..n_pairs-1 are left out; each pair occurs once at most. */
+int mira_pair_positions(const int32_t* pair_order, int32_t m, int32_t n_pairs, int32_t* pair_pos,
+                        hipStream_t stream);
+
+/* ---- combine of the experts' rows -------------------------------------------
+ * After the down product, whose rows are in the pairs' order:
+ *   out[t] = residual[t] + sum over j of w[t][j] y[pair_pos[t*k+j]]
+ *          + sum over s of y[pair_pos[T*k + s*T + t]],
+ * in this order (residual last), fp32, rounded once.  Positions outside
+ * 0..y_rows-1 are left out.  Without topk_weight the weights are 1: that is also the
+ * gradient of gathering a token's row for its pairs. */
+typedef struct mira_combine_args {
+  const void* y;            /* [y_rows][cols] y_dtype */
+  const float* topk_weight; /* optional [T][k] */
+  const int32_t* pair_pos;  /* [T*k + S*T] */
+  const void* residual;     /* optional [T][cols] out_dtype */
+  int32_t n_tokens;         /* T: 0..2^28, and T * (k + S) <= 2^30 */
+  int32_t top_k;            /* k: 1..MIRA_MAX_TOPK */
+  int32_t n_shared;         /* S: 0..MIRA_MAX_EXPERTS */
+  int32_t cols;             /* 1..2^24 */
+  int32_t y_rows;           /* >= 0 */
+  int32_t y_dtype;          /* mira_dtype */
+  int32_t out_dtype;        /* mira_dtype of residual and out */
+  int32_t reserved;         /* must be 0 */
+  uint64_t ldy;             /* elements between rows; 0 = cols (here and below) */
+  uint64_t ld_res;
+  void* out;                /* [T][cols] out_dtype; may be residual itself (same ld), overlaps y nowhere */
+  uint64_t ld_out;
+} mira_combine_args;
+
+int mira_combine(const mira_combine_args* a, hipStream_t stream);
+
+/* Its gradients, for dout arriving at out (which is the residual's):
+ *   dy[pair_pos[t*k+j]] = w[t][j] dout[t],  shared pairs dout[t],
+ *   dweight[t][j]       = sum over columns of dout[t] y[pair_pos[t*k+j]]
+ * (0 where the position is outside 0..y_rows-1), fp32 arithmetic.  q and scale are
+ * dy in e4m3, as mira_fp8_quantize (block_rows 1, eps q_eps) makes it of fp32 rows,
+ * for the product with the down matrices' transposed copies.  Rows of dy, q and scale
+ * that no pair has keep their bytes; a position occurs once at most. */
+typedef struct mira_combine_grad_args {
+  const void* dout;         /* [T][cols] out_dtype */
+  const void* y;            /* [y_rows][cols] y_dtype; may be NULL without dweight */
+  const float* topk_weight; /* optional [T][k]; NULL = 1 */
+  const int32_t* pair_pos;  /* [T*k + S*T] */
+  int32_t n_tokens;         /* as above, here and below */
+  int32_t top_k;
+  int32_t n_shared;
+  int32_t cols;
+  int32_t y_rows;
+  int32_t y_dtype;          /* of y and dy */
+  int32_t out_dtype;        /* of dout */
+  float q_eps;              /* 1e-30..1e30 */
+  uint64_t ld_dout;         /* elements between rows; 0 = cols (here and below) */
+  uint64_t ldy;
+  void* dy;                 /* optional [y_rows][cols] y_dtype; may be y itself (same ld) */
+  uint64_t ld_dy;
+  void* q;                  /* optional [y_rows][ldq] e4m3 bytes, 16-byte aligned */
+  uint64_t ldq;             /* bytes: a multiple of 16; 0 = cols rounded up to one */
+  float* scale;             /* with q, and only with it: [y_rows][ceil(cols/128)] */
+  uint64_t ld_scale;        /* 0 = dense */
+  float* dweight;           /* optional [T][k] */
+} mira_combine_grad_args;
+
+/* At least one of dy, q and dweight is given. */
+int mira_combine_grad(const mira_combine_grad_args* a, hipStream_t stream);
+
+/* ---- gradient of SwiGLU -------------------------------------------------------
+ * Of act = silu(gate) up, which mira_fp8_quantize computes with MIRA_FP8_SWIGLU
+ * from x = [gate | up], for dact arriving at act: with s = sigmoid(gate),
+ *   dgate = dact up s (1 + gate (1 - s)),  dup = dact gate s,
+ * side by side as dx, in fp32 and rounded once, and as q and scale (mira_fp8_quantize
+ * with block_rows 1 and eps q_eps on the fp32 values, [rows][2 cols]) for the product
+ * with the gate and up matrices' transposed copies.  dgate is NaN for infinite gates. */
+typedef struct mira_swiglu_grad_args {
+  const void* x;      /* [rows][2 cols] x_dtype */
+  const void* dact;   /* [rows][cols] d_dtype */
+  int32_t x_dtype;    /* mira_dtype of x and dx */
+  int32_t d_dtype;
+  int32_t rows;       /* >= 0; rows * ceil(2 cols/128) < 2^31 */
+  int32_t cols;       /* 1..2^23 */
+  float q_eps;        /* 1e-30..1e30 */
+  int32_t reserved;   /* must be 0 */
+  uint64_t ldx;       /* elements between rows; 0 = dense (here and below) */
+  uint64_t ld_dact;
+  void* dx;           /* optional [rows][2 cols] x_dtype; overlaps no input */
+  uint64_t ld_dx;
+  void* q;            /* optional [rows][ldq] e4m3 bytes, 16-byte aligned */
+  uint64_t ldq;       /* bytes: a multiple of 16; 0 = 2 cols rounded up to one */
+  float* scale;       /* with q, and only with it: [rows][ceil(2 cols/128)] */
+  uint64_t ld_scale;  /* 0 = dense */
+} mira_swiglu_grad_args;
+
+/* At least one of dx and q is given. */
+int mira_swiglu_grad(const mira_swiglu_grad_args* a, hipStream_t stream);
 
 /* ---- expert staging (sections IV-C, IV-E, IV-F) ------------------------- */
 /* Copy one packed expert from pinned host memory into slot `slot` of a slot

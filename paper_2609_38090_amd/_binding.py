@@ -22,6 +22,7 @@ MIRA_MAX_TOPK = 16
 MIRA_NOALLOC_SCRATCH_BYTES = 16 << 20
 MIRA_FP8_BLOCK = 128
 MIRA_FP8_SWIGLU = 0x1
+MIRA_ROUTE_SIGMOID, MIRA_ROUTE_RENORM = 0x1, 0x2
 MIRA_VRAM_LARGE, MIRA_VRAM_SMALL = 0, 1
 MIRA_HEAD_NONE, MIRA_HEAD_MLP, MIRA_HEAD_MIXTURE, MIRA_HEAD_GIVEN = 0, 1, 2, 3
 MIRA_STACK_EVENTS = ("hot_hit", "stage_hit", "demand", "predicted", "prefetch", "prefetch_cached",
@@ -93,13 +94,61 @@ class _Fp8GemmArgs(ctypes.Structure):
          ("pair_order", _VP), ("out", _VP), ("ldo", _U64), ("workspace", _VP), ("workspace_bytes", _U64)]
 
 
+class _RmsNormArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("x", "residual", "weight")] + \
+        [(n, _I32) for n in ("x_dtype", "w_dtype", "y_dtype", "rows", "cols")] + \
+        [("eps", _F32), ("q_eps", _F32), ("reserved", _I32), ("ldx", _U64), ("ld_res", _U64), ("sum", _VP), ("ld_sum", _U64),
+         ("y", _VP), ("ldy", _U64), ("q", _VP), ("ldq", _U64), ("scale", _VP), ("ld_scale", _U64)]
+
+
+class _RmsNormGradArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("dy", "dsum", "h", "weight")] + \
+        [(n, _I32) for n in ("x_dtype", "w_dtype", "y_dtype", "rows", "cols")] + \
+        [("eps", _F32), ("ld_dy", _U64), ("ld_dsum", _U64), ("ld_h", _U64), ("dx", _VP), ("ld_dx", _U64), ("dweight", _VP),
+         ("workspace", _VP), ("workspace_bytes", _U64)]
+
+
+class _RouteSelectArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("logits", "bias", "mask")] + \
+        [(n, _I32) for n in ("logits_dtype", "n_tokens", "n_experts", "top_k", "n_shared", "n_groups", "top_groups", "group_best")] + \
+        [("flags", _U32), ("scale", _F32), ("ld_logits", _U64)] + \
+        [(n, _VP) for n in ("topk_idx", "topk_weight", "expert_counts", "expert_offsets", "pair_order", "pair_pos", "workspace")] + \
+        [("workspace_bytes", _U64)]
+
+
+class _RouteSelectGradArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("logits", "topk_idx", "dweight", "add")] + \
+        [(n, _I32) for n in ("logits_dtype", "n_tokens", "n_experts", "top_k")] + \
+        [("flags", _U32), ("scale", _F32), ("ld_logits", _U64), ("ld_add", _U64), ("ld_dlogits", _U64), ("dlogits", _VP)]
+
+
+class _CombineArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("y", "topk_weight", "pair_pos", "residual")] + \
+        [(n, _I32) for n in ("n_tokens", "top_k", "n_shared", "cols", "y_rows", "y_dtype", "out_dtype", "reserved")] + \
+        [("ldy", _U64), ("ld_res", _U64), ("out", _VP), ("ld_out", _U64)]
+
+
+class _CombineGradArgs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("dout", "y", "topk_weight", "pair_pos")] + \
+        [(n, _I32) for n in ("n_tokens", "top_k", "n_shared", "cols", "y_rows", "y_dtype", "out_dtype")] + \
+        [("q_eps", _F32), ("ld_dout", _U64), ("ldy", _U64), ("dy", _VP), ("ld_dy", _U64), ("q", _VP), ("ldq", _U64),
+         ("scale", _VP), ("ld_scale", _U64), ("dweight", _VP)]
+
+
+class _SwigluGradArgs(ctypes.Structure):
+    _fields_ = [("x", _VP), ("dact", _VP)] + [(n, _I32) for n in ("x_dtype", "d_dtype", "rows", "cols")] + \
+        [("q_eps", _F32), ("reserved", _I32), ("ldx", _U64), ("ld_dact", _U64), ("dx", _VP), ("ld_dx", _U64), ("q", _VP),
+         ("ldq", _U64), ("scale", _VP), ("ld_scale", _U64)]
+
+
 def _fill(struct, args):
     """The C structure of an argument dataclass whose fields have its names."""
     d = args.__dict__
     return struct(*[_ptr(d[n]) if p else d[n] for n, p in struct._plan])
 
 
-for _s in (_BalanceArgs, _Fp8QuantArgs, _Fp8GemmArgs):
+for _s in (_BalanceArgs, _Fp8QuantArgs, _Fp8GemmArgs, _RmsNormArgs, _RmsNormGradArgs, _RouteSelectArgs, _RouteSelectGradArgs,
+           _CombineArgs, _CombineGradArgs, _SwigluGradArgs):
     _s._plan = [(n, t is _VP) for n, t in _s._fields_]
 
 
@@ -286,6 +335,190 @@ class Fp8GemmArgs:
         return _fill(_Fp8GemmArgs, self)
 
 
+@dataclass
+class RmsNormArgs:
+    """mira_rmsnorm_args.  Pointer fields take torch tensors, integer addresses or None."""
+    x: Any = None
+    residual: Any = None
+    weight: Any = None
+    x_dtype: int = MIRA_BF16
+    w_dtype: int = MIRA_BF16
+    y_dtype: int = MIRA_BF16
+    rows: int = 0
+    cols: int = 0
+    eps: float = 1e-6
+    q_eps: float = 1e-8
+    reserved: int = 0
+    ldx: int = 0
+    ld_res: int = 0
+    sum: Any = None
+    ld_sum: int = 0
+    y: Any = None
+    ldy: int = 0
+    q: Any = None
+    ldq: int = 0
+    scale: Any = None
+    ld_scale: int = 0
+
+    def _c(self) -> _RmsNormArgs:
+        return _fill(_RmsNormArgs, self)
+
+
+@dataclass
+class RmsNormGradArgs:
+    """mira_rmsnorm_grad_args.  Pointer fields take torch tensors, integer addresses or None."""
+    dy: Any = None
+    dsum: Any = None
+    h: Any = None
+    weight: Any = None
+    x_dtype: int = MIRA_BF16
+    w_dtype: int = MIRA_BF16
+    y_dtype: int = MIRA_BF16
+    rows: int = 0
+    cols: int = 0
+    eps: float = 1e-6
+    ld_dy: int = 0
+    ld_dsum: int = 0
+    ld_h: int = 0
+    dx: Any = None
+    ld_dx: int = 0
+    dweight: Any = None
+    workspace: Any = None
+    workspace_bytes: int = 0
+
+    def _c(self) -> _RmsNormGradArgs:
+        return _fill(_RmsNormGradArgs, self)
+
+
+@dataclass
+class RouteSelectArgs:
+    """mira_route_select_args.  Pointer fields take torch tensors, integer addresses or None."""
+    logits: Any = None
+    bias: Any = None
+    mask: Any = None
+    logits_dtype: int = MIRA_F32
+    n_tokens: int = 0
+    n_experts: int = 0
+    top_k: int = 0
+    n_shared: int = 0
+    n_groups: int = 1
+    top_groups: int = 1
+    group_best: int = 1
+    flags: int = 0
+    scale: float = 1.0
+    ld_logits: int = 0
+    topk_idx: Any = None
+    topk_weight: Any = None
+    expert_counts: Any = None
+    expert_offsets: Any = None
+    pair_order: Any = None
+    pair_pos: Any = None
+    workspace: Any = None
+    workspace_bytes: int = 0
+
+    def _c(self) -> _RouteSelectArgs:
+        return _fill(_RouteSelectArgs, self)
+
+
+@dataclass
+class RouteSelectGradArgs:
+    """mira_route_select_grad_args.  Pointer fields take torch tensors, integer addresses or None."""
+    logits: Any = None
+    topk_idx: Any = None
+    dweight: Any = None
+    add: Any = None
+    logits_dtype: int = MIRA_F32
+    n_tokens: int = 0
+    n_experts: int = 0
+    top_k: int = 0
+    flags: int = 0
+    scale: float = 1.0
+    ld_logits: int = 0
+    ld_add: int = 0
+    ld_dlogits: int = 0
+    dlogits: Any = None
+
+    def _c(self) -> _RouteSelectGradArgs:
+        return _fill(_RouteSelectGradArgs, self)
+
+
+@dataclass
+class CombineArgs:
+    """mira_combine_args.  Pointer fields take torch tensors, integer addresses or None."""
+    y: Any = None
+    topk_weight: Any = None
+    pair_pos: Any = None
+    residual: Any = None
+    n_tokens: int = 0
+    top_k: int = 0
+    n_shared: int = 0
+    cols: int = 0
+    y_rows: int = 0
+    y_dtype: int = MIRA_BF16
+    out_dtype: int = MIRA_BF16
+    reserved: int = 0
+    ldy: int = 0
+    ld_res: int = 0
+    out: Any = None
+    ld_out: int = 0
+
+    def _c(self) -> _CombineArgs:
+        return _fill(_CombineArgs, self)
+
+
+@dataclass
+class CombineGradArgs:
+    """mira_combine_grad_args.  Pointer fields take torch tensors, integer addresses or None."""
+    dout: Any = None
+    y: Any = None
+    topk_weight: Any = None
+    pair_pos: Any = None
+    n_tokens: int = 0
+    top_k: int = 0
+    n_shared: int = 0
+    cols: int = 0
+    y_rows: int = 0
+    y_dtype: int = MIRA_BF16
+    out_dtype: int = MIRA_BF16
+    q_eps: float = 1e-8
+    ld_dout: int = 0
+    ldy: int = 0
+    dy: Any = None
+    ld_dy: int = 0
+    q: Any = None
+    ldq: int = 0
+    scale: Any = None
+    ld_scale: int = 0
+    dweight: Any = None
+
+    def _c(self) -> _CombineGradArgs:
+        return _fill(_CombineGradArgs, self)
+
+
+@dataclass
+class SwigluGradArgs:
+    """mira_swiglu_grad_args.  Pointer fields take torch tensors, integer addresses or None."""
+    x: Any = None
+    dact: Any = None
+    x_dtype: int = MIRA_BF16
+    d_dtype: int = MIRA_BF16
+    rows: int = 0
+    cols: int = 0
+    q_eps: float = 1e-8
+    reserved: int = 0
+    ldx: int = 0
+    ld_dact: int = 0
+    dx: Any = None
+    ld_dx: int = 0
+    q: Any = None
+    ldq: int = 0
+    scale: Any = None
+    ld_scale: int = 0
+
+    def _c(self) -> _SwigluGradArgs:
+        return _fill(_SwigluGradArgs, self)
+
+
 def _ptr(v) -> Optional[int]:
     if v is None:
         return None
@@ -386,6 +619,16 @@ def load():
             "mira_fp8_quantize": (ctypes.c_int, [ctypes.POINTER(_Fp8QuantArgs), vp]),
             "mira_fp8_gemm_workspace_bytes": (sz, [ctypes.POINTER(_Fp8GemmArgs)]),
             "mira_fp8_gemm": (ctypes.c_int, [ctypes.POINTER(_Fp8GemmArgs), vp]),
+            "mira_rmsnorm": (ctypes.c_int, [ctypes.POINTER(_RmsNormArgs), vp]),
+            "mira_rmsnorm_grad_workspace_bytes": (sz, [i32, i32]),
+            "mira_rmsnorm_grad": (ctypes.c_int, [ctypes.POINTER(_RmsNormGradArgs), vp]),
+            "mira_route_select_workspace_bytes": (sz, [i32, i32, i32, i32]),
+            "mira_route_select": (ctypes.c_int, [ctypes.POINTER(_RouteSelectArgs), vp]),
+            "mira_route_select_grad": (ctypes.c_int, [ctypes.POINTER(_RouteSelectGradArgs), vp]),
+            "mira_pair_positions": (ctypes.c_int, [vp, i32, i32, vp, vp]),
+            "mira_combine": (ctypes.c_int, [ctypes.POINTER(_CombineArgs), vp]),
+            "mira_combine_grad": (ctypes.c_int, [ctypes.POINTER(_CombineGradArgs), vp]),
+            "mira_swiglu_grad": (ctypes.c_int, [ctypes.POINTER(_SwigluGradArgs), vp]),
             "mira_stage_expert": (ctypes.c_int, [vp, u64, i32, vp, u64, vp, vp]),
             "mira_set_slot": (ctypes.c_int, [vp, i32, i32, vp]),
             "mira_stack_create": (ctypes.c_int, [ctypes.POINTER(_StackConfig), ctypes.POINTER(_Shape), vp, vp, vp,
@@ -519,6 +762,52 @@ def mira_fp8_gemm_workspace_bytes(args: Fp8GemmArgs) -> int:
 
 def mira_fp8_gemm(args: Fp8GemmArgs, stream=None):
     _check(load().mira_fp8_gemm(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_rmsnorm(args: RmsNormArgs, stream=None):
+    _check(load().mira_rmsnorm(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_rmsnorm_grad_workspace_bytes(max_rows: int, cols: int) -> int:
+    n = int(load().mira_rmsnorm_grad_workspace_bytes(max_rows, cols))
+    if n == 0:
+        raise MiraError(-2, "invalid sizes for mira_rmsnorm_grad_workspace_bytes")
+    return n
+
+
+def mira_rmsnorm_grad(args: RmsNormGradArgs, stream=None):
+    _check(load().mira_rmsnorm_grad(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_route_select_workspace_bytes(max_tokens: int, n_experts: int, top_k: int, n_shared: int = 0) -> int:
+    n = int(load().mira_route_select_workspace_bytes(max_tokens, n_experts, top_k, n_shared))
+    if n == 0:
+        raise MiraError(-2, "invalid sizes for mira_route_select_workspace_bytes")
+    return n
+
+
+def mira_route_select(args: RouteSelectArgs, stream=None):
+    _check(load().mira_route_select(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_route_select_grad(args: RouteSelectGradArgs, stream=None):
+    _check(load().mira_route_select_grad(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_pair_positions(pair_order, m: int, n_pairs: int, pair_pos, stream=None):
+    _check(load().mira_pair_positions(_ptr(pair_order), m, n_pairs, _ptr(pair_pos), _stream(stream)))
+
+
+def mira_combine(args: CombineArgs, stream=None):
+    _check(load().mira_combine(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_combine_grad(args: CombineGradArgs, stream=None):
+    _check(load().mira_combine_grad(ctypes.byref(args._c()), _stream(stream)))
+
+
+def mira_swiglu_grad(args: SwigluGradArgs, stream=None):
+    _check(load().mira_swiglu_grad(ctypes.byref(args._c()), _stream(stream)))
 
 
 def mira_stage_expert(slot_pool, slot_stride: int, slot: int, pinned_src, nbytes: int,

@@ -18,7 +18,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmira.so")
 
 SOURCES = ["route.hip", "decode.hip", "prefill.hip", "pack.hip", "predict.hip", "mixture.hip", "noalloc.hip",
-           "balance.hip", "fp8_quant.hip", "fp8_gemm.hip", "mira_api.cpp", "ops_api.cpp", "stack.cpp"]
+           "balance.hip", "fp8_quant.hip", "fp8_gemm.hip", "norm.hip", "select.hip", "combine.hip", "swiglu.hip", "mira_api.cpp", "ops_api.cpp", "stack.cpp"]
 ARCH = "gfx950"
 
 COMMON = [

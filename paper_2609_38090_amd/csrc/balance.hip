@@ -60,46 +60,6 @@ struct BalanceParams {
   uint64_t inv_k;  // 2^34 / k rounded up: i / k = i * inv_k >> 34 for i < 2^30, k <= 16
 };
 
-// Reductions over groups of L = 1, 2, .. 64 consecutive lanes.  After each step all
-// lanes of the smaller group agree, so mirrors serve as exchanges.
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
-}
-struct MaxOp {
-  __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); }
-};
-struct AddOp {
-  __device__ __forceinline__ static float of(float a, float b) { return a + b; }
-};
-template <int L, typename Op>
-__device__ __forceinline__ float lanes_reduce(float v) {
-  if constexpr (L >= 2) v = Op::of(v, dpp<0xB1>(v));    // quad_perm 1,0,3,2
-  if constexpr (L >= 4) v = Op::of(v, dpp<0x4E>(v));    // quad_perm 2,3,0,1
-  if constexpr (L >= 8) v = Op::of(v, dpp<0x141>(v));   // mirror in 8
-  if constexpr (L >= 16) v = Op::of(v, dpp<0x140>(v));  // mirror in 16
-  if constexpr (L >= 32) {  // both halves of the 32 swapped: one result is the lane's own value
-    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = Op::of(__uint_as_float(w[0]), __uint_as_float(w[1]));
-  }
-  if constexpr (L >= 64) {
-    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = Op::of(__uint_as_float(w[0]), __uint_as_float(w[1]));
-  }
-  return v;
-}
-
-// exp(x) for x <= 0 with the product x log2(e) carried to two parts, so that
-// its rounding does not grow with |x| (2 ulp; exp(-inf) = 0, NaN stays).
-__device__ __forceinline__ float exp_neg(float x) {
-  x = x < -200.f ? -200.f : x;
-  const float log2e = 1.44269502162933349609375f, rest = 1.92596299112661746887e-8f;
-  const float t = x * log2e;
-  const float r = fmaf(x, rest, fmaf(x, log2e, -t));
-  const float e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e, r * 0.693147182464599609375f, e);
-}
-
 // The logits of a row that a lane holds, up to four: VEC: 4l .. 4l+3 (E a multiple
 // of 4, rows aligned to four elements), else l, l+L, l+2L, l+3L.  FEW: the largest power
 // of two of lanes that the experts fill, at most two values a lane; four would leave

@@ -6,14 +6,11 @@
 // copies, 353 MB, 70 us, 5.1 TB/s; 8 x 4096, 5.4 us, is a launch).  A value is multiplied by the
 // block's inverse instead of divided by its scale: one correctly rounded
 // division per block instead of one per value (about ten instructions each).
-#include "device_util.h"
-#include "mira_internal.h"
+#include "fp8_dev.h"
 
 namespace mira {
 
 namespace {
-
-constexpr float kE4m3Max = 448.f;
 
 struct QuantParams {
   const void* x;
@@ -25,26 +22,6 @@ struct QuantParams {
   int rows, cols;
   float eps;
 };
-
-// Four values to four e4m3 bytes (nearest even; |v| <= 448 (1 + 2^-23), which rounds to 448).
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-}
-
-__device__ __forceinline__ float max_abs(float m, float v) { return fmaxf(m, fabsf(v)); }
-
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
-}
-// Maximum over each 16 consecutive lanes, in all of them.
-__device__ __forceinline__ float max16(float v) {
-  v = fmaxf(v, dpp<0xB1>(v));
-  v = fmaxf(v, dpp<0x4E>(v));
-  v = fmaxf(v, dpp<0x141>(v));
-  return fmaxf(v, dpp<0x140>(v));
-}
 
 // silu(g) u.  exp(-g) = 2^t with the rounding of t = -g log2(e) carried in r (2
 // steps), the quotient by the reciprocal instruction (1 step); a correctly rounded
@@ -59,53 +36,6 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   // (a quarter of 1 + e: the instruction gives 0 for a reciprocal below 2^-126, where g
   // times it is still a normal number)
   return g * (__builtin_amdgcn_rcpf(fmaf(e, 0.25f, 0.25f)) * 0.25f) * u;
-}
-
-// Vectors at the alignment of their elements: global loads take any, so rows of
-// every length and start load 16 bytes at a time.
-typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef int v4i_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef int v2i_any __attribute__((ext_vector_type(2), aligned(2)));
-
-__device__ __forceinline__ void load_n(const float* p, float (&v)[4]) {
-  const v4f q = *(const v4f_any*)p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = q[i];
-}
-__device__ __forceinline__ void load_n(const uint16_t* p, float (&v)[4]) {
-  const v2i_any q = *(const v2i_any*)p;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    v[2 * i] = __uint_as_float((uint32_t)q[i] << 16);
-    v[2 * i + 1] = __uint_as_float((uint32_t)q[i] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ void load_n(const float* p, float (&v)[8]) {
-  const v4f a = *(const v4f_any*)p, b = *(const v4f_any*)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = a[i];
-    v[4 + i] = b[i];
-  }
-}
-__device__ __forceinline__ void load_n(const uint16_t* p, float (&v)[8]) {
-  const v4i q = *(const v4i_any*)p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float((uint32_t)q[i] << 16);
-    v[2 * i + 1] = __uint_as_float((uint32_t)q[i] & 0xFFFF0000u);
-  }
-}
-
-// N values of a row from column c on; those from cols on are 0.
-template <int N, typename T>
-__device__ __forceinline__ void load_cols(const T* row, int c, int cols, float (&v)[N]) {
-  if (c + N <= cols) {
-    load_n(row + c, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = c + i < cols ? load_act(row, c + i) : 0.f;
-  }
 }
 
 // 1 x 128 blocks: 16 lanes hold a block, eight values each, so that a lane's load is

@@ -271,6 +271,16 @@ hipError_t launch_fp8_quantize(const mira_fp8_quant_args& a, hipStream_t st);
 bool fp8_gemm_fits(const mira_fp8_gemm_args& a);  // one launch holds the tiles
 size_t fp8_gemm_ws_bytes(const mira_fp8_gemm_args& a);
 hipError_t launch_fp8_gemm(const mira_fp8_gemm_args& a, hipStream_t st);
+hipError_t launch_rmsnorm(const mira_rmsnorm_args& a, hipStream_t st);
+size_t rmsnorm_grad_ws_bytes(int rows, int cols);
+hipError_t launch_rmsnorm_grad(const mira_rmsnorm_grad_args& a, hipStream_t st);
+size_t route_select_ws_bytes(int T, int E, int S);
+hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st);
+hipError_t launch_route_select_grad(const mira_route_select_grad_args& a, hipStream_t st);
+hipError_t launch_pair_positions(const int32_t* order, int m, int n_pairs, int32_t* pos, hipStream_t st);
+hipError_t launch_combine(const mira_combine_args& a, hipStream_t st);
+hipError_t launch_combine_grad(const mira_combine_grad_args& a, hipStream_t st);
+hipError_t launch_swiglu_grad(const mira_swiglu_grad_args& a, hipStream_t st);
 hipError_t launch_set_slot(int32_t* table, int expert, int slot, hipStream_t st);
 // Device address of the library's scratch array on the current device
 // (noalloc.hip), looked up on the first call per device.

@@ -1,11 +1,14 @@
 // Selection of experts from logits, the order of the (token, expert) pairs, and
 // the gradient of the weights.
 //
-// Selection: a wave takes a row, V consecutive experts to a lane, so that the lowest lane
-// of equal values has the lowest expert.  Without a bias (and without sums of a group's two
-// best) the logits themselves are compared, which is exact.  Otherwise c = s + bias is
-// computed in fp32 with an error below `delta` (see margin_of); where two candidates of a
-// step lie closer than their errors allow, the row is done again with c in 64 bits.
+// Selection: 16 lanes take a row, V experts l, l + 16, .. to a lane.  A candidate is one
+// 32-bit key: 24 bits of its c = s + bias in fixed point (without bias of its logit, whose
+// order is that of s) and 255 - expert below, so that sorting and taking maxima move value and
+// index at once and equal values give the lower expert.  A lane sorts its best four; k + 1
+// times the row's largest head is taken.  What is cut off and what fp32 rounds may hide the
+// order of two candidates: where two neighbours of the result, or the groups at the border,
+// lie closer than that (see `delta`), or a lane's four do not suffice, or a logit is NaN, a
+// whole wave does the row again with c in 64 bits.
 //
 // Order: a chunk of tokens is a workgroup.  Each expert has a bit for every token of the
 // chunk, so a pair's rank in its expert's list is a count of bits: no order of atomics
@@ -17,8 +20,10 @@ namespace mira {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = 1024;  // of a chunk's workgroup; kOneThreads where one chunk is all
+constexpr int kOneThreads = 512;
 constexpr int kChunk = 256;     // most tokens of a chunk
+constexpr int kFewChunks = 64;  // of a call that adds up its chunks' counts where they are used
 constexpr int kWords = kChunk / 32;
 constexpr float kTiny = 1e-20f;
 constexpr int kMaxGrid = 1 << 21;  // workgroups of 256 threads: fewer than 2^32 in a launch
@@ -31,6 +36,8 @@ struct SelectParams {
   float* weight;        // may be null
   int32_t* counts;      // [chunks][G] workspace
   int32_t* totals;      // [G] workspace
+  int32_t* again_n;     // [chunks] workspace: rows that are to be done in 64 bits
+  uint8_t* again;       // [chunks][kChunk] workspace: their numbers
   int32_t* counts_out;  // may be null, as the next three
   int32_t* offsets_out;
   int32_t* order;
@@ -46,192 +53,476 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-__device__ __forceinline__ float wave_best(float v) { return lanes_reduce<64, MaxOp>(v); }
-__device__ __forceinline__ double wave_best(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
-  return v;
-}
-
 // 1 / (1 + exp(-x)) without overflow, 4 steps.
 __device__ __forceinline__ float sigmoid(float x) {
   const float e = exp_neg(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e);
   return x >= 0.f ? r : e * r;
 }
 
-// The selection proper: key[i] is the rank of expert V lane + i (-inf: not to be selected),
-// gkey[i] its c for the groups' scores.  Lane j < k returns the j-th expert or -1.  With
-// margins above 0, *close is set where they do not tell two candidates apart.
-template <int V, typename F>
-__device__ __forceinline__ int choose(const SelectParams& p, F (&key)[V], const F (&gkey)[V], F key_margin, F group_margin,
-                                      F* scr, bool* close) {
+// A wave's scratch: its four rows' candidates, or each lane's best two of eight groups, or
+// c of one row in 64 bits with its groups' scores.
+constexpr int kPairStride = 66;  // (lanes of eight groups read in different banks)
+union SelectScratch {
+  uint32_t part[4][MIRA_MAX_EXPERTS];
+  uint2 pair[8][kPairStride];
+  struct {
+    double c[MIRA_MAX_EXPERTS];
+    double group[MIRA_MAX_EXPERTS];
+  } wide;
+};
+
+// Lane j < k of a row's (or the wave's) lanes: the j-th expert, or -1, and its weight.
+struct Pick {
+  int e;
+  float w;
+};
+
+// The weights of a row's selection, held by 16 lanes.
+template <typename T>
+__device__ __forceinline__ Pick weigh(const SelectParams& p, const T* x, int e, float m, float inv_sum, bool nan) {
+  float s = 0.f;
+  if (e >= 0) {
+    const float v = load_act(x, e);
+    s = p.sigmoid ? sigmoid(v) : exp_neg(v - m) * inv_sum;
+  }
+  float scale = p.scale;
+  if (p.renorm) scale *= __builtin_amdgcn_rcpf(lanes_reduce<16, AddOp>(s) + kTiny);
+  return Pick{e, e < 0 ? 0.f : nan ? __builtin_nanf("") : s * scale};
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint32_t max16_u(uint32_t v) {
+  v = max(v, dpp_u<0xB1>(v));
+  v = max(v, dpp_u<0x4E>(v));
+  v = max(v, dpp_u<0x141>(v));
+  return max(v, dpp_u<0x140>(v));
+}
+// Over the wave: of 64-bit values, and the least of 32-bit ones.
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  return __longlong_as_double((long long)((uint64_t)dpp_u<CTRL>((uint32_t)(u >> 32)) << 32 | dpp_u<CTRL>((uint32_t)u)));
+}
+__device__ __forceinline__ double wave_max64(double v) {
+  v = fmax(v, dpp_d<0xB1>(v));
+  v = fmax(v, dpp_d<0x4E>(v));
+  v = fmax(v, dpp_d<0x141>(v));
+  v = fmax(v, dpp_d<0x140>(v));
+  v = fmax(v, __shfl_xor(v, 16, 64));
+  return fmax(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ int wave_min(int v) {
+  uint32_t u = max16_u(~(uint32_t)v);
+  u = max(u, (uint32_t)__shfl_xor((int)u, 16, 64));
+  u = max(u, (uint32_t)__shfl_xor((int)u, 32, 64));
+  return (int)~u;
+}
+
+// One row by the whole wave with c in 64 bits; few rows come here, so registers are
+// spared instead of time.  The result is in lanes 0..15.
+template <typename T>
+__device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, SelectScratch& scr) {
   const int lane = threadIdx.x & 63;
-  const F none = -(F)INFINITY;
-  bool near = false;
+  const T* x = (const T*)p.logits + (size_t)row * p.ld;
+  const double none = -(double)INFINITY;
+  float v[4], m = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = lane + 64 * i < p.E ? load_act(x, lane + 64 * i) : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    nan |= v[i] != v[i];
+    m = fmaxf(m, v[i]);
+  }
+  m = lanes_reduce<64, MaxOp>(m);
+  if (!p.sigmoid) nan |= m == INFINITY;
+  nan = __ballot(nan) != 0;
+  m = m == -INFINITY ? 0.f : m;
+  // (as loops: four copies of a 64-bit exp would take twice the registers)
+  auto at = [&](int i) { return i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3]; };
+  double total = 0.0;
+  if (!p.sigmoid) {
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) total += exp((double)at(i) - (double)m);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
+  }
+  const bool sums = p.groups > 1 && p.best == 2;
+  // c of an expert, or its logit where that has the same order; -inf and NaN are never selected
+  auto fill = [&](bool score) {
+#pragma unroll 1
+    for (int e = lane, i = 0; e < p.E; e += 64, ++i) {
+      double c = at(i);
+      if (score && !nan) {
+        c = p.sigmoid ? 1.0 / (1.0 + exp(-c)) : exp(c - (double)m) / total;
+        if (p.bias) c += (double)p.bias[e];
+      }
+      scr.wide.c[e] = at(i) > -INFINITY ? c : none;
+    }
+    wave_sync();
+  };
+  fill(p.bias || sums);
   if (p.groups > 1) {
     const int size = p.E / p.groups;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (V * lane + i < p.E) scr[V * lane + i] = gkey[i];
-    wave_sync();
-    F score[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int g = lane + 64 * i;
-      score[i] = none;
-      if (g >= p.groups) continue;
-      F b1 = none, b2 = none;
+#pragma unroll 1
+    for (int g = lane; g < p.groups; g += 64) {
+      double b1 = none, b2 = none;
+#pragma unroll 1
       for (int e = g * size; e < (g + 1) * size; ++e) {
-        const F c = scr[e];
+        const double c = scr.wide.c[e];
         b2 = c > b1 ? b1 : c > b2 ? c : b2;
         b1 = c > b1 ? c : b1;
       }
-      score[i] = p.best == 2 && b2 != none ? b1 + b2 : b1;
+      scr.wide.group[g] = p.best == 2 && b2 != none ? b1 + b2 : b1;
     }
     wave_sync();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < p.groups) scr[lane + 64 * i] = score[i];
-    wave_sync();
-    bool keep[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int g = lane + 64 * i;
-      keep[i] = false;
-      if (g >= p.groups) continue;
+    uint32_t keep = 0;
+#pragma unroll 1
+    for (int g = lane, i = 0; g < p.groups; g += 64, ++i) {
+      const double mine = scr.wide.group[g];
       int before = 0;
+#pragma unroll 1
       for (int h = 0; h < p.groups; ++h) {
-        const F o = scr[h];
-        before += o > score[i] || (o == score[i] && h < g);
-        near |= h != g && o != none && fabs(o - score[i]) <= group_margin;
+        const double o = scr.wide.group[h];
+        before += o > mine || (o == mine && h < g);
       }
-      keep[i] = before < p.top_groups;
+      keep |= (uint32_t)(before < p.top_groups) << i;
     }
     wave_sync();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < p.groups) scr[lane + 64 * i] = keep[i] ? (F)1 : (F)0;
+    for (int g = lane, i = 0; g < p.groups; g += 64, ++i) scr.wide.group[g] = keep >> i & 1 ? 1.0 : 0.0;
     wave_sync();
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (V * lane + i < p.E && scr[(V * lane + i) / size] == (F)0) key[i] = none;
+    if (!p.bias) fill(false);
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 64)
+      if (scr.wide.group[e / size] == 0.0) scr.wide.c[e] = none;
     wave_sync();
   }
   int mine = -1;
+#pragma unroll 1
   for (int j = 0; j < p.k; ++j) {
-    F b = key[0];
-#pragma unroll
-    for (int i = 1; i < V; ++i) b = key[i] > b ? key[i] : b;
-    const F m = wave_best(b);
-    if (m == none) break;
-    const int who = __ffsll((unsigned long long)__ballot(b == m)) - 1;
-    int at = 0;
-#pragma unroll
-    for (int i = V - 1; i >= 0; --i) at = key[i] == m ? i : at;
-    const int e = __builtin_amdgcn_readlane(V * lane + at, who);
-    if (lane == j) mine = e;
-    if (lane == who) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i == at) key[i] = none;
+    double best = none;
+    int at = 1 << 20;
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 64) {
+      const double c = scr.wide.c[e];
+      if (c > best) best = c, at = e;
     }
-    if (key_margin >= (F)0) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) near |= key[i] >= m - key_margin;
-    }
+    const double top = wave_max64(best);
+    if (top == none) break;
+    at = wave_min(best == top ? at : 1 << 20);
+    if (lane == j) mine = at;
+    if ((at & 63) == lane) scr.wide.c[at] = none;
+    wave_sync();
   }
-  *close = __ballot(near) != 0;
-  return mine;
+  const Pick r = weigh(p, x, mine, m, p.sigmoid ? 1.f : (float)(1.0 / total), nan);
+  wave_sync();
+  return r;
 }
 
-// One row by one wave.  Lane j < k returns the j-th expert (or -1) and its weight.
-template <int V, typename T>
-__device__ __forceinline__ int select_row(const SelectParams& p, int row, const float (&bias)[V], float bias_max, double* scr,
-                                          float* weight) {
-  const int lane = threadIdx.x & 63;
-  *weight = 0.f;
-  if (p.mask && !p.mask[row]) return -1;
-  const T* x = (const T*)p.logits + (size_t)row * p.ld;
-  float v[V], s[V];
-  bool nan = false;
+__device__ __forceinline__ void order2(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+__device__ __forceinline__ void sort4(uint32_t* a) {
+  order2(a[0], a[1]);
+  order2(a[2], a[3]);
+  order2(a[0], a[2]);
+  order2(a[1], a[3]);
+  order2(a[1], a[2]);
+}
+// Puts a sequence that falls and rises, or rises and falls, in descending order.
+template <int N>
+__device__ __forceinline__ void order_bitonic(uint32_t* a) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    v[i] = V * lane + i < p.E ? load_act(x, V * lane + i) : -INFINITY;
-    nan |= v[i] != v[i];
+  for (int d = N / 2; d >= 1; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((i & d) == 0) order2(a[i], a[i + d]);
+}
+// The largest N of two descending sequences of N, descending, in a.
+template <int N>
+__device__ __forceinline__ void merge_best(uint32_t* a, const uint32_t* b) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) a[i] = max(a[i], b[N - 1 - i]);
+  order_bitonic<N>(a);
+}
+// The largest D of a lane's keys, descending, in a[0..D-1].  Of V = 16 six: with four, one row
+// in 30 (8 of 256 in half of the groups) would have more of its selection in one lane.
+template <int V>
+constexpr int kDepth = V < 4 ? V : V < 16 ? 4 : 6;
+template <int V>
+__device__ __forceinline__ void best_keys(uint32_t (&a)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) sort4(a + i);
   }
-  float top = 1.f;  // the largest score
-  float m = 0.f, sum = 1.f;
-  if (p.sigmoid) {
+  if constexpr (V == 8) merge_best<4>(a, a + 4);
+  if constexpr (V == 16) {
+    // two fours, one of them turned round, to a descending eight
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = sigmoid(v[i]);
+    for (int i = 0; i < 16; i += 8) {
+      const uint32_t t4 = a[i + 4], t5 = a[i + 5];
+      a[i + 4] = a[i + 7];
+      a[i + 5] = a[i + 6];
+      a[i + 6] = t5;
+      a[i + 7] = t4;
+      order_bitonic<8>(a + i);
+    }
+    merge_best<8>(a, a + 8);  // (what only places beyond the sixth need falls away)
+  }
+}
+
+// c step + from is 1 for the least c and below 2^24 for the largest.
+__device__ __forceinline__ float fixed_step(float bias_max) { return 16777210.f / (1.f + 2.f * bias_max); }
+__device__ __forceinline__ float fixed_from(float bias_max) { return fmaf(bias_max, fixed_step(bias_max), 2.f); }
+
+__device__ __forceinline__ uint32_t order_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+// Adds 1 to `before` for each of eight groups (their scores, all different, are in the row's lanes
+// 0..7) that comes before the lane's own.
+template <int H>
+__device__ __forceinline__ void rank_step(int score, int& before) {
+  before += (int)dpp_u<0x150 + H>((uint32_t)score) > score;  // lane H of each 16
+  if constexpr (H + 1 < 8) rank_step<H + 1>(score, before);
+}
+
+// A row to each 16 lanes of the wave.  bias, as its fixed point, is in LDS, bias_max its largest magnitude.  *again
+// says in some of its lanes that a row's result does not hold.
+template <int V, typename T>
+__device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool live, const float* bias, float bias_max,
+                                            SelectScratch& scr, bool* again) {
+  const int lane = threadIdx.x & 63, l = lane & 15;
+  // (Conditions on these are worked out anew for every row: kept through the loop over rows, all of
+  // them unrolled, they would fill the scalar registers and then vector ones.)
+  int E = p.E, groups = p.groups, k = p.k;
+  asm volatile("" : "+s"(E), "+s"(groups), "+s"(k));
+  const T* x = (const T*)p.logits + (size_t)row * p.ld;
+  if (p.mask) live = live && p.mask[row] != 0;
+  const bool sums = groups > 1 && p.best == 2, scored = p.bias || sums;
+  float v[V];
+  float any = 0.f;  // -inf or NaN, if one of the row's logits is
+  const bool full = E == 16 * V;
+  // (No branch around a single load: each would be waited for before the next.)
+  if (full) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = load_act(x, l + 16 * i);
+#pragma unroll
+    for (int i = 0; i < V; ++i) any += v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = load_act(x, min(l + 16 * i, E - 1));
+#pragma unroll
+    for (int i = 0; i < V; ++i) any += v[i];  // (the last one's copies do no harm)
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = l + 16 * i < E ? v[i] : -INFINITY;
+  }
+  const bool holes = __ballot(!(any > -INFINITY)) != 0;
+  bool wide = any != any;
+  // Fixed point of what is compared.  c = s + bias from 1 for the least that it can be (bias is held as
+  // bias step + from); logits in steps of 2^-19 below the largest, down to 32 below.  Scores: with
+  // t = x log2(e) rounded, 2^t is off by |t| half steps and a few; s (1 - s), or a share of the largest,
+  // at most 2^-|t|, makes that less than 2^-22 of the largest score's whatever t.  The sum of a softmax
+  // adds 20 half steps, which all have.  c is off by the addition's half step more: less than delta.
+  constexpr float kLog2e = 1.44269502162933349609375f;
+  const float step = fixed_step(bias_max);
+  float m = 0.f, inv_sum = 1.f, top = 1.f;  // top: the largest score
+  float c[V];
+  if (p.sigmoid && scored) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      c[i] = fmaf(__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v[i] * -kLog2e)), step, bias[l + 16 * i]);
   } else {
     m = v[0];
 #pragma unroll
-    for (int i = 1; i < V; ++i) m = fmaxf(m, v[i]);
-    m = lanes_reduce<64, MaxOp>(m);
-    nan |= m == INFINITY;
+    for (int i = 1; i < V; ++i) m = __builtin_amdgcn_fmed3f(m, v[i], INFINITY);  // the larger (fmaxf would first quiet both)
+    m = lanes_reduce<16, MaxOp>(m);
+    wide |= m == INFINITY;
     m = m == -INFINITY ? 0.f : m;
-    sum = 0.f;
+    if (!p.sigmoid && (scored || !p.renorm)) {  // (renormalised weights of the largest do not need the sum)
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      s[i] = exp_neg(v[i] - m);
-      sum += s[i];
+      for (int i = 0; i < V; ++i) {
+        c[i] = __builtin_amdgcn_exp2f((v[i] - m) * kLog2e);
+        sum += c[i];
+      }
+      sum = lanes_reduce<16, AddOp>(sum);
+      inv_sum = top = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
     }
-    sum = lanes_reduce<64, AddOp>(sum);
-    top = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
+    if (scored) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] *= top;
+      for (int i = 0; i < V; ++i) c[i] = fmaf(c[i], inv_sum * step, bias[l + 16 * i]);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) c[i] = fmaxf(fmaf(v[i] - m, 0x1p19f, 16777215.f), 1.f);
+    }
   }
-  nan = __ballot(nan) != 0;
-  const bool sums = p.groups > 1 && p.best == 2;
-  float key[V], gkey[V];
+  const float delta = (p.sigmoid ? 0x1p-21f : 0x1p-19f * top) + 0x1p-23f * (top + bias_max);
+  // (four roundings and what is cut off beside the errors themselves)
+  const int c_margin = (int)fminf(2.f * delta * step, 16777216.f) + 5;
+  const int margin = scored ? c_margin : sizeof(T) == 4 ? 4 : -1;
+  uint32_t key[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const bool can = v[i] > -INFINITY;  // (neither -inf nor NaN)
-    const float c = p.bias ? s[i] + bias[i] : s[i];
-    key[i] = !can ? -INFINITY : p.bias && !nan ? c : v[i];
-    gkey[i] = !can ? -INFINITY : (p.bias || sums) && !nan ? c : v[i];
+  for (int i = 0; i < V; ++i) key[i] = (uint32_t)c[i] << 8;
+  if constexpr (sizeof(T) == 2) {
+    if (!scored) {  // (16-bit logits are whole in 24 bits)
+#pragma unroll
+      for (int i = 0; i < V; ++i) key[i] = order_key(v[i]) & 0xFFFFFF00u;
+    }
   }
-  // An s is off by less than 2^-19 of the largest (softmax: 2 steps of exp, 10 additions, the
-  // reciprocal and a product, 20 half steps in all; sigmoid: 8), c by the addition's half step
-  // more; two of them, and a sum of two against another, by 2 and 4 times that (and its half step).
-  const float delta = 0x1p-19f * top + 0x1p-22f * (top + bias_max);
-  bool close;
-  int e = choose<V, float>(p, key, gkey, p.bias && !nan ? 2.f * delta : -1.f, (p.bias || sums) && !nan ? 4.5f * delta : -1.f, (float*)scr,
-                           &close);
-  if (close) {  // the whole wave
-    double wide[V], wkey[V], wgkey[V], total = 0.0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      wide[i] = p.sigmoid ? 1.0 / (1.0 + exp(-(double)v[i])) : exp((double)v[i] - (double)m);
-      total += wide[i];
-    }
-    if (!p.sigmoid) {
+  for (int i = 0; i < V; ++i) key[i] |= (uint32_t)(255 - l - 16 * i);
+  if (holes || !full) {
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
-#pragma unroll
-      for (int i = 0; i < V; ++i) wide[i] /= total;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const bool can = v[i] > -INFINITY;
-      const double c = p.bias ? wide[i] + (double)bias[i] : wide[i];
-      wkey[i] = !can ? -(double)INFINITY : p.bias ? c : (double)v[i];
-      wgkey[i] = !can ? -(double)INFINITY : p.bias || sums ? c : (double)v[i];
-    }
-    e = choose<V, double>(p, wkey, wgkey, -1.0, -1.0, scr, &close);
+    for (int i = 0; i < V; ++i) key[i] = v[i] > -INFINITY ? key[i] : 0u;  // (neither -inf nor NaN)
   }
-  float* held = (float*)scr;
+  if (groups > 1) {
+    // The groups' scores in the units of the keys; below all others (and so before none) where a
+    // group has no expert left.
+    const int base = sums ? (int)fixed_from(bias_max) : 0, size = E / groups;
+    constexpr int kNone = -(1 << 25);
+    auto part = [&](int i) { return key[i] >> 8; };
+    auto score_of = [&](uint32_t b1, uint32_t b2) {
+      return b1 == 0 ? kNone : (int)b1 + (sums && b2 != 0 ? (int)b2 - base : 0);
+    };
+    int least = -kNone, most = kNone;  // of the groups kept and dropped
+    if (groups <= 8 && size % 16 == 0) {
+      // a group is the same few of every lane's experts: lanes g and g + 8 find group g's best
+      // two among those of eight lanes each
+      const int each = size >> 4;
+      int g = 0, left = each;
+      uint32_t b1 = 0, b2 = 0;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (V * lane + i < p.E) held[V * lane + i] = s[i];
-  wave_sync();
-  float w = e >= 0 ? held[e] : 0.f;
-  wave_sync();
-  float scale = p.scale;
-  if (p.renorm) scale /= lanes_reduce<64, AddOp>(w) + kTiny;
-  *weight = e < 0 ? 0.f : nan ? __builtin_nanf("") : w * scale;
-  return e;
+      for (int i = 0; i < V; ++i) {
+        const uint32_t o = part(i);
+        b2 = max(b2, min(b1, o));
+        b1 = max(b1, o);
+        if (--left == 0) {  // (the same for the whole wave)
+          scr.pair[g++][lane] = uint2{b1, b2};
+          b1 = b2 = 0;
+          left = each;
+        }
+      }
+      wave_sync();
+      const uint2* from8 = &scr.pair[l & 7][lane & 56];
+      b1 = b2 = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint2 o = from8[i];
+        const uint32_t lo = min(b1, o.x);
+        b1 = max(b1, o.x);
+        b2 = max(max(b2, o.y), lo);
+      }
+      {
+        const uint32_t o1 = dpp_u<0x128>(b1), o2 = dpp_u<0x128>(b2);  // (row_ror 8)
+        const uint32_t lo = min(b1, o1);
+        b1 = max(b1, o1);
+        b2 = max(max(b2, o2), lo);
+      }
+      wave_sync();
+      // (the lower group first among equals; lanes of no group last)
+      const int score = score_of(b1, b2);
+      const int ranked = (l & 7) < groups ? score * 16 + 15 - (l & 7) : (2 * kNone - l) * 16;
+      int before = 0;
+      rank_step<0>(ranked, before);
+      const bool in = before < p.top_groups;
+      if ((l & 7) < groups) {
+        if (in) least = score;
+        else most = score;
+      }
+      const uint32_t keep = (uint32_t)(__ballot(in) >> (lane & 48));
+      g = 0, left = each;
+      uint32_t all = (uint32_t)__builtin_amdgcn_sbfe(keep, 0, 1);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        key[i] &= all;
+        if (--left == 0) {
+          left = each;
+          all = (uint32_t)__builtin_amdgcn_sbfe(keep, ++g, 1);
+        }
+      }
+    } else {
+      uint32_t* mine = scr.part[lane >> 4];
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (l + 16 * i < E) mine[l + 16 * i] = part(i);
+      wave_sync();
+      // lane l takes groups l, l + 16, ..; scores go where the first experts were: group g's start at g or later
+#pragma unroll 1
+      for (int g0 = 0; g0 < groups; g0 += 16) {
+        const int g = g0 + l;
+        uint32_t b1 = 0, b2 = 0;
+        if (g < groups) {
+#pragma unroll 4
+          for (int e = g * size; e < (g + 1) * size; ++e) {
+            const uint32_t o = mine[e];
+            b2 = max(b2, min(b1, o));
+            b1 = max(b1, o);
+          }
+        }
+        wave_sync();
+        if (g < groups) mine[g] = (uint32_t)score_of(b1, b2);
+        wave_sync();
+      }
+      uint32_t keep = 0;
+#pragma unroll 1
+      for (int g = l, i = 0; g < groups; g += 16, ++i) {
+        const int own = (int)mine[g];
+        int before = 0;
+#pragma unroll 4
+        for (int h = 0; h < groups; ++h) {
+          const int o = (int)mine[h];
+          before += o > own || (o == own && h < g);
+        }
+        const bool in = before < p.top_groups;
+        keep |= (uint32_t)in << i;
+        if (in) least = min(least, own);
+        else most = max(most, own);
+      }
+      wave_sync();
+#pragma unroll 1
+      for (int g = l, i = 0; g < groups; g += 16, ++i) mine[g] = keep >> i & 1;
+      wave_sync();
+      const uint32_t inv_size = 65536u / (uint32_t)size + 1u;  // e / size for e < 256
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const uint32_t g = min((uint32_t)(l + 16 * i) * inv_size >> 16, (uint32_t)groups - 1);
+        if (mine[g] == 0) key[i] = 0u;
+      }
+      wave_sync();
+    }
+    least = (int)(~max16_u(~((uint32_t)least ^ 0x80000000u)) ^ 0x80000000u);
+    most = (int)(max16_u((uint32_t)most ^ 0x80000000u) ^ 0x80000000u);
+    // (two sums of two, and the unit that `base` is off)
+    const int group_margin = sums ? 2 * c_margin + 2 : margin;
+    wide |= most > kNone && least - most <= group_margin;
+  }
+  best_keys<V>(key);
+  constexpr int D = kDepth<V>;
+  const uint32_t last = key[D - 1];
+  uint32_t mine = 0, next = 0;
+  for (int j = 0; j <= k; ++j) {
+    const uint32_t top_key = max16_u(key[0]);
+    if (l == j) mine = top_key;
+    next = top_key;  // in the end the first that is not selected
+    const bool won = key[0] == top_key;
+#pragma unroll
+    for (int i = 0; i + 1 < D; ++i) key[i] = won ? key[i + 1] : key[i];
+    key[D - 1] = won ? 0u : key[D - 1];
+  }
+  if (V > D) wide |= key[0] == 0u && last != 0u;  // a lane may have had more
+  const uint32_t right = dpp_u<0x101>(mine);  // (row_shl 1: the next lane's, read by all lanes)
+  const uint32_t after = l == k - 1 ? next : right;
+  const int e = l < k && mine != 0u ? 255 - (int)(mine & 255u) : -1;
+  wide |= e >= 0 && after != 0u && (int)(mine >> 8) - (int)(after >> 8) <= margin;
+  *again = wide && live;
+  return weigh(p, x, live ? e : -1, m, inv_sum, false);
 }
 
 // Exclusive sum over threads 0..255 (each its own count; others 0); total in all threads.
@@ -265,10 +556,10 @@ struct PlaceLds {
 // Order and positions of a chunk's pairs, by the whole workgroup.  sel(i) is the expert
 // of pair i of the chunk, kept(t) whether its token t has shared experts; total(g) the pairs
 // of group g in the call, before(g) those in earlier chunks.
-template <typename Sel, typename Kept, typename Total, typename Before>
+template <int THREADS, typename Sel, typename Kept, typename Total, typename Before>
 __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, int chunk, Sel sel, Kept kept, Total total, Before before) {
   const int t = threadIdx.x, G = p.E + p.S, t0 = chunk * p.chunk, n = min(p.chunk, p.T - t0);
-  for (int i = t; i < G * kWords; i += kThreads) (&L.bits[0][0])[i] = 0;
+  for (int i = t; i < G * kWords; i += THREADS) (&L.bits[0][0])[i] = 0;
   int all;
   const int mine = t < G ? total(t) : 0;
   const int off = scan256(mine, L.wave_sums, &all);  // (its barrier: the bits are zero)
@@ -290,14 +581,14 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
     *tok = i - routed - s * n;
     return kept(*tok) ? p.E + s : -1;
   };
-  for (int i = t; i < pairs; i += kThreads) {
+  for (int i = t; i < pairs; i += THREADS) {
     int tok;
     const int g = pair_of(i, &tok);
     if (g >= 0) atomicOr(&L.bits[g][tok >> 5], 1u << (tok & 31));
   }
   __syncthreads();
   const size_t P = (size_t)p.T * (p.k + p.S), Tk = (size_t)p.T * p.k;
-  for (int i = t; i < pairs; i += kThreads) {
+  for (int i = t; i < pairs; i += THREADS) {
     int tok;
     const int g = pair_of(i, &tok);
     const size_t pair = i < routed ? (size_t)t0 * p.k + i : Tk + (size_t)((i - routed) / n) * p.T + t0 + tok;
@@ -310,53 +601,97 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
     if (p.pos) p.pos[pair] = at;
   }
   if (p.order)
-    for (size_t i = (size_t)all + (size_t)chunk * kThreads + t; i < P; i += (size_t)p.chunks * kThreads) p.order[i] = -1;
+    for (size_t i = (size_t)all + (size_t)chunk * THREADS + t; i < P; i += (size_t)p.chunks * THREADS) p.order[i] = -1;
 }
 
-// A chunk of tokens: a wave takes a row at a time.  One chunk places its pairs at once
-// (ONE); several leave their counts.
+// A chunk of tokens: a wave takes four rows at a time.  One chunk does again what has to be and
+// places its pairs at once (ONE); several leave the counts of the rows that hold, and a list of
+// those that do not for a launch of its own: their code takes twice the registers.
 template <int V, bool ONE, typename T>
-__global__ __launch_bounds__(kThreads) void route_select_kernel(SelectParams p) {
-  __shared__ double scr[kWaves][MIRA_MAX_EXPERTS];
+__global__ __launch_bounds__(ONE ? kOneThreads : kThreads) void route_select_kernel(SelectParams p) {
+  constexpr int THREADS = ONE ? kOneThreads : kThreads, WAVES = THREADS / 64;
+  __shared__ SelectScratch scr[WAVES];
+  __shared__ float bias[MIRA_MAX_EXPERTS];
+  __shared__ float wave_max_bias[4];
   __shared__ int hist[MIRA_MAX_EXPERTS];
-  __shared__ int kept;
+  __shared__ int kept, n_again;
+  __shared__ uint8_t rows_again[kChunk];
   __shared__ int16_t sel[ONE ? kChunk * MIRA_MAX_TOPK : 1];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l = lane & 15;
   const int t0 = blockIdx.x * p.chunk, n = min(p.chunk, p.T - t0);
-  if (t < MIRA_MAX_EXPERTS) hist[t] = 0;
-  if (t == 0) kept = 0;
-  float bias[V], bias_max = 0.f;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    bias[i] = p.bias && V * lane + i < p.E ? p.bias[V * lane + i] : 0.f;
-    bias_max = fmaxf(bias_max, fabsf(bias[i]));
+  if (t < MIRA_MAX_EXPERTS) {
+    hist[t] = 0;
+    bias[t] = p.bias && t < p.E ? p.bias[t] : 0.f;
+    const float b = lanes_reduce<64, MaxOp>(fabsf(bias[t]));
+    if (lane == 0) wave_max_bias[wave] = b;
   }
-  bias_max = lanes_reduce<64, MaxOp>(bias_max);
+  if (t == 0) kept = n_again = 0;
   __syncthreads();
-  for (int i = wave; i < n; i += kWaves) {
-    float w;
-    const int e = select_row<V, T>(p, t0 + i, bias, bias_max, scr[wave], &w);
-    if (lane < p.k) {
-      const size_t at = (size_t)(t0 + i) * p.k + lane;
-      p.idx[at] = e;
-      if (p.weight) p.weight[at] = w;
-      if (p.place) {
-        if (ONE) sel[i * p.k + lane] = (int16_t)e;
-        if (e >= 0) atomicAdd(&hist[e], 1);
-      }
+  const float bias_max = fmaxf(fmaxf(wave_max_bias[0], wave_max_bias[1]), fmaxf(wave_max_bias[2], wave_max_bias[3]));
+  if (t < MIRA_MAX_EXPERTS) bias[t] = fmaf(bias[t], fixed_step(bias_max), fixed_from(bias_max));
+  __syncthreads();
+  auto write = [&](int i, const Pick& r) {  // lane l of a row's lanes
+    if (l >= p.k) return;
+    const size_t at = (size_t)(t0 + i) * p.k + l;
+    p.idx[at] = r.e;
+    if (p.weight) p.weight[at] = r.w;
+    if (p.place) {
+      if (ONE) sel[i * p.k + l] = (int16_t)r.e;
+      if (r.e >= 0) atomicAdd(&hist[r.e], 1);
     }
-    if (p.place && lane == 0 && (!p.mask || p.mask[t0 + i])) atomicAdd(&kept, 1);
+  };
+  for (int i0 = wave * 4; i0 < n; i0 += WAVES * 4) {
+    const int i = i0 + (lane >> 4);
+    const bool live = i < n;
+    bool again;
+    const Pick r = select_rows<V, T>(p, t0 + min(i, n - 1), live, bias, bias_max, scr[wave], &again);
+    const bool row_again = (__ballot(again) >> (lane & 48) & 0xFFFFu) != 0;
+    if (!live) continue;
+    if (!row_again) write(i, r);
+    else if (l == 0) rows_again[atomicAdd(&n_again, 1)] = (uint8_t)i;
+    if (p.place && l == 0 && (!p.mask || p.mask[t0 + i])) atomicAdd(&kept, 1);
   }
-  if (!p.place) return;
   __syncthreads();
-  auto count = [&](int g) { return g < p.E ? hist[g] : kept; };
+  const int redo = n_again;
   if constexpr (ONE) {
+    for (int j = wave; j < redo; j += WAVES) {
+      const int i = rows_again[j];
+      const Pick r = select_wide<T>(p, t0 + i, scr[wave]);
+      if (lane < 16) write(i, r);
+    }
+    if (!p.place) return;
+    __syncthreads();
     __shared__ PlaceLds place;
-    place_pairs(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; }, count,
-                [](int) { return 0; });
+    place_pairs<THREADS>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; },
+                         [&](int g) { return g < p.E ? hist[g] : kept; }, [](int) { return 0; });
   } else {
-    if (t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = count(t);
+    for (int j = t; j < redo; j += THREADS) p.again[(size_t)blockIdx.x * kChunk + j] = rows_again[j];
+    if (t == 0) p.again_n[blockIdx.x] = redo;
+    if (p.place && t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = t < p.E ? hist[t] : kept;
   }
+}
+
+// The rows of a chunk that are to be done in 64 bits.
+template <typename T>
+__global__ __launch_bounds__(256) void route_again_kernel(SelectParams p) {
+  __shared__ SelectScratch scr[4];
+  __shared__ int hist[MIRA_MAX_EXPERTS];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, chunk = blockIdx.x, n = p.again_n[chunk];
+  if (n == 0) return;
+  hist[t] = 0;
+  __syncthreads();
+  for (int j = wave; j < n; j += 4) {
+    const int row = chunk * p.chunk + p.again[(size_t)chunk * kChunk + j];
+    const Pick r = select_wide<T>(p, row, scr[wave]);
+    if (lane < p.k) {
+      const size_t at = (size_t)row * p.k + lane;
+      p.idx[at] = r.e;
+      if (p.weight) p.weight[at] = r.w;
+      if (r.e >= 0) atomicAdd(&hist[r.e], 1);
+    }
+  }
+  __syncthreads();
+  if (p.place && t < p.E) p.counts[(size_t)chunk * (p.E + p.S) + t] += hist[t];
 }
 
 // For each group the chunks' counts to sums of those before, and the total.
@@ -376,12 +711,34 @@ __global__ __launch_bounds__(256) void route_scan_kernel(SelectParams p) {
   if (threadIdx.x == 0) p.totals[g] = run;
 }
 
+// Places a chunk's pairs.  FEW: the chunks' counts are added up here.
+template <bool FEW>
 __global__ __launch_bounds__(kThreads) void route_place_kernel(SelectParams p) {
   __shared__ PlaceLds place;
-  const int chunk = blockIdx.x, t0 = chunk * p.chunk;
+  __shared__ int before_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS], total_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS];
+  const int chunk = blockIdx.x, t0 = chunk * p.chunk, G = p.E + p.S;
+  if constexpr (FEW) {  // four threads to a group
+    const int g = threadIdx.x & 255, q = threadIdx.x >> 8;
+    int before = 0, total = 0;
+    if (g < G) {
+#pragma unroll 4
+      for (int c = q; c < p.chunks; c += 4) {
+        const int v = p.counts[(size_t)c * G + g];
+        total += v;
+        before += c < chunk ? v : 0;
+      }
+    }
+    before_s[q][g] = before;
+    total_s[q][g] = total;
+    __syncthreads();
+  }
   const int32_t* idx = p.idx + (size_t)t0 * p.k;
-  place_pairs(p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; },
-              [&](int g) { return p.totals[g]; }, [&](int g) { return p.counts[(size_t)chunk * (p.E + p.S) + g]; });
+  place_pairs<kThreads>(
+      p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; },
+      [&](int g) { return FEW ? total_s[0][g] + total_s[FEW][g] + total_s[FEW * 2][g] + total_s[FEW * 3][g] : p.totals[g]; },
+      [&](int g) {
+        return FEW ? before_s[0][g] + before_s[FEW][g] + before_s[FEW * 2][g] + before_s[FEW * 3][g] : p.counts[(size_t)chunk * G + g];
+      });
 }
 
 // Tokens of a chunk: 32 until the chunks fill the CUs, then more, in steps of 32.
@@ -393,17 +750,20 @@ int chunk_count(int T) { return (int)(((int64_t)T + chunk_tokens(T) - 1) / chunk
 
 template <int V, typename T>
 void launch_select(const SelectParams& p, hipStream_t st) {
-  if (p.chunks == 1)
-    launch_timed("route_select", route_select_kernel<V, true, T>, dim3(1), dim3(kThreads), 0, st, p);
-  else
-    launch_timed("route_select", route_select_kernel<V, false, T>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+  if (p.chunks == 1) {
+    launch_timed("route_select", route_select_kernel<V, true, T>, dim3(1), dim3(kOneThreads), 0, st, p);
+    return;
+  }
+  launch_timed("route_select", route_select_kernel<V, false, T>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+  launch_timed("route_again", route_again_kernel<T>, dim3(p.chunks), dim3(256), 0, st, p);
 }
 
 template <typename T>
 void launch_select_of(const SelectParams& p, hipStream_t st) {
-  if (p.E <= 64) launch_select<1, T>(p, st);
-  else if (p.E <= 128) launch_select<2, T>(p, st);
-  else launch_select<4, T>(p, st);
+  if (p.E <= 16) launch_select<1, T>(p, st);
+  else if (p.E <= 64) launch_select<4, T>(p, st);
+  else if (p.E <= 128) launch_select<8, T>(p, st);
+  else launch_select<16, T>(p, st);
 }
 
 // ---- the weights' gradient ----------------------------------------------------
@@ -517,11 +877,15 @@ uint32_t grid_of(int n) { return ((uint32_t)n + 255) / 256; }
 
 }  // namespace
 
+static size_t ws_counts(size_t chunks, size_t G) {
+  return align_up(chunks * G * 4, 256) + align_up(chunks * 4, 256) + chunks * kChunk;
+}
+
 size_t route_select_ws_bytes(int T, int E, int S) {
   const size_t G = (size_t)E + S;
   // the most chunks that any call of up to T tokens has: chunks of 32 up to 8192 tokens, 256 chunks up to 65536
   const size_t chunks = T <= 8192 ? ((size_t)T + 31) / 32 : T <= 65536 ? 256 : ((size_t)T + kChunk - 1) / kChunk;
-  return align_up((chunks < 1 ? 1 : chunks) * G * 4, 256) + align_up(G * 4, 256);
+  return ws_counts(chunks < 1 ? 1 : chunks, G) + align_up(G * 4, 256);
 }
 
 hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) {
@@ -551,12 +915,19 @@ hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) 
   p.place = p.counts_out || p.offsets_out || p.order || p.pos;
   const int G = p.E + p.S;
   p.counts = (int32_t*)a.workspace;
-  p.totals = (int32_t*)((char*)a.workspace + align_up((size_t)p.chunks * G * 4, 256));
+  char* ws = (char*)a.workspace + align_up((size_t)p.chunks * G * 4, 256);
+  p.again_n = (int32_t*)ws;
+  p.again = (uint8_t*)(ws + align_up((size_t)p.chunks * 4, 256));
+  p.totals = (int32_t*)((char*)a.workspace + ws_counts(p.chunks, G));
   if (a.logits_dtype == MIRA_F32) launch_select_of<float>(p, st);
   else launch_select_of<uint16_t>(p, st);
   if (p.place && p.chunks > 1) {
-    launch_timed("route_scan", route_scan_kernel, dim3(G), dim3(256), 0, st, p);
-    launch_timed("route_place", route_place_kernel, dim3(p.chunks), dim3(kThreads), 0, st, p);
+    if (p.chunks <= kFewChunks) {
+      launch_timed("route_place", route_place_kernel<true>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+    } else {
+      launch_timed("route_scan", route_scan_kernel, dim3(G), dim3(256), 0, st, p);
+      launch_timed("route_place", route_place_kernel<false>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+    }
   }
   return hipGetLastError();
 }

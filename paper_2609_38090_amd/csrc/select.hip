@@ -4,10 +4,10 @@
 // Selection: 16 lanes take a row, V experts l, l + 16, .. to a lane.  A candidate is one
 // 32-bit key: 24 bits of its c = s + bias in fixed point (without bias of its logit, whose
 // order is that of s) and 255 - expert below, so that sorting and taking maxima move value and
-// index at once and equal values give the lower expert.  A lane sorts its best four; k + 1
+// index at once and equal values give the lower expert.  A lane sorts its best four or five; k + 1
 // times the row's largest head is taken.  What is cut off and what fp32 rounds may hide the
 // order of two candidates: where two neighbours of the result, or the groups at the border,
-// lie closer than that (see `delta`), or a lane's four do not suffice, or a logit is NaN, a
+// lie closer than that (see `delta`), or a lane's best do not suffice, or a logit is NaN, a
 // whole wave does the row again with c in 64 bits.
 //
 // Order: a chunk of tokens is a workgroup.  Each expert has a bit for every token of the
@@ -20,8 +20,8 @@ namespace mira {
 
 namespace {
 
-constexpr int kThreads = 1024;  // of a chunk's workgroup; kOneThreads where one chunk is all
-constexpr int kOneThreads = 512;
+constexpr int kThreads = 512, kWaves = kThreads / 64;  // of a chunk's workgroup
+constexpr int kPlaceThreads = 1024;
 constexpr int kChunk = 256;     // most tokens of a chunk
 constexpr int kFewChunks = 64;  // of a call that adds up its chunks' counts where they are used
 constexpr int kWords = kChunk / 32;
@@ -36,8 +36,6 @@ struct SelectParams {
   float* weight;        // may be null
   int32_t* counts;      // [chunks][G] workspace
   int32_t* totals;      // [G] workspace
-  int32_t* again_n;     // [chunks] workspace: rows that are to be done in 64 bits
-  uint8_t* again;       // [chunks][kChunk] workspace: their numbers
   int32_t* counts_out;  // may be null, as the next three
   int32_t* offsets_out;
   int32_t* order;
@@ -121,8 +119,7 @@ __device__ __forceinline__ int wave_min(int v) {
   return (int)~u;
 }
 
-// One row by the whole wave with c in 64 bits; few rows come here, so registers are
-// spared instead of time.  The result is in lanes 0..15.
+// One row by the whole wave with c in 64 bits.  The result is in lanes 0..15.
 template <typename T>
 __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, SelectScratch& scr) {
   const int lane = threadIdx.x & 63;
@@ -141,36 +138,38 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
   if (!p.sigmoid) nan |= m == INFINITY;
   nan = __ballot(nan) != 0;
   m = m == -INFINITY ? 0.f : m;
-  // (as loops: four copies of a 64-bit exp would take twice the registers)
-  auto at = [&](int i) { return i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3]; };
-  double total = 0.0;
-  if (!p.sigmoid) {
+  const bool sums = p.groups > 1 && p.best == 2, scored = (p.bias || sums) && !nan;
+  // The candidates' c, or their logits where these have the same order, -inf and NaN being none.
+#pragma unroll
+  for (int i = 0; i < 4; ++i) scr.wide.c[lane + 64 * i] = v[i] > -INFINITY ? (double)v[i] : none;
+  double total = 1.0;
+  if (scored || !p.sigmoid) {
+    total = 0.0;
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) total += exp((double)at(i) - (double)m);
+    for (int e = lane; e < p.E; e += 64) {
+      const double x = scr.wide.c[e];
+      const double ex = exp(p.sigmoid ? -x : x - (double)m);
+      scr.wide.group[e] = ex;
+      total += ex;
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
   }
-  const bool sums = p.groups > 1 && p.best == 2;
-  // c of an expert, or its logit where that has the same order; -inf and NaN are never selected
-  auto fill = [&](bool score) {
+  if (scored) {
 #pragma unroll 1
-    for (int e = lane, i = 0; e < p.E; e += 64, ++i) {
-      double c = at(i);
-      if (score && !nan) {
-        c = p.sigmoid ? 1.0 / (1.0 + exp(-c)) : exp(c - (double)m) / total;
-        if (p.bias) c += (double)p.bias[e];
-      }
-      scr.wide.c[e] = at(i) > -INFINITY ? c : none;
+    for (int e = lane; e < p.E; e += 64) {
+      const double ex = scr.wide.group[e];
+      const double c = (p.sigmoid ? 1.0 : ex) / (p.sigmoid ? 1.0 + ex : total) + (p.bias ? (double)p.bias[e] : 0.0);
+      if (scr.wide.c[e] != none) scr.wide.c[e] = c;
     }
-    wave_sync();
-  };
-  fill(p.bias || sums);
+  }
+  wave_sync();
   if (p.groups > 1) {
     const int size = p.E / p.groups;
 #pragma unroll 1
     for (int g = lane; g < p.groups; g += 64) {
       double b1 = none, b2 = none;
-#pragma unroll 1
+#pragma unroll 8
       for (int e = g * size; e < (g + 1) * size; ++e) {
         const double c = scr.wide.c[e];
         b2 = c > b1 ? b1 : c > b2 ? c : b2;
@@ -194,28 +193,29 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
     wave_sync();
     for (int g = lane, i = 0; g < p.groups; g += 64, ++i) scr.wide.group[g] = keep >> i & 1 ? 1.0 : 0.0;
     wave_sync();
-    if (!p.bias) fill(false);
 #pragma unroll 1
     for (int e = lane; e < p.E; e += 64)
       if (scr.wide.group[e / size] == 0.0) scr.wide.c[e] = none;
     wave_sync();
   }
+  double c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c[i] = lane + 64 * i < p.E ? scr.wide.c[lane + 64 * i] : none;
+    if (!p.bias && c[i] != none) c[i] = (double)v[i];  // (scores may have ended at 0 or 1, where logits differ)
+  }
   int mine = -1;
 #pragma unroll 1
   for (int j = 0; j < p.k; ++j) {
-    double best = none;
-    int at = 1 << 20;
-#pragma unroll 1
-    for (int e = lane; e < p.E; e += 64) {
-      const double c = scr.wide.c[e];
-      if (c > best) best = c, at = e;
-    }
-    const double top = wave_max64(best);
+    const double top = wave_max64(fmax(fmax(c[0], c[1]), fmax(c[2], c[3])));
     if (top == none) break;
-    at = wave_min(best == top ? at : 1 << 20);
+    int at = 1 << 20;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) at = c[i] == top ? lane + 64 * i : at;
+    at = wave_min(at);
     if (lane == j) mine = at;
-    if ((at & 63) == lane) scr.wide.c[at] = none;
-    wave_sync();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = lane + 64 * i == at ? none : c[i];
   }
   const Pick r = weigh(p, x, mine, m, p.sigmoid ? 1.f : (float)(1.0 / total), nan);
   wave_sync();
@@ -250,10 +250,10 @@ __device__ __forceinline__ void merge_best(uint32_t* a, const uint32_t* b) {
   for (int i = 0; i < N; ++i) a[i] = max(a[i], b[N - 1 - i]);
   order_bitonic<N>(a);
 }
-// The largest D of a lane's keys, descending, in a[0..D-1].  Of V = 16 six: with four, one row
-// in 30 (8 of 256 in half of the groups) would have more of its selection in one lane.
+// The largest of a lane's V keys, as many as are looked at, descending, in front.  Of 16 five: a row in
+// 2500 has more of its 8 of 128 in one lane, with four one in 80, and such a row is done again.
 template <int V>
-constexpr int kDepth = V < 4 ? V : V < 16 ? 4 : 6;
+constexpr int kDepth = V < 4 ? V : V < 16 ? 4 : 5;
 template <int V>
 __device__ __forceinline__ void best_keys(uint32_t (&a)[V]) {
   if constexpr (V >= 4) {
@@ -272,7 +272,7 @@ __device__ __forceinline__ void best_keys(uint32_t (&a)[V]) {
       a[i + 7] = t4;
       order_bitonic<8>(a + i);
     }
-    merge_best<8>(a, a + 8);  // (what only places beyond the sixth need falls away)
+    merge_best<8>(a, a + 8);  // (what only places beyond the fifth need falls away)
   }
 }
 
@@ -293,37 +293,44 @@ __device__ __forceinline__ void rank_step(int score, int& before) {
   if constexpr (H + 1 < 8) rank_step<H + 1>(score, before);
 }
 
-// A row to each 16 lanes of the wave.  bias, as its fixed point, is in LDS, bias_max its largest magnitude.  *again
-// says in some of its lanes that a row's result does not hold.
+// A row to each 16 lanes of the wave: its logits, expert l + 16 i to lane l, copies of the last behind it.
 template <int V, typename T>
-__device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool live, const float* bias, float bias_max,
-                                            SelectScratch& scr, bool* again) {
-  const int lane = threadIdx.x & 63, l = lane & 15;
-  // (Conditions on these are worked out anew for every row: kept through the loop over rows, all of
-  // them unrolled, they would fill the scalar registers and then vector ones.)
-  int E = p.E, groups = p.groups, k = p.k;
-  asm volatile("" : "+s"(E), "+s"(groups), "+s"(k));
+__device__ __forceinline__ void load_rows(const SelectParams& p, int row, float (&v)[V]) {
+  int l = threadIdx.x & 15, E = p.E;
+  asm volatile("" : "+v"(l), "+s"(E));  // (see select_rows)
   const T* x = (const T*)p.logits + (size_t)row * p.ld;
-  if (p.mask) live = live && p.mask[row] != 0;
-  const bool sums = groups > 1 && p.best == 2, scored = p.bias || sums;
-  float v[V];
-  float any = 0.f;  // -inf or NaN, if one of the row's logits is
-  const bool full = E == 16 * V;
   // (No branch around a single load: each would be waited for before the next.)
-  if (full) {
+  if (E == 16 * V) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = load_act(x, l + 16 * i);
-#pragma unroll
-    for (int i = 0; i < V; ++i) any += v[i];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = load_act(x, min(l + 16 * i, E - 1));
+  }
+}
+
+// ... and its selection.  bias, as its fixed point, is in LDS, bias_max its largest magnitude.  *again:
+// the row's result does not hold.
+template <int V, typename T>
+__device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool live, float (&v)[V], const float* bias, float bias_max,
+                                            SelectScratch& scr, bool* again) {
+  const int lane = threadIdx.x & 63;
+  // (What follows from these is worked out anew for every row: kept through the loop over rows, all of
+  // it unrolled, it would fill the scalar registers and then vector ones.)
+  int l = lane & 15, E = p.E, groups = p.groups, k = p.k;
+  asm volatile("" : "+v"(l), "+s"(E), "+s"(groups), "+s"(k));
+  const T* x = (const T*)p.logits + (size_t)row * p.ld;
+  if (p.mask) live = live && p.mask[row] != 0;
+  const bool sums = groups > 1 && p.best == 2, scored = p.bias || sums;
+  const bool full = E == 16 * V;
+  float any = 0.f;  // -inf or NaN, if one of the row's logits is
 #pragma unroll
-    for (int i = 0; i < V; ++i) any += v[i];  // (the last one's copies do no harm)
+  for (int i = 0; i < V; ++i) any += v[i];
+  if (!full) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = l + 16 * i < E ? v[i] : -INFINITY;
   }
-  const bool holes = __ballot(!(any > -INFINITY)) != 0;
+  const bool holes = !full || __ballot(!(any > -INFINITY)) != 0;
   bool wide = any != any;
   // Fixed point of what is compared.  c = s + bias from 1 for the least that it can be (bias is held as
   // bias step + from); logits in steps of 2^-19 below the largest, down to 32 below.  Scores: with
@@ -368,19 +375,22 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
   const int c_margin = (int)fminf(2.f * delta * step, 16777216.f) + 5;
   const int margin = scored ? c_margin : sizeof(T) == 4 ? 4 : -1;
   uint32_t key[V];
+  if (scored || sizeof(T) == 4) {
+    if (holes) {  // 0, neither -inf nor NaN being candidates
 #pragma unroll
-  for (int i = 0; i < V; ++i) key[i] = (uint32_t)c[i] << 8;
-  if constexpr (sizeof(T) == 2) {
-    if (!scored) {  // (16-bit logits are whole in 24 bits)
-#pragma unroll
-      for (int i = 0; i < V; ++i) key[i] = order_key(v[i]) & 0xFFFFFF00u;
+      for (int i = 0; i < V; ++i) c[i] = v[i] > -INFINITY ? c[i] : 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = (uint32_t)c[i] << 8;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = v[i] > -INFINITY ? order_key(v[i]) & 0xFFFFFF00u : 0u;  // (16-bit logits are whole in 24 bits)
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) key[i] |= (uint32_t)(255 - l - 16 * i);
-  if (holes || !full) {
+  if (holes) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = v[i] > -INFINITY ? key[i] : 0u;  // (neither -inf nor NaN)
+    for (int i = 0; i < V; ++i) key[i] = key[i] > 255u ? key[i] : 0u;
   }
   if (groups > 1) {
     // The groups' scores in the units of the keys; below all others (and so before none) where a
@@ -521,7 +531,7 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
   const uint32_t after = l == k - 1 ? next : right;
   const int e = l < k && mine != 0u ? 255 - (int)(mine & 255u) : -1;
   wide |= e >= 0 && after != 0u && (int)(mine >> 8) - (int)(after >> 8) <= margin;
-  *again = wide && live;
+  *again = (__ballot(wide && live) >> (lane & 48) & 0xFFFFu) != 0;
   return weigh(p, x, live ? e : -1, m, inv_sum, false);
 }
 
@@ -604,13 +614,12 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
     for (size_t i = (size_t)all + (size_t)chunk * THREADS + t; i < P; i += (size_t)p.chunks * THREADS) p.order[i] = -1;
 }
 
-// A chunk of tokens: a wave takes four rows at a time.  One chunk does again what has to be and
-// places its pairs at once (ONE); several leave the counts of the rows that hold, and a list of
-// those that do not for a launch of its own: their code takes twice the registers.
+// A chunk of tokens: a wave takes four rows at a time, then the rows that are to be done again, one by
+// one (within the loop the constants of a 64-bit exp would take the registers of half the waves).
+// One chunk places its pairs at once (ONE); several leave their counts.
 template <int V, bool ONE, typename T>
-__global__ __launch_bounds__(ONE ? kOneThreads : kThreads) void route_select_kernel(SelectParams p) {
-  constexpr int THREADS = ONE ? kOneThreads : kThreads, WAVES = THREADS / 64;
-  __shared__ SelectScratch scr[WAVES];
+__global__ __launch_bounds__(kThreads) void route_select_kernel(SelectParams p) {
+  __shared__ SelectScratch scr[kWaves];
   __shared__ float bias[MIRA_MAX_EXPERTS];
   __shared__ float wave_max_bias[4];
   __shared__ int hist[MIRA_MAX_EXPERTS];
@@ -640,58 +649,36 @@ __global__ __launch_bounds__(ONE ? kOneThreads : kThreads) void route_select_ker
       if (r.e >= 0) atomicAdd(&hist[r.e], 1);
     }
   };
-  for (int i0 = wave * 4; i0 < n; i0 += WAVES * 4) {
+  for (int i0 = wave * 4; i0 < n; i0 += kWaves * 4) {
     const int i = i0 + (lane >> 4);
     const bool live = i < n;
+    float v[V];
+    load_rows<V, T>(p, t0 + min(i, n - 1), v);
     bool again;
-    const Pick r = select_rows<V, T>(p, t0 + min(i, n - 1), live, bias, bias_max, scr[wave], &again);
-    const bool row_again = (__ballot(again) >> (lane & 48) & 0xFFFFu) != 0;
-    if (!live) continue;
-    if (!row_again) write(i, r);
-    else if (l == 0) rows_again[atomicAdd(&n_again, 1)] = (uint8_t)i;
-    if (p.place && l == 0 && (!p.mask || p.mask[t0 + i])) atomicAdd(&kept, 1);
+    const Pick r = select_rows<V, T>(p, t0 + min(i, n - 1), live, v, bias, bias_max, scr[wave], &again);
+    if (live) {
+      if (!again) write(i, r);
+      else if (l == 0) rows_again[atomicAdd(&n_again, 1)] = (uint8_t)i;
+      if (p.place && l == 0 && (!p.mask || p.mask[t0 + i])) atomicAdd(&kept, 1);
+    }
   }
   __syncthreads();
   const int redo = n_again;
+  for (int j = wave; j < redo; j += kWaves) {
+    const int i = rows_again[j];
+    const Pick r = select_wide<T>(p, t0 + i, scr[wave]);
+    if (lane < 16) write(i, r);
+  }
+  if (!p.place) return;
+  __syncthreads();
+  auto count = [&](int g) { return g < p.E ? hist[g] : kept; };
   if constexpr (ONE) {
-    for (int j = wave; j < redo; j += WAVES) {
-      const int i = rows_again[j];
-      const Pick r = select_wide<T>(p, t0 + i, scr[wave]);
-      if (lane < 16) write(i, r);
-    }
-    if (!p.place) return;
-    __syncthreads();
     __shared__ PlaceLds place;
-    place_pairs<THREADS>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; },
-                         [&](int g) { return g < p.E ? hist[g] : kept; }, [](int) { return 0; });
+    place_pairs<kThreads>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; }, count,
+                          [](int) { return 0; });
   } else {
-    for (int j = t; j < redo; j += THREADS) p.again[(size_t)blockIdx.x * kChunk + j] = rows_again[j];
-    if (t == 0) p.again_n[blockIdx.x] = redo;
-    if (p.place && t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = t < p.E ? hist[t] : kept;
+    if (t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = count(t);
   }
-}
-
-// The rows of a chunk that are to be done in 64 bits.
-template <typename T>
-__global__ __launch_bounds__(256) void route_again_kernel(SelectParams p) {
-  __shared__ SelectScratch scr[4];
-  __shared__ int hist[MIRA_MAX_EXPERTS];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, chunk = blockIdx.x, n = p.again_n[chunk];
-  if (n == 0) return;
-  hist[t] = 0;
-  __syncthreads();
-  for (int j = wave; j < n; j += 4) {
-    const int row = chunk * p.chunk + p.again[(size_t)chunk * kChunk + j];
-    const Pick r = select_wide<T>(p, row, scr[wave]);
-    if (lane < p.k) {
-      const size_t at = (size_t)row * p.k + lane;
-      p.idx[at] = r.e;
-      if (p.weight) p.weight[at] = r.w;
-      if (r.e >= 0) atomicAdd(&hist[r.e], 1);
-    }
-  }
-  __syncthreads();
-  if (p.place && t < p.E) p.counts[(size_t)chunk * (p.E + p.S) + t] += hist[t];
 }
 
 // For each group the chunks' counts to sums of those before, and the total.
@@ -713,7 +700,7 @@ __global__ __launch_bounds__(256) void route_scan_kernel(SelectParams p) {
 
 // Places a chunk's pairs.  FEW: the chunks' counts are added up here.
 template <bool FEW>
-__global__ __launch_bounds__(kThreads) void route_place_kernel(SelectParams p) {
+__global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(SelectParams p) {
   __shared__ PlaceLds place;
   __shared__ int before_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS], total_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS];
   const int chunk = blockIdx.x, t0 = chunk * p.chunk, G = p.E + p.S;
@@ -733,7 +720,7 @@ __global__ __launch_bounds__(kThreads) void route_place_kernel(SelectParams p) {
     __syncthreads();
   }
   const int32_t* idx = p.idx + (size_t)t0 * p.k;
-  place_pairs<kThreads>(
+  place_pairs<kPlaceThreads>(
       p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; },
       [&](int g) { return FEW ? total_s[0][g] + total_s[FEW][g] + total_s[FEW * 2][g] + total_s[FEW * 3][g] : p.totals[g]; },
       [&](int g) {
@@ -750,12 +737,8 @@ int chunk_count(int T) { return (int)(((int64_t)T + chunk_tokens(T) - 1) / chunk
 
 template <int V, typename T>
 void launch_select(const SelectParams& p, hipStream_t st) {
-  if (p.chunks == 1) {
-    launch_timed("route_select", route_select_kernel<V, true, T>, dim3(1), dim3(kOneThreads), 0, st, p);
-    return;
-  }
-  launch_timed("route_select", route_select_kernel<V, false, T>, dim3(p.chunks), dim3(kThreads), 0, st, p);
-  launch_timed("route_again", route_again_kernel<T>, dim3(p.chunks), dim3(256), 0, st, p);
+  launch_timed("route_select", p.chunks == 1 ? route_select_kernel<V, true, T> : route_select_kernel<V, false, T>, dim3(p.chunks),
+               dim3(kThreads), 0, st, p);
 }
 
 template <typename T>
@@ -877,15 +860,11 @@ uint32_t grid_of(int n) { return ((uint32_t)n + 255) / 256; }
 
 }  // namespace
 
-static size_t ws_counts(size_t chunks, size_t G) {
-  return align_up(chunks * G * 4, 256) + align_up(chunks * 4, 256) + chunks * kChunk;
-}
-
 size_t route_select_ws_bytes(int T, int E, int S) {
   const size_t G = (size_t)E + S;
   // the most chunks that any call of up to T tokens has: chunks of 32 up to 8192 tokens, 256 chunks up to 65536
-  const size_t chunks = T <= 8192 ? ((size_t)T + 31) / 32 : T <= 65536 ? 256 : ((size_t)T + kChunk - 1) / kChunk;
-  return ws_counts(chunks < 1 ? 1 : chunks, G) + align_up(G * 4, 256);
+  const size_t chunks = T <= 8192 ? ((size_t)T + 31) / 32 : T <= 256 * kChunk ? 256 : ((size_t)T + kChunk - 1) / kChunk;
+  return align_up((chunks < 1 ? 1 : chunks) * G * 4, 256) + align_up(G * 4, 256);
 }
 
 hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) {
@@ -915,18 +894,15 @@ hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) 
   p.place = p.counts_out || p.offsets_out || p.order || p.pos;
   const int G = p.E + p.S;
   p.counts = (int32_t*)a.workspace;
-  char* ws = (char*)a.workspace + align_up((size_t)p.chunks * G * 4, 256);
-  p.again_n = (int32_t*)ws;
-  p.again = (uint8_t*)(ws + align_up((size_t)p.chunks * 4, 256));
-  p.totals = (int32_t*)((char*)a.workspace + ws_counts(p.chunks, G));
+  p.totals = (int32_t*)((char*)a.workspace + align_up((size_t)p.chunks * G * 4, 256));
   if (a.logits_dtype == MIRA_F32) launch_select_of<float>(p, st);
   else launch_select_of<uint16_t>(p, st);
   if (p.place && p.chunks > 1) {
     if (p.chunks <= kFewChunks) {
-      launch_timed("route_place", route_place_kernel<true>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+      launch_timed("route_place", route_place_kernel<true>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p);
     } else {
       launch_timed("route_scan", route_scan_kernel, dim3(G), dim3(256), 0, st, p);
-      launch_timed("route_place", route_place_kernel<false>, dim3(p.chunks), dim3(kThreads), 0, st, p);
+      launch_timed("route_place", route_place_kernel<false>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p);
     }
   }
   return hipGetLastError();

@@ -75,55 +75,88 @@ struct CombineGradParams {
   float q_eps;
 };
 
-// A workgroup takes a token, 2048 columns at a time; a wave's sums of products meet in LDS.
-template <typename Y, typename O>
-__global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradParams p) {
-  __shared__ float part[2][4][MIRA_MAX_TOPK];
-  const int end = (int)align_up((size_t)p.cols, 2048);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// 2^share waves take a token, 512 columns each at a time; their sums of products meet in LDS.  A
+// token's positions and weights are loaded at once, one to a lane, and so are four pairs' rows: with
+// each pair's loads behind the last one's, 2048 tokens of 8 x 2048 to e4m3 took 28 us, so 25 (93 MB;
+// eight pairs' rows at once the same).
+// The blocks' maxima of w dout are w times those of dout, rounding being monotonic, so a block is
+// searched once for all the token's pairs.
+template <int K, typename Y, typename O>
+__global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradParams p, int share) {
+  constexpr int NB = 4;
+  __shared__ float part[2][4][K];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = 4 >> share;  // tokens of a workgroup
+  const int first = wave & ((1 << share) - 1), span = 512 << share;
+  const int end = (int)align_up((size_t)p.cols, 512), pairs = p.k + p.S;
+  const bool dots = p.dw && p.y_rows > 0;
   int turn = 0;
-  for (int t = blockIdx.x; t < p.T; t += gridDim.x, turn ^= 1) {
-    float dot[MIRA_MAX_TOPK];
+  for (int t0 = blockIdx.x * per; t0 < p.T; t0 += gridDim.x * per, turn ^= 1) {
+    const int t = __builtin_amdgcn_readfirstlane(t0 + (wave >> share));
+    float dot[K];
 #pragma unroll
-    for (int j = 0; j < MIRA_MAX_TOPK; ++j) dot[j] = 0.f;
-    for (int c = threadIdx.x * 8; c < end; c += 2048) {
-      float d[8];
-      load_cols((const O*)p.dout + (size_t)t * p.ld_dout, c, p.cols, d);
-      auto pair = [&](int j) {
-        const Pair a = pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, j);
-        float s = 0.f;
-        if (a.pos < 0) return s;
-        if (p.dw && j < p.k) {
-          float v[8];
-          load_cols((const Y*)p.y + (size_t)a.pos * p.ldy, c, p.cols, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s = fmaf(d[i], v[i], s);
-        }
-        if (p.dy || p.q) {
+    for (int j = 0; j < K; ++j) dot[j] = 0.f;
+    if (t < p.T) {
+      Pair held{-1, 0.f};  // of pair `lane`
+      if (lane < pairs) held = pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, lane);
+      auto pair = [&](int j) {  // (j is the same for the whole wave)
+        if (j >= 64) return pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, j);
+        return Pair{__builtin_amdgcn_readlane(held.pos, j),
+                    __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held.w), j))};
+      };
+      for (int c = first * 512 + lane * 8; c < end; c += span) {  // (whole waves leave)
+        float d[8];
+        load_cols((const O*)p.dout + (size_t)t * p.ld_dout, c, p.cols, d);
+        const float block_max = p.q ? max16(max_abs8(d)) : 0.f;
+        auto rows = [&](const Pair& a) {
+          if (a.pos < 0) return;
           float o[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = a.w * d[i];
+          clear_beyond(o, c, p.cols);
           if (p.dy) store_cols((Y*)p.dy + (size_t)a.pos * p.ld_dy, c, p.cols, o);
-          if (p.q) quantize_block(o, c, p.cols, p.q_eps, p.q + (size_t)a.pos * p.ldq, p.scale + (size_t)a.pos * p.ld_s);
-        }
-        return s;
-      };
+          if (p.q) store_block(o, fmaxf(fabsf(a.w) * block_max, p.q_eps), c, p.cols, p.q + (size_t)a.pos * p.ldq, p.scale + (size_t)a.pos * p.ld_s);
+        };
 #pragma unroll
-      for (int j = 0; j < MIRA_MAX_TOPK; ++j)
-        if (j < p.k) dot[j] += pair(j);
-      for (int j = p.k; j < p.k + p.S; ++j) pair(j);
+        for (int j0 = 0; j0 < K; j0 += NB) {
+          if (j0 >= p.k) continue;
+          Raw8<Y> v[NB];
+          if (dots) {
+#pragma unroll
+            for (int u = 0; u < NB; ++u)  // (a row of any pair beyond the last, or without a position)
+              load_raw((const Y*)p.y + (size_t)max(pair(min(j0 + u, p.k - 1)).pos, 0) * p.ldy, c, p.cols, v[u]);
+          }
+          if (p.dy || p.q) {
+#pragma unroll
+            for (int u = 0; u < NB; ++u)
+              if (j0 + u < p.k) rows(pair(j0 + u));
+          }
+          if (dots) {
+#pragma unroll
+            for (int u = 0; u < NB; ++u) {
+              float s = 0.f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) s = fmaf(d[i], v[u][i], s);
+              dot[j0 + u] += j0 + u < p.k && pair(j0 + u).pos >= 0 ? s : 0.f;
+            }
+          }
+        }
+        if (p.dy || p.q)
+          for (int j = p.k; j < pairs; ++j) rows(pair(j));
+      }
     }
     if (p.dw) {
 #pragma unroll
-      for (int j = 0; j < MIRA_MAX_TOPK; ++j)
+      for (int j = 0; j < K; ++j)
         if (j < p.k) {
           const float s = lanes_reduce<64, AddOp>(dot[j]);
           if (lane == 0) part[turn][wave][j] = s;
         }
       __syncthreads();
-      if ((int)threadIdx.x < p.k)
-        p.dw[(size_t)t * p.k + threadIdx.x] = part[turn][0][threadIdx.x] + part[turn][1][threadIdx.x] + part[turn][2][threadIdx.x] +
-                                              part[turn][3][threadIdx.x];
+      if (t < p.T && first == 0 && lane < p.k) {
+        float s = 0.f;
+        for (int i = 0; i < 1 << share; ++i) s += part[turn][wave + i][lane];
+        p.dw[(size_t)t * p.k + lane] = s;
+      }
     }
   }
 }
@@ -138,7 +171,9 @@ void launch_combine_of(const CombineParams& p, hipStream_t st) {
 }
 template <typename Y, typename O>
 void launch_combine_grad_of(const CombineGradParams& p, hipStream_t st) {
-  launch_timed("combine_grad", combine_grad_kernel<Y, O>, dim3((uint32_t)p.T < kMaxGrid ? p.T : kMaxGrid), dim3(256), 0, st, p);
+  const int share = p.cols <= 512 ? 0 : p.cols <= 1024 ? 1 : 2;
+  const uint32_t blocks = ((uint32_t)p.T + (4 >> share) - 1) / (4 >> share);
+  launch_timed("combine_grad", p.k <= 8 ? combine_grad_kernel<8, Y, O> : combine_grad_kernel<MIRA_MAX_TOPK, Y, O>, dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(256), 0, st, p, share);
 }
 
 }  // namespace

@@ -161,18 +161,24 @@ __device__ __forceinline__ uint2 to_e4m3x8(const float v[8], float inv) {
                to_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
 }
 
-// Those of a row's block: 16 lanes, eight columns each from c on, write the row's bytes up
-// to the next multiple of 16 columns, zeros there, and the block's scale.
-__device__ __forceinline__ void quantize_block(float (&v)[8], int c, int cols, float eps, uint8_t* q, float* scale) {
-  if (c + 8 > cols) {  // (a factor may have made -0 or NaN of what is beyond)
+// Zeros in place of what is beyond a row's columns (a factor may have made -0 or NaN of it).
+__device__ __forceinline__ void clear_beyond(float (&v)[8], int c, int cols) {
+  if (c + 8 > cols) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? v[i] : 0.f;
   }
-  const float m = fmaxf(max16(max_abs8(v)), eps);
-  const float inv = kE4m3Max / m;
+}
+// A row's block of maximum m: 16 lanes, eight columns each from c on (zeros beyond the row), write the
+// row's bytes up to the next multiple of 16 columns and the block's scale.
+__device__ __forceinline__ void store_block(const float (&v)[8], float m, int c, int cols, uint8_t* q, float* scale) {
   if (c >= (int)align_up((size_t)cols, 16)) return;
   if ((c & 127) == 0) scale[c >> 7] = m / kE4m3Max;
-  *(uint2*)(q + c) = to_e4m3x8(v, inv);
+  *(uint2*)(q + c) = to_e4m3x8(v, kE4m3Max / m);
+}
+// ... whose maximum is to be found.
+__device__ __forceinline__ void quantize_block(float (&v)[8], int c, int cols, float eps, uint8_t* q, float* scale) {
+  clear_beyond(v, c, cols);
+  store_block(v, fmaxf(max16(max_abs8(v)), eps), c, cols, q, scale);
 }
 
 }  // namespace mira

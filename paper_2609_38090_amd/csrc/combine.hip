@@ -33,6 +33,24 @@ __device__ __forceinline__ Pair pair_of(const int32_t* pos, const float* w, int 
   return Pair{(uint32_t)p < (uint32_t)y_rows ? p : -1, w && j < k ? w[at] : 1.f};
 }
 
+// The pairs of a token, one to a lane (further ones as they are asked for); j is the same for the
+// whole wave.
+struct TokenPairs {
+  const int32_t* pos;
+  const float* w;
+  int T, k, y_rows, t;
+  Pair held{-1, 0.f};
+  __device__ __forceinline__ TokenPairs(const int32_t* pos, const float* w, int T, int k, int S, int y_rows, int t)
+      : pos(pos), w(w), T(T), k(k), y_rows(y_rows), t(t) {
+    const int lane = threadIdx.x & 63;
+    if (lane < k + S) held = pair_of(pos, w, T, k, y_rows, t, lane);
+  }
+  __device__ __forceinline__ Pair operator[](int j) const {
+    if (j >= 64) return pair_of(pos, w, T, k, y_rows, t, j);
+    return Pair{__builtin_amdgcn_readlane(held.pos, j), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held.w), j))};
+  }
+};
+
 // A wave takes 512 columns of a token; a workgroup's four waves those of one token, or of
 // two or four where rows are short (`share`: log2 of the waves that share a token).
 template <typename Y, typename O>
@@ -43,19 +61,30 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineParams p, int share
   for (int tw = blockIdx.x * (4 >> share) + (wave >> share); tw < p.T; tw += step) {
     const int t = __builtin_amdgcn_readfirstlane(tw);
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < p.k + p.S; ++j) {
-      const Pair a = pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, j);
-      if (a.pos < 0) continue;
-      float v[8];
-      load_cols((const Y*)p.y + (size_t)a.pos * p.ldy, c, p.cols, v);
+    const TokenPairs all(p.pos, p.w, p.T, p.k, p.S, p.y_rows, t);
+    Raw8<O> res;
+    if (p.residual) load_raw((const O*)p.residual + (size_t)t * p.ld_res, c, p.cols, res);
+    for (int j0 = 0; j0 < p.k + p.S; j0 += 4) {
+      Raw8<Y> v[4];
+      if (p.y_rows > 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = fmaf(a.w, v[i], acc[i]);
+        for (int u = 0; u < 4; ++u)  // (a row of any pair beyond the last, or without a position)
+          load_raw((const Y*)p.y + (size_t)max(all[min(j0 + u, p.k + p.S - 1)].pos, 0) * p.ldy, c, p.cols, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (j0 + u >= p.k + p.S) continue;
+        const Pair a = all[j0 + u];
+        if (a.pos < 0) continue;
+        settle(v[u], c, p.cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = fmaf(a.w, v[u][i], acc[i]);
+      }
     }
     if (p.residual) {
-      float v[8];
-      load_cols((const O*)p.residual + (size_t)t * p.ld_res, c, p.cols, v);
+      settle(res, c, p.cols);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      for (int i = 0; i < 8; ++i) acc[i] += res[i];
     }
     store_cols((O*)p.out + (size_t)t * p.ld_out, c, p.cols, acc);
   }
@@ -96,17 +125,17 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradParams p, 
 #pragma unroll
     for (int j = 0; j < K; ++j) dot[j] = 0.f;
     if (t < p.T) {
-      Pair held{-1, 0.f};  // of pair `lane`
-      if (lane < pairs) held = pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, lane);
-      auto pair = [&](int j) {  // (j is the same for the whole wave)
-        if (j >= 64) return pair_of(p.pos, p.w, p.T, p.k, p.y_rows, t, j);
-        return Pair{__builtin_amdgcn_readlane(held.pos, j),
-                    __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held.w), j))};
-      };
+      const TokenPairs pair(p.pos, p.w, p.T, p.k, p.S, p.y_rows, t);
       for (int c = first * 512 + lane * 8; c < end; c += span) {  // (whole waves leave)
-        float d[8];
-        load_cols((const O*)p.dout + (size_t)t * p.ld_dout, c, p.cols, d);
-        const float block_max = p.q ? max16(max_abs8(d)) : 0.f;
+        Raw8<O> d;
+        load_raw((const O*)p.dout + (size_t)t * p.ld_dout, c, p.cols, d);
+        settle(d, c, p.cols);
+        float block_max = 0.f;
+        if (p.q) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) block_max = max_abs(block_max, d[i]);
+          block_max = max16(block_max);
+        }
         auto rows = [&](const Pair& a) {
           if (a.pos < 0) return;
           float o[8];
@@ -123,25 +152,26 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradParams p, 
           if (dots) {
 #pragma unroll
             for (int u = 0; u < NB; ++u)  // (a row of any pair beyond the last, or without a position)
-              load_raw((const Y*)p.y + (size_t)max(pair(min(j0 + u, p.k - 1)).pos, 0) * p.ldy, c, p.cols, v[u]);
+              load_raw((const Y*)p.y + (size_t)max(pair[min(j0 + u, p.k - 1)].pos, 0) * p.ldy, c, p.cols, v[u]);
           }
           if (p.dy || p.q) {
 #pragma unroll
             for (int u = 0; u < NB; ++u)
-              if (j0 + u < p.k) rows(pair(j0 + u));
+              if (j0 + u < p.k) rows(pair[j0 + u]);
           }
           if (dots) {
 #pragma unroll
             for (int u = 0; u < NB; ++u) {
+              settle(v[u], c, p.cols);
               float s = 0.f;
 #pragma unroll
               for (int i = 0; i < 8; ++i) s = fmaf(d[i], v[u][i], s);
-              dot[j0 + u] += j0 + u < p.k && pair(j0 + u).pos >= 0 ? s : 0.f;
+              dot[j0 + u] += j0 + u < p.k && pair[j0 + u].pos >= 0 ? s : 0.f;
             }
           }
         }
         if (p.dy || p.q)
-          for (int j = p.k; j < pairs; ++j) rows(pair(j));
+          for (int j = p.k; j < pairs; ++j) rows(pair[j]);
       }
     }
     if (p.dw) {

@@ -89,6 +89,13 @@ struct Raw8<float> {
     if (i < 4) a[i] = v;
     else b[i - 4] = v;
   }
+  // n values move out in front, zeros in behind.
+  __device__ __forceinline__ void shift(int n) {
+    if (n & 4) a = b, b = v4f{0.f, 0.f, 0.f, 0.f};
+    if (n & 2) a = v4f{a[2], a[3], b[0], b[1]}, b = v4f{b[2], b[3], 0.f, 0.f};
+    if (n & 1) a = v4f{a[1], a[2], a[3], b[0]}, b = v4f{b[1], b[2], b[3], 0.f};
+    if (n >= 8) zero();
+  }
 };
 template <>
 struct Raw8<uint16_t> {
@@ -100,17 +107,34 @@ struct Raw8<uint16_t> {
   __device__ __forceinline__ void load(const uint16_t* p) { q = *(const v4i_any*)p; }
   __device__ __forceinline__ void zero() { q = v4i{0, 0, 0, 0}; }
   __device__ __forceinline__ void put(int i, uint16_t v) { q[i >> 1] |= (int)((uint32_t)v << (i & 1 ? 16 : 0)); }
+  __device__ __forceinline__ void shift(int n) {
+    if (n & 4) q = v4i{q[2], q[3], 0, 0};
+    if (n & 2) q = v4i{q[1], q[2], q[3], 0};
+    if (n & 1) {
+      auto half = [](int lo, int hi) { return (int)((uint32_t)lo >> 16 | (uint32_t)hi << 16); };
+      q = v4i{half(q[0], q[1]), half(q[1], q[2]), half(q[2], q[3]), half(q[3], 0)};
+    }
+    if (n >= 8) zero();
+  }
 };
+// Columns c .. c + 7 of a row.  A lane at the row's end loads the row's last eight, and settle(), called
+// once all loads are on their way, moves them to their places, zeros behind: a load behind a
+// condition of its own would be waited for before the next (a row's three loads one after another:
+// 30000 x 700 bf16 82 us for a norm's gradient, NORMTAIL so).
 template <typename T>
 __device__ __forceinline__ void load_raw(const T* row, int c, int cols, Raw8<T>& v) {
-  if (c + 8 <= cols) {
-    v.load(row + c);
+  if (cols >= 8) {  // (the same for all)
+    v.load(row + min(c, cols - 8));
   } else {
     v.zero();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (c + i < cols) v.put(i, row[c + i]);
   }
+}
+template <typename T>
+__device__ __forceinline__ void settle(Raw8<T>& v, int c, int cols) {
+  if (cols >= 8 && c + 8 > cols) v.shift(c + 8 - cols);
 }
 
 // Two values to two bf16, nearest even, NaN kept (one instruction on gfx950).

@@ -3,10 +3,10 @@
 //   dx = dsum + r (g - n mean(n g)),  g = dy w,  n = h r;   dweight = sum over rows of dy n.
 // Memory bound: a row is read once into registers, eight consecutive columns to a lane
 // (16 bytes of bf16; 16 lanes hold a block of 128 that shares a scale), its sums are taken
-// across the lanes, and every output is written from there.  A row is shared by as many
-// threads as hold it at eight values each, 64 to 1024 (sixteen above 8192 columns); rows of
-// more than 16384 are read twice.  The gradient of the weight is
-// summed in registers over the rows that a workgroup walks, then over workgroups in order.
+// across the lanes, and every output is written from there.  A row is shared by as many waves
+// as hold it at eight values a lane (sixteen above 8192 columns), a workgroup of its own from two
+// waves on; rows of more than 16384 are read twice.  The gradient of the weight is summed in
+// registers over the rows that a workgroup walks, then over workgroups in order.
 #include "fp8_dev.h"
 
 namespace mira {
@@ -21,12 +21,15 @@ constexpr uint32_t kMaxGrid = 1u << 21;  // workgroups of a launch: fewer than 2
 // 2^24 squares of fp32's largest values fits then).
 constexpr float kDown = 8.271806125530276748714e-25f;
 
-// Threads of a workgroup whose rows are shared by L: one row, or four where a wave takes
-// one (waves of one row meet at barriers, which rows of one workgroup could not do apart).
-constexpr int threads_of(int L) { return L == 64 ? 256 : L; }
+// Workgroups of one row have 128 to 1024 threads, those of four rows (a wave each) 256: waves of one
+// row meet at barriers, which rows of one workgroup could not do apart.
+int row_threads(int cols) {
+  const int n = cols <= 8192 ? cols : (cols + 1) / 2;
+  return (n + 511) / 512 * 64;
+}
 
 // Workgroups that sum the gradient of the weight: what the CUs hold at once.
-constexpr int parts_of(int L) { return L == 64 ? 1024 : 262144 / L; }
+int parts_of(int threads) { return threads == 64 ? 1024 : 262144 / threads; }
 
 struct NormParams {
   const void* x;
@@ -62,61 +65,68 @@ __device__ __forceinline__ void load8(const void* p, size_t row_at, bool f32, in
   else load_cols((const uint16_t*)p + row_at, c, cols, v);
 }
 
-// Sum over the L threads of a row, in all of them.  Waves of one row meet in LDS; `turn`
-// alternates between two sets of it, so that one barrier a sum suffices.
-template <int L>
+// Sum over the threads of a row, in all of them: a wave, or (ROW) the workgroup, whose waves meet in
+// LDS.  `turn` alternates between two sets of it, so that one barrier a sum suffices.
+template <bool ROW>
 __device__ __forceinline__ float row_sum(float v, float (*part)[16], int turn) {
   v = lanes_reduce<64, AddOp>(v);
-  if constexpr (L > 64) {
+  if constexpr (ROW) {
     if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.f;
-#pragma unroll
-    for (int i = 0; i < L / 64; ++i) v += part[turn][i];
+    for (int i = 0; i < (int)blockDim.x >> 6; ++i) v += part[turn][i];
   }
   return v;
 }
-
 // Two sums at once.
-template <int L>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float (*part)[32], int turn) {
+template <bool ROW>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*part)[16], int turn) {
   a = lanes_reduce<64, AddOp>(a);
   b = lanes_reduce<64, AddOp>(b);
-  if constexpr (L > 64) {
-    if ((threadIdx.x & 63) == 0) {
-      part[turn][threadIdx.x >> 6] = a;
-      part[turn][16 + (threadIdx.x >> 6)] = b;
-    }
+  if constexpr (ROW) {
+    if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = float2{a, b};
     __syncthreads();
     a = b = 0.f;
-#pragma unroll
-    for (int i = 0; i < L / 64; ++i) {
-      a += part[turn][i];
-      b += part[turn][16 + i];
+    for (int i = 0; i < (int)blockDim.x >> 6; ++i) {
+      a += part[turn][i].x;
+      b += part[turn][i].y;
     }
   }
 }
 
-template <int L, int NV, typename T>
-__global__ __launch_bounds__(threads_of(L)) void rmsnorm_kernel(NormParams p) {
-  constexpr int kThreads = threads_of(L);
+template <bool ROW, int NV, typename T, typename W>
+__global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_kernel(NormParams p) {
+  constexpr int kRows = ROW ? 1 : 4;
   __shared__ float part[4][16];
-  const int l = threadIdx.x % L;
+  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63;
   const float inv_cols = 1.f / (float)p.cols;
   int turn = 0;
-  for (size_t r = (size_t)blockIdx.x * (kThreads / L) + threadIdx.x / L; r < (size_t)p.rows; r += (size_t)gridDim.x * (kThreads / L)) {
+  for (size_t r = (size_t)blockIdx.x * kRows + (ROW ? 0 : threadIdx.x >> 6); r < (size_t)p.rows; r += (size_t)gridDim.x * kRows) {
     const T* x = (const T*)p.x + r * p.ldx;
     float v[NV][8], ss = 0.f;
+    Raw8<T> raw[NV], res[NV];
+    Raw8<W> w[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_cols(x, (i * L + l) * 8, p.cols, v[i]);
+    for (int i = 0; i < NV; ++i) load_raw(x, (i * L + l) * 8, p.cols, raw[i]);
     if (p.residual) {
       const T* e = (const T*)p.residual + r * p.ld_res;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float o[8];
-        load_cols(e, (i * L + l) * 8, p.cols, o);
+      for (int i = 0; i < NV; ++i) load_raw(e, (i * L + l) * 8, p.cols, res[i]);
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = held(v[i][j] + o[j], x);
+    for (int i = 0; i < NV; ++i) load_raw((const W*)p.w, (i * L + l) * 8, p.cols, w[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      settle(raw[i], (i * L + l) * 8, p.cols);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
+    }
+    if (p.residual) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        settle(res[i], (i * L + l) * 8, p.cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = held(v[i][j] + res[i][j], x);
       }
     }
     if (p.sum) {
@@ -127,7 +137,7 @@ __global__ __launch_bounds__(threads_of(L)) void rmsnorm_kernel(NormParams p) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
-    ss = row_sum<L>(ss, part, turn & 1);
+    ss = row_sum<ROW>(ss, part, turn & 1);
     float rs;
     if (ss <= 3.4028234e38f || ss != ss) {
       rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_cols, p.eps));
@@ -140,17 +150,16 @@ __global__ __launch_bounds__(threads_of(L)) void rmsnorm_kernel(NormParams p) {
           v[i][j] *= kDown;
           ss = fmaf(v[i][j], v[i][j], ss);
         }
-      ss = row_sum<L>(ss, part, 2 + (turn & 1));
+      ss = row_sum<ROW>(ss, part, 2 + (turn & 1));
       rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_cols, p.eps * kDown * kDown));
     }
     ++turn;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * L + l) * 8;
-      float w[8];
-      load8(p.w, 0, p.w_f32, c, p.cols, w);
+      settle(w[i], c, p.cols);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rs * w[j];
+      for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rs * w[i][j];
       if (p.y) {
         if (p.y_f32) store_cols((float*)p.y + r * p.ldy, c, p.cols, v[i]);
         else store_cols((uint16_t*)p.y + r * p.ldy, c, p.cols, v[i]);
@@ -193,8 +202,8 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormParams p) {
         down = fmaf(d, d, down);
       }
     }
-    ss = row_sum<1024>(ss, part, turn & 1);
-    down = row_sum<1024>(down, part, 2 + (turn & 1));
+    ss = row_sum<true>(ss, part, turn & 1);
+    down = row_sum<true>(down, part, 2 + (turn & 1));
     ++turn;
     const bool far = ss > 3.4028234e38f;
     const float rs = __builtin_amdgcn_rsqf(far ? fmaf(down, inv_cols, p.eps * kDown * kDown) : fmaf(ss, inv_cols, p.eps)), pre = far ? kDown : 1.f;
@@ -219,9 +228,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormParams p) {
 struct RowGrad {
   float pre, rs, inner;  // n = h pre rs
 };
-template <int L, int NV, typename T, typename D, typename W>
+template <bool ROW, int NV, typename T, typename D, typename W>
 __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<D> (&d)[NV], W weights, float eps, float inv_cols,
-                                             float (*part)[32], int turn) {
+                                             float2 (*part)[16], int turn) {
   RowGrad o;
   o.pre = 1.f;
   float ss, hg;
@@ -238,7 +247,7 @@ __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<
         hg = fmaf(v, d[i][j] * w[j], hg);
       }
     }
-    row_sum2<L>(ss, hg, part, set);
+    row_sum2<ROW>(ss, hg, part, set);
   };
   sums(turn & 1);
   if (ss > 3.4028234e38f) {  // (the whole row's threads)
@@ -252,11 +261,11 @@ __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<
   return o;
 }
 
-template <int L, int NV, bool DW, typename T, typename D>
-__global__ __launch_bounds__(threads_of(L)) void rmsnorm_grad_kernel(NormGradParams p) {
-  constexpr int kThreads = threads_of(L), kRows = kThreads / L;
-  __shared__ float part[4][32];
-  const int l = threadIdx.x % L;
+template <bool ROW, int NV, bool DW, typename T, typename D>
+__global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_grad_kernel(NormGradParams p) {
+  constexpr int kRows = ROW ? 1 : 4;
+  __shared__ float2 part[4][16];
+  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63;
   const float inv_cols = 1.f / (float)p.cols;
   float held_w[8], acc[NV][8];
   load8(p.w, 0, p.w_f32, l * 8, p.cols, held_w);
@@ -275,7 +284,7 @@ __global__ __launch_bounds__(threads_of(L)) void rmsnorm_grad_kernel(NormGradPar
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
   int turn = 0;
-  for (size_t r = (size_t)blockIdx.x * kRows + threadIdx.x / L; r < (size_t)p.rows; r += (size_t)gridDim.x * kRows, ++turn) {
+  for (size_t r = (size_t)blockIdx.x * kRows + (ROW ? 0 : threadIdx.x >> 6); r < (size_t)p.rows; r += (size_t)gridDim.x * kRows, ++turn) {
     Raw8<T> h[NV], s[NV];
     Raw8<D> d[NV];
 #pragma unroll
@@ -284,12 +293,21 @@ __global__ __launch_bounds__(threads_of(L)) void rmsnorm_grad_kernel(NormGradPar
       load_raw((const T*)p.h + r * p.ld_h, c, p.cols, h[i]);
       load_raw((const D*)p.dy + r * p.ld_dy, c, p.cols, d[i]);
     }
+    if (p.dsum) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load_raw((const T*)p.dsum + r * p.ld_dsum, (i * L + l) * 8, p.cols, s[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) s[i].zero();
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (p.dsum) load_raw((const T*)p.dsum + r * p.ld_dsum, (i * L + l) * 8, p.cols, s[i]);
-      else s[i].zero();
+      const int c = (i * L + l) * 8;
+      settle(h[i], c, p.cols);
+      settle(d[i], c, p.cols);
+      settle(s[i], c, p.cols);
     }
-    const RowGrad o = grad_sums<L, NV>(h, d, weights, p.eps, inv_cols, part, turn);
+    const RowGrad o = grad_sums<ROW, NV>(h, d, weights, p.eps, inv_cols, part, turn);
     const float out_scale = o.rs * o.pre;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -306,17 +324,15 @@ __global__ __launch_bounds__(threads_of(L)) void rmsnorm_grad_kernel(NormGradPar
   }
   if constexpr (DW) {
     float* out = p.partial + (size_t)blockIdx.x * p.cols;
-    if constexpr (kRows == 1) {
+    if constexpr (ROW) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_cols(out, (i * L + l) * 8, p.cols, acc[i]);
     } else {
-      __shared__ float rows_acc[kRows][NV * L * 8];
+      __shared__ float rows_acc[kRows][512];
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) rows_acc[threadIdx.x / L][(i * L + l) * 8 + j] = acc[i][j];
+      for (int j = 0; j < 8; ++j) rows_acc[threadIdx.x >> 6][l * 8 + j] = acc[0][j];
       __syncthreads();
-      for (int c = threadIdx.x; c < p.cols; c += kThreads) {
+      for (int c = threadIdx.x; c < p.cols; c += 256) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < kRows; ++i) s += rows_acc[i][c];
@@ -356,10 +372,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradParams 
       }
     }
     const int b = (turn & 1) * 4;
-    ss = row_sum<1024>(ss, part, b);
-    hg = row_sum<1024>(hg, part, b + 1);
-    ds = row_sum<1024>(ds, part, b + 2);
-    dg = row_sum<1024>(dg, part, b + 3);
+    ss = row_sum<true>(ss, part, b);
+    hg = row_sum<true>(hg, part, b + 1);
+    ds = row_sum<true>(ds, part, b + 2);
+    dg = row_sum<true>(dg, part, b + 3);
     const bool far = ss > 3.4028234e38f;
     const float rs = __builtin_amdgcn_rsqf(far ? fmaf(ds, inv_cols, p.eps * kDown * kDown) : fmaf(ss, inv_cols, p.eps)), pre = far ? kDown : 1.f;
     const float inner = rs * (far ? dg : hg) * inv_cols;
@@ -419,21 +435,16 @@ uint32_t row_grid(int rows, int rows_per_block, uint32_t most) {
   return n < most ? n : most;
 }
 
-template <int L, int NV, typename T>
-void launch_norm(const NormParams& p, hipStream_t st) {
-  constexpr int kThreads = threads_of(L);
-  launch_timed("rmsnorm", rmsnorm_kernel<L, NV, T>, dim3(row_grid(p.rows, kThreads / L, kMaxGrid)), dim3(kThreads), 0, st, p);
-}
-
-template <typename T>
+template <typename T, typename W>
 void launch_norm_of(const NormParams& p, hipStream_t st) {
-  if (p.cols <= 512) launch_norm<64, 1, T>(p, st);
-  else if (p.cols <= 1024) launch_norm<128, 1, T>(p, st);
-  else if (p.cols <= 2048) launch_norm<256, 1, T>(p, st);
-  else if (p.cols <= 4096) launch_norm<512, 1, T>(p, st);
-  else if (p.cols <= 8192) launch_norm<1024, 1, T>(p, st);
-  else if (p.cols <= kRegCols) launch_norm<1024, 2, T>(p, st);
-  else launch_timed("rmsnorm_long", rmsnorm_long_kernel<T>, dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(1024), 0, st, p);
+  const int threads = row_threads(p.cols);
+  if (p.cols > kRegCols)
+    launch_timed("rmsnorm_long", rmsnorm_long_kernel<T>, dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(1024), 0, st, p);
+  else if (threads == 64)
+    launch_timed("rmsnorm", rmsnorm_kernel<false, 1, T, W>, dim3(row_grid(p.rows, 4, kMaxGrid)), dim3(256), 0, st, p);
+  else
+    launch_timed("rmsnorm", p.cols <= 8192 ? rmsnorm_kernel<true, 1, T, W> : rmsnorm_kernel<true, 2, T, W>,
+                 dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(threads), 0, st, p);
 }
 
 // Parts of the weight's gradient: two rows to a workgroup where there are not many for each (1201 x
@@ -446,33 +457,29 @@ int parts_for(int rows, int rows_per_block, int most) {
 
 int grad_parts(int rows, int cols) {
   if (cols > kRegCols) return rows < kLongParts ? rows : kLongParts;
-  if (cols <= 512) return parts_for(rows, 4, parts_of(64));
-  return parts_for(rows, 1, parts_of(cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024));
+  const int threads = row_threads(cols);
+  return parts_for(rows, threads == 64 ? 4 : 1, parts_of(threads));
 }
 
 // Launches the rows' pass; returns the parts of the weight's gradient that it leaves.
-template <int L, int NV, typename T, typename D>
-int launch_grad(const NormGradParams& p, bool dw, hipStream_t st) {
-  constexpr int kThreads = threads_of(L);
-  const uint32_t grid = dw ? (uint32_t)parts_for(p.rows, kThreads / L, parts_of(L)) : row_grid(p.rows, kThreads / L, kMaxGrid);
-  if (dw) launch_timed("rmsnorm_grad", rmsnorm_grad_kernel<L, NV, true, T, D>, dim3(grid), dim3(kThreads), 0, st, p);
-  else launch_timed("rmsnorm_grad", rmsnorm_grad_kernel<L, NV, false, T, D>, dim3(grid), dim3(kThreads), 0, st, p);
+template <bool DW, typename T, typename D>
+int launch_grad(const NormGradParams& p, hipStream_t st) {
+  const int threads = row_threads(p.cols);
+  const uint32_t grid = DW ? (uint32_t)grad_parts(p.rows, p.cols) : row_grid(p.rows, threads == 64 ? 4 : 1, kMaxGrid);
+  launch_timed("rmsnorm_grad",
+               threads == 64      ? rmsnorm_grad_kernel<false, 1, DW, T, D>
+               : p.cols <= 8192 ? rmsnorm_grad_kernel<true, 1, DW, T, D>
+                                : rmsnorm_grad_kernel<true, 2, DW, T, D>,
+               dim3(grid), dim3(threads == 64 ? 256 : threads), 0, st, p);
   return (int)grid;
-}
-
-template <typename T, typename D>
-int launch_grad_cols(const NormGradParams& p, bool dw, hipStream_t st) {
-  if (p.cols <= 512) return launch_grad<64, 1, T, D>(p, dw, st);
-  if (p.cols <= 1024) return launch_grad<128, 1, T, D>(p, dw, st);
-  if (p.cols <= 2048) return launch_grad<256, 1, T, D>(p, dw, st);
-  if (p.cols <= 4096) return launch_grad<512, 1, T, D>(p, dw, st);
-  if (p.cols <= 8192) return launch_grad<1024, 1, T, D>(p, dw, st);
-  return launch_grad<1024, 2, T, D>(p, dw, st);
 }
 
 template <typename T>
 int launch_grad_of(const NormGradParams& p, bool dw, hipStream_t st) {
-  if (p.cols <= kRegCols) return p.y_f32 ? launch_grad_cols<T, float>(p, dw, st) : launch_grad_cols<T, uint16_t>(p, dw, st);
+  if (p.cols <= kRegCols) {
+    if (p.y_f32) return dw ? launch_grad<true, T, float>(p, st) : launch_grad<false, T, float>(p, st);
+    return dw ? launch_grad<true, T, uint16_t>(p, st) : launch_grad<false, T, uint16_t>(p, st);
+  }
   launch_timed("rmsnorm_grad_long", rmsnorm_grad_long_kernel<T>, dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(1024), 0, st, p);
   const int parts = grad_parts(p.rows, p.cols);
   if (dw)
@@ -506,8 +513,8 @@ hipError_t launch_rmsnorm(const mira_rmsnorm_args& a, hipStream_t st) {
   p.y_f32 = a.y_dtype == MIRA_F32;
   p.eps = a.eps;
   p.q_eps = a.q_eps;
-  if (a.x_dtype == MIRA_F32) launch_norm_of<float>(p, st);
-  else launch_norm_of<uint16_t>(p, st);
+  if (a.x_dtype == MIRA_F32) p.w_f32 ? launch_norm_of<float, float>(p, st) : launch_norm_of<float, uint16_t>(p, st);
+  else p.w_f32 ? launch_norm_of<uint16_t, float>(p, st) : launch_norm_of<uint16_t, uint16_t>(p, st);
   return hipGetLastError();
 }
 

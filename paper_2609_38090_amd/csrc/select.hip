@@ -23,7 +23,9 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / 64;  // of a chunk's workgroup
 constexpr int kPlaceThreads = 1024;
 constexpr int kChunk = 256;     // most tokens of a chunk
-constexpr int kFewChunks = 64;  // of a call that adds up its chunks' counts where they are used
+// Counts (chunks times groups) that every chunk's workgroup adds up for itself, instead of a launch
+// in between.
+constexpr int kFewCounts = 16384;
 constexpr int kWords = kChunk / 32;
 constexpr float kTiny = 1e-20f;
 constexpr int kMaxGrid = 1 << 21;  // workgroups of 256 threads: fewer than 2^32 in a launch
@@ -564,8 +566,8 @@ struct PlaceLds {
 };
 
 // Order and positions of a chunk's pairs, by the whole workgroup.  sel(i) is the expert
-// of pair i of the chunk, kept(t) whether its token t has shared experts; total(g) the pairs
-// of group g in the call, before(g) those in earlier chunks.
+// of pair i of the chunk, kept(t) whether its token t has shared experts; total(g), called by
+// thread g, the pairs of group g in the call, before(g) those in earlier chunks.
 template <int THREADS, typename Sel, typename Kept, typename Total, typename Before>
 __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, int chunk, Sel sel, Kept kept, Total total, Before before) {
   const int t = threadIdx.x, G = p.E + p.S, t0 = chunk * p.chunk, n = min(p.chunk, p.T - t0);
@@ -698,34 +700,41 @@ __global__ __launch_bounds__(256) void route_scan_kernel(SelectParams p) {
   if (threadIdx.x == 0) p.totals[g] = run;
 }
 
-// Places a chunk's pairs.  FEW: the chunks' counts are added up here.
+// Places a chunk's pairs.  FEW: the chunks' counts are added up here, by as many threads to a group as
+// there are for the next power of two of groups.
 template <bool FEW>
-__global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(SelectParams p) {
+__global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(SelectParams p, int log_groups) {
   __shared__ PlaceLds place;
-  __shared__ int before_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS], total_s[FEW ? 4 : 1][MIRA_MAX_EXPERTS];
-  const int chunk = blockIdx.x, t0 = chunk * p.chunk, G = p.E + p.S;
-  if constexpr (FEW) {  // four threads to a group
-    const int g = threadIdx.x & 255, q = threadIdx.x >> 8;
-    int before = 0, total = 0;
+  __shared__ int2 part[FEW ? kPlaceThreads : 1];  // pairs of earlier chunks, of all
+  const int chunk = blockIdx.x, t0 = chunk * p.chunk, t = threadIdx.x, G = p.E + p.S;
+  int before = 0, total = 0;  // of group t
+  if constexpr (FEW) {
+    const int g = t & ((1 << log_groups) - 1), many = kPlaceThreads >> log_groups;
+    int2 s{0, 0};
     if (g < G) {
-#pragma unroll 4
-      for (int c = q; c < p.chunks; c += 4) {
+#pragma unroll 8
+      for (int c = t >> log_groups; c < p.chunks; c += many) {
         const int v = p.counts[(size_t)c * G + g];
-        total += v;
-        before += c < chunk ? v : 0;
+        s.x += c < chunk ? v : 0;
+        s.y += v;
       }
     }
-    before_s[q][g] = before;
-    total_s[q][g] = total;
+    part[t] = s;
     __syncthreads();
+    if (t < G)
+      for (int i = 0; i < many; ++i) {
+        const int2 o = part[(i << log_groups) + t];
+        before += o.x;
+        total += o.y;
+      }
+  } else if (t < G) {
+    before = p.counts[(size_t)chunk * G + t];
+    total = p.totals[t];
   }
   const int32_t* idx = p.idx + (size_t)t0 * p.k;
   place_pairs<kPlaceThreads>(
       p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; },
-      [&](int g) { return FEW ? total_s[0][g] + total_s[FEW][g] + total_s[FEW * 2][g] + total_s[FEW * 3][g] : p.totals[g]; },
-      [&](int g) {
-        return FEW ? before_s[0][g] + before_s[FEW][g] + before_s[FEW * 2][g] + before_s[FEW * 3][g] : p.counts[(size_t)chunk * G + g];
-      });
+      [&](int) { return total; }, [&](int) { return before; });
 }
 
 // Tokens of a chunk: 32 until the chunks fill the CUs, then more, in steps of 32.
@@ -898,11 +907,13 @@ hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) 
   if (a.logits_dtype == MIRA_F32) launch_select_of<float>(p, st);
   else launch_select_of<uint16_t>(p, st);
   if (p.place && p.chunks > 1) {
-    if (p.chunks <= kFewChunks) {
-      launch_timed("route_place", route_place_kernel<true>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p);
+    int log_groups = 4;
+    while (1 << log_groups < G) ++log_groups;
+    if ((int64_t)p.chunks * G <= kFewCounts) {
+      launch_timed("route_place", route_place_kernel<true>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p, log_groups);
     } else {
       launch_timed("route_scan", route_scan_kernel, dim3(G), dim3(256), 0, st, p);
-      launch_timed("route_place", route_place_kernel<false>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p);
+      launch_timed("route_place", route_place_kernel<false>, dim3(p.chunks), dim3(kPlaceThreads), 0, st, p, log_groups);
     }
   }
   return hipGetLastError();

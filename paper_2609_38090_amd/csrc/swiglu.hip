@@ -46,12 +46,17 @@ __global__ __launch_bounds__(256) void swiglu_grad_kernel(SwigluGradParams p, in
     const size_t r = block / (uint32_t)nb;
     const int c = (int)(block - (uint32_t)r * nb) * 128 + (threadIdx.x & 15) * 8;
     const T* x = (const T*)p.x + r * p.ldx;
-    float g[8], u[8], d[8];
-    load_cols(x, c, p.cols, g);
-    load_cols(x + p.cols, c, p.cols, u);
-    load_cols((const D*)p.d + r * p.ldd, c, p.cols, d);
+    Raw8<T> gate, up;
+    Raw8<D> d;
+    load_raw(x, c, p.cols, gate);
+    load_raw(x + p.cols, c, p.cols, up);
+    load_raw((const D*)p.d + r * p.ldd, c, p.cols, d);
+    settle(gate, c, p.cols);
+    settle(up, c, p.cols);
+    settle(d, c, p.cols);
+    float g[8], u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) swiglu_grad(g[i], u[i], d[i], &g[i], &u[i]);
+    for (int i = 0; i < 8; ++i) swiglu_grad(gate[i], up[i], d[i], &g[i], &u[i]);
     if (p.dx) {
       T* o = (T*)p.dx + r * p.ld_dx;
       store_cols(o, c, p.cols, g);

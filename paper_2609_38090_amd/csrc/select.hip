@@ -20,12 +20,14 @@ namespace mira {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;  // of a chunk's workgroup
+constexpr int kThreads = 512;      // of a chunk's workgroup, kOneThreads where one chunk is all
+constexpr int kOneThreads = 1024;
 constexpr int kPlaceThreads = 1024;
 constexpr int kChunk = 256;     // most tokens of a chunk
 // Counts (chunks times groups) that every chunk's workgroup adds up for itself, instead of a launch
-// in between.
-constexpr int kFewCounts = 16384;
+// in between (us with and without: 64 chunks of 66 groups 10.0 and 12.8, 256 of 66 12.9 and 13.8, 256
+// of 256 21.3 and 20.3).
+constexpr int kFewCounts = 32768;
 constexpr int kWords = kChunk / 32;
 constexpr float kTiny = 1e-20f;
 constexpr int kMaxGrid = 1 << 21;  // workgroups of 256 threads: fewer than 2^32 in a launch
@@ -77,14 +79,9 @@ struct Pick {
   float w;
 };
 
-// The weights of a row's selection, held by 16 lanes.
-template <typename T>
-__device__ __forceinline__ Pick weigh(const SelectParams& p, const T* x, int e, float m, float inv_sum, bool nan) {
-  float s = 0.f;
-  if (e >= 0) {
-    const float v = load_act(x, e);
-    s = p.sigmoid ? sigmoid(v) : exp_neg(v - m) * inv_sum;
-  }
+// The weights of a row's selection, held by 16 lanes: experts and their logits.
+__device__ __forceinline__ Pick weigh(const SelectParams& p, int e, float v, float m, float inv_sum, bool nan) {
+  const float s = e < 0 ? 0.f : p.sigmoid ? sigmoid(v) : exp_neg(v - m) * inv_sum;
   float scale = p.scale;
   if (p.renorm) scale *= __builtin_amdgcn_rcpf(lanes_reduce<16, AddOp>(s) + kTiny);
   return Pick{e, e < 0 ? 0.f : nan ? __builtin_nanf("") : s * scale};
@@ -106,19 +103,27 @@ __device__ __forceinline__ double dpp_d(double v) {
   const uint64_t u = (uint64_t)__double_as_longlong(v);
   return __longlong_as_double((long long)((uint64_t)dpp_u<CTRL>((uint32_t)(u >> 32)) << 32 | dpp_u<CTRL>((uint32_t)u)));
 }
+// (Both halves of 32 or 64 lanes swapped: one of the two results is the lane's own value.)
 __device__ __forceinline__ double wave_max64(double v) {
   v = fmax(v, dpp_d<0xB1>(v));
   v = fmax(v, dpp_d<0x4E>(v));
   v = fmax(v, dpp_d<0x141>(v));
   v = fmax(v, dpp_d<0x140>(v));
-  v = fmax(v, __shfl_xor(v, 16, 64));
-  return fmax(v, __shfl_xor(v, 32, 64));
+  uint64_t u = (uint64_t)__double_as_longlong(v);
+  auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = fmax(__longlong_as_double((long long)((uint64_t)hi[0] << 32 | lo[0])), __longlong_as_double((long long)((uint64_t)hi[1] << 32 | lo[1])));
+  u = (uint64_t)__double_as_longlong(v);
+  lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return fmax(__longlong_as_double((long long)((uint64_t)hi[0] << 32 | lo[0])), __longlong_as_double((long long)((uint64_t)hi[1] << 32 | lo[1])));
 }
 __device__ __forceinline__ int wave_min(int v) {
   uint32_t u = max16_u(~(uint32_t)v);
-  u = max(u, (uint32_t)__shfl_xor((int)u, 16, 64));
-  u = max(u, (uint32_t)__shfl_xor((int)u, 32, 64));
-  return (int)~u;
+  auto w = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = max(w[0], w[1]);
+  w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return (int)~max(w[0], w[1]);
 }
 
 // One row by the whole wave with c in 64 bits.  The result is in lanes 0..15.
@@ -127,10 +132,13 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
   const int lane = threadIdx.x & 63;
   const T* x = (const T*)p.logits + (size_t)row * p.ld;
   const double none = -(double)INFINITY;
-  float v[4], m = -INFINITY;
+  float v[4], b[4], m = -INFINITY;
   bool nan = false;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = lane + 64 * i < p.E ? load_act(x, lane + 64 * i) : -INFINITY;
+  for (int i = 0; i < 4; ++i) {
+    v[i] = lane + 64 * i < p.E ? load_act(x, lane + 64 * i) : -INFINITY;
+    b[i] = p.bias && lane + 64 * i < p.E ? p.bias[lane + 64 * i] : 0.f;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     nan |= v[i] != v[i];
@@ -158,10 +166,12 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
     for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
   }
   if (scored) {
-#pragma unroll 1
-    for (int e = lane; e < p.E; e += 64) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = lane + 64 * i;
+      if (e >= p.E) continue;
       const double ex = scr.wide.group[e];
-      const double c = (p.sigmoid ? 1.0 : ex) / (p.sigmoid ? 1.0 + ex : total) + (p.bias ? (double)p.bias[e] : 0.0);
+      const double c = (p.sigmoid ? 1.0 : ex) / (p.sigmoid ? 1.0 + ex : total) + (double)b[i];
       if (scr.wide.c[e] != none) scr.wide.c[e] = c;
     }
   }
@@ -185,7 +195,7 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
     for (int g = lane, i = 0; g < p.groups; g += 64, ++i) {
       const double mine = scr.wide.group[g];
       int before = 0;
-#pragma unroll 1
+#pragma unroll 4
       for (int h = 0; h < p.groups; ++h) {
         const double o = scr.wide.group[h];
         before += o > mine || (o == mine && h < g);
@@ -219,7 +229,7 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
 #pragma unroll
     for (int i = 0; i < 4; ++i) c[i] = lane + 64 * i == at ? none : c[i];
   }
-  const Pick r = weigh(p, x, mine, m, p.sigmoid ? 1.f : (float)(1.0 / total), nan);
+  const Pick r = weigh(p, mine, mine >= 0 ? load_act(x, mine) : 0.f, m, p.sigmoid ? 1.f : (float)(1.0 / total), nan);
   wave_sync();
   return r;
 }
@@ -532,9 +542,17 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
   const uint32_t right = dpp_u<0x101>(mine);  // (row_shl 1: the next lane's, read by all lanes)
   const uint32_t after = l == k - 1 ? next : right;
   const int e = l < k && mine != 0u ? 255 - (int)(mine & 255u) : -1;
-  wide |= e >= 0 && after != 0u && (int)(mine >> 8) - (int)(after >> 8) <= margin;
+  const float of_e = e >= 0 ? load_act(x, e) : 0.f;
+  bool order = (int)(mine >> 8) - (int)(after >> 8) > margin;
+  if constexpr (sizeof(T) == 4) {
+    // among the selected, logits themselves tell whether their order is right
+    const float of_right = dpp<0x101>(of_e);
+    const int e_right = (int)dpp_u<0x101>((uint32_t)e);
+    if (!scored && l < k - 1) order = of_e > of_right || (of_e == of_right && e < e_right);
+  }
+  wide |= e >= 0 && after != 0u && !order;
   *again = (__ballot(wide && live) >> (lane & 48) & 0xFFFFu) != 0;
-  return weigh(p, x, live ? e : -1, m, inv_sum, false);
+  return weigh(p, live ? e : -1, of_e, m, inv_sum, false);
 }
 
 // Exclusive sum over threads 0..255 (each its own count; others 0); total in all threads.
@@ -620,7 +638,8 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
 // one (within the loop the constants of a 64-bit exp would take the registers of half the waves).
 // One chunk places its pairs at once (ONE); several leave their counts.
 template <int V, bool ONE, typename T>
-__global__ __launch_bounds__(kThreads) void route_select_kernel(SelectParams p) {
+__global__ __launch_bounds__(ONE ? kOneThreads : kThreads) void route_select_kernel(SelectParams p) {
+  constexpr int kWaves = (ONE ? kOneThreads : kThreads) / 64;
   __shared__ SelectScratch scr[kWaves];
   __shared__ float bias[MIRA_MAX_EXPERTS];
   __shared__ float wave_max_bias[4];
@@ -676,7 +695,7 @@ __global__ __launch_bounds__(kThreads) void route_select_kernel(SelectParams p) 
   auto count = [&](int g) { return g < p.E ? hist[g] : kept; };
   if constexpr (ONE) {
     __shared__ PlaceLds place;
-    place_pairs<kThreads>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; }, count,
+    place_pairs<kOneThreads>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; }, count,
                           [](int) { return 0; });
   } else {
     if (t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = count(t);
@@ -737,17 +756,22 @@ __global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(SelectParams
       [&](int) { return total; }, [&](int) { return before; });
 }
 
+// Most tokens of a call in one launch, a workgroup of 64 rows at a time (us, in one against two: 64 of
+// 256 experts 7.6 and 9.0, 96 8.8 and 9.0, 128 11.2 and 9.1, of 64 experts 7.8 and 9.0).
+int one_tokens(int E) { return E <= 64 ? 128 : 64; }
+
 // Tokens of a chunk: 32 until the chunks fill the CUs, then more, in steps of 32.
-int chunk_tokens(int T) {
+int chunk_tokens(int T, int E) {
+  if (T <= one_tokens(E)) return one_tokens(E);
   const int c = ((T + 255) / 256 + 31) / 32 * 32;
   return c < 32 ? 32 : c > kChunk ? kChunk : c;
 }
-int chunk_count(int T) { return (int)(((int64_t)T + chunk_tokens(T) - 1) / chunk_tokens(T)); }
+int chunk_count(int T, int E) { return (int)(((int64_t)T + chunk_tokens(T, E) - 1) / chunk_tokens(T, E)); }
 
 template <int V, typename T>
 void launch_select(const SelectParams& p, hipStream_t st) {
   launch_timed("route_select", p.chunks == 1 ? route_select_kernel<V, true, T> : route_select_kernel<V, false, T>, dim3(p.chunks),
-               dim3(kThreads), 0, st, p);
+               dim3(p.chunks == 1 ? kOneThreads : kThreads), 0, st, p);
 }
 
 template <typename T>
@@ -895,8 +919,8 @@ hipError_t launch_route_select(const mira_route_select_args& a, hipStream_t st) 
   p.groups = a.top_groups == a.n_groups ? 1 : a.n_groups;  // all groups kept is none
   p.top_groups = a.top_groups;
   p.best = a.group_best;
-  p.chunk = chunk_tokens(p.T);
-  p.chunks = chunk_count(p.T < 1 ? 1 : p.T);
+  p.chunk = chunk_tokens(p.T, p.E);
+  p.chunks = p.T < 1 ? 1 : chunk_count(p.T, p.E);
   p.sigmoid = a.flags & MIRA_ROUTE_SIGMOID;
   p.renorm = a.flags & MIRA_ROUTE_RENORM;
   p.scale = a.scale;

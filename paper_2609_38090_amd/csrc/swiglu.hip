@@ -2,8 +2,9 @@
 //   dgate = d up s (1 + gate (1 - s)),  dup = d gate s,
 // as rows and as e4m3 with one scale per block of 1 x 128.  Memory bound: each value is
 // read once, eight columns of gate, up and d to a lane, and both results leave from there.
-// Where cols is no multiple of 128, e4m3 blocks do not line up between the halves: lanes
-// then go by blocks of the result and read their three values for each half.
+// Where cols is no multiple of 128, e4m3 blocks do not line up between the halves: a row then
+// belongs to a wave or a workgroup, whose blocks' maxima meet in LDS (maxima do not depend on the
+// order of their atomics).
 #include "fp8_dev.h"
 
 namespace mira {
@@ -71,7 +72,99 @@ __global__ __launch_bounds__(256) void swiglu_grad_kernel(SwigluGradParams p, in
   }
 }
 
-// By blocks of the result.
+// A row's gradient in e4m3 for any number of columns up to kRowCols: a wave (ROW false, up to 512
+// columns, four rows to a workgroup) or a workgroup to a row.
+constexpr int kRowCols = 16384;
+typedef int v2i_bytes __attribute__((ext_vector_type(2), aligned(1)));  // (global stores take any alignment)
+
+template <bool ROW, int NV, typename T, typename D>
+__global__ __launch_bounds__(ROW ? 1024 : 256) void swiglu_grad_row_kernel(SwigluGradParams p) {
+  constexpr int kRows = ROW ? 1 : 4, kBlocks = ROW ? 2 * kRowCols / 128 : 8;
+  __shared__ uint32_t largest[kRows][kBlocks];  // of each block of the result, as the bits of a magnitude
+  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63, w = ROW ? 0 : threadIdx.x >> 6;
+  const int blocks = (2 * p.cols + 127) / 128;
+  auto meet = [] {
+    if constexpr (ROW) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  for (size_t r = (size_t)blockIdx.x * kRows + w; r < (size_t)p.rows; r += (size_t)gridDim.x * kRows) {
+    const T* x = (const T*)p.x + r * p.ldx;
+    Raw8<T> gate[NV], up[NV];
+    Raw8<D> d[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * L + l) * 8;
+      load_raw(x, c, p.cols, gate[i]);
+      load_raw(x + p.cols, c, p.cols, up[i]);
+      load_raw((const D*)p.d + r * p.ldd, c, p.cols, d[i]);
+    }
+    meet();  // (the last row's maxima have been read)
+    for (int b = l; b < blocks; b += L) largest[w][b] = 0;
+    meet();
+    float g[NV][8], u[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * L + l) * 8;
+      settle(gate[i], c, p.cols);
+      settle(up[i], c, p.cols);
+      settle(d[i], c, p.cols);
+      // dup's columns are cols + c on; from `split` of them on they are in the next block
+      const int first = (p.cols + c) >> 7, split = 128 - ((p.cols + c) & 127);
+      float m = 0.f, lo = 0.f, hi = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        swiglu_grad(gate[i][j], up[i][j], d[i][j], &g[i][j], &u[i][j]);
+        m = max_abs(m, g[i][j]);
+        lo = j < split ? max_abs(lo, u[i][j]) : lo;
+        hi = j < split ? hi : max_abs(hi, u[i][j]);
+      }
+      m = max16(m);
+      if (c < p.cols) {
+        if ((l & 15) == 0) atomicMax(&largest[w][c >> 7], __float_as_uint(m));
+        atomicMax(&largest[w][first], __float_as_uint(lo));
+        if (hi > 0.f) atomicMax(&largest[w][first + 1], __float_as_uint(hi));
+      }
+    }
+    meet();
+    for (int b = l; b < blocks; b += L) p.scale[r * p.ld_s + b] = fmaxf(__uint_as_float(largest[w][b]), p.q_eps) / kE4m3Max;
+    uint8_t* q = p.q + r * p.ldq;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * L + l) * 8;
+      if (c >= p.cols) continue;
+      if (p.dx) {
+        T* o = (T*)p.dx + r * p.ld_dx;
+        store_cols(o, c, p.cols, g[i]);
+        store_cols(o + p.cols, c, p.cols, u[i]);
+      }
+      const int first = (p.cols + c) >> 7, split = 128 - ((p.cols + c) & 127);
+      auto inverse = [&](int b) { return kE4m3Max / fmaxf(__uint_as_float(largest[w][min(b, blocks - 1)]), p.q_eps); };
+      const float inv_lo = inverse(first), inv_hi = inverse(first + 1);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[i][j] *= j < split ? inv_lo : inv_hi;
+      const uint2 qg = to_e4m3x8(g[i], inverse(c >> 7)), qu = to_e4m3x8(u[i], 1.f);
+      if (c + 8 <= p.cols) {
+        *(uint2*)(q + c) = qg;
+        *(v2i_bytes*)(q + p.cols + c) = v2i_bytes{(int)qu.x, (int)qu.y};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < p.cols) {
+            q[c + j] = (uint8_t)((j < 4 ? qg.x : qg.y) >> (j & 3) * 8);
+            q[p.cols + c + j] = (uint8_t)((j < 4 ? qu.x : qu.y) >> (j & 3) * 8);
+          }
+      }
+    }
+    const int behind = 2 * p.cols + l;  // zeros up to the next multiple of 16
+    if (behind < (int)align_up((size_t)p.cols * 2, 16)) q[behind] = 0;
+  }
+}
+
+// Longer rows, by blocks of the result: the three values are read for each half.
 template <typename T, typename D>
 __global__ __launch_bounds__(256) void swiglu_grad_any_kernel(SwigluGradParams p, int nb) {
   const uint32_t total = (uint32_t)p.rows * nb;  // < 2^31
@@ -112,6 +205,16 @@ __global__ __launch_bounds__(256) void swiglu_grad_any_kernel(SwigluGradParams p
 template <typename T, typename D>
 void launch_of(const SwigluGradParams& p, hipStream_t st) {
   const bool step = !p.q || p.cols % 128 == 0;
+  if (!step && p.cols <= kRowCols) {
+    const int lanes = p.cols <= 8192 ? p.cols : (p.cols + 1) / 2, threads = (lanes + 511) / 512 * 64;
+    const uint32_t blocks = threads == 64 ? ((uint32_t)p.rows + 3) / 4 : (uint32_t)p.rows;
+    launch_timed("swiglu_grad_row",
+                 threads == 64      ? swiglu_grad_row_kernel<false, 1, T, D>
+                 : p.cols <= 8192 ? swiglu_grad_row_kernel<true, 1, T, D>
+                                  : swiglu_grad_row_kernel<true, 2, T, D>,
+                 dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(threads == 64 ? 256 : threads), 0, st, p);
+    return;
+  }
   const int nb = (int)(((size_t)p.cols * (step ? 1 : 2) + 127) / 128);
   const size_t blocks = ((size_t)p.rows * nb + 15) / 16;
   const dim3 grid((uint32_t)(blocks < kMaxGrid ? blocks : kMaxGrid));

@@ -9,7 +9,8 @@ from layer_reference import U32, Guarded, code, dt, e4m3_close, f64, swiglu_grad
 from ops_reference import TABLE
 
 pytestmark = pytest.mark.gpu
-SIZES = [(1, 1), (1, 128), (3, 127), (5, 129), (2, 64), (17, 1000), (301, 1001), (7, 1408), (4, 14336), (2, 20001), (600, 40)]
+SIZES = [(1, 1), (1, 128), (3, 127), (5, 129), (2, 64), (17, 1000), (301, 1001), (7, 1408), (4, 14336), (2, 20001), (600, 40), (3, 9001), (5, 520), (9, 65),
+         (3, 8193), (2, 16383), (6, 512), (6, 511), (5, 7)]
 # exp 4 half steps (and of its rounded sum), the reciprocal 2, 1 - s 2 more, three products; beside the terms' magnitude
 STEPS = 16
 

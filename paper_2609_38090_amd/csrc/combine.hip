@@ -105,16 +105,18 @@ struct CombineGradParams {
 };
 
 // 2^share waves take a token, 512 columns each at a time; their sums of products meet in LDS.  A
+// workgroup has four waves, or 16 for one token where tokens are few and rows long (2 tokens of 9 x
+// 14595 33 us with four, 18 so).  A
 // token's positions and weights are loaded at once, one to a lane, and so are four pairs' rows: with
 // each pair's loads behind the last one's, 2048 tokens of 8 x 2048 to e4m3 took 28 us, so 25 (93 MB;
 // eight pairs' rows at once the same).
 // The blocks' maxima of w dout are w times those of dout, rounding being monotonic, so a block is
 // searched once for all the token's pairs.
 template <int K, typename Y, typename O>
-__global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradParams p, int share) {
+__global__ __launch_bounds__(1024) void combine_grad_kernel(CombineGradParams p, int share) {
   constexpr int NB = 4;
-  __shared__ float part[2][4][K];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = 4 >> share;  // tokens of a workgroup
+  __shared__ float part[2][16][K];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = ((int)blockDim.x >> 6) >> share;  // tokens of a workgroup
   const int first = wave & ((1 << share) - 1), span = 512 << share;
   const int end = (int)align_up((size_t)p.cols, 512), pairs = p.k + p.S;
   const bool dots = p.dw && p.y_rows > 0;
@@ -201,9 +203,11 @@ void launch_combine_of(const CombineParams& p, hipStream_t st) {
 }
 template <typename Y, typename O>
 void launch_combine_grad_of(const CombineGradParams& p, hipStream_t st) {
-  const int share = p.cols <= 512 ? 0 : p.cols <= 1024 ? 1 : 2;
-  const uint32_t blocks = ((uint32_t)p.T + (4 >> share) - 1) / (4 >> share);
-  launch_timed("combine_grad", p.k <= 8 ? combine_grad_kernel<8, Y, O> : combine_grad_kernel<MIRA_MAX_TOPK, Y, O>, dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(256), 0, st, p, share);
+  const bool wide = p.T <= 256 && p.cols > 2048;
+  const int share = wide ? 4 : p.cols <= 512 ? 0 : p.cols <= 1024 ? 1 : 2, per = wide ? 1 : 4 >> share;
+  const uint32_t blocks = ((uint32_t)p.T + per - 1) / per;
+  launch_timed("combine_grad", p.k <= 8 ? combine_grad_kernel<8, Y, O> : combine_grad_kernel<MIRA_MAX_TOPK, Y, O>,
+               dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(wide ? 1024 : 256), 0, st, p, share);
 }
 
 }  // namespace

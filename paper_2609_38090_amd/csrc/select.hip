@@ -543,13 +543,11 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
   const uint32_t after = l == k - 1 ? next : right;
   const int e = l < k && mine != 0u ? 255 - (int)(mine & 255u) : -1;
   const float of_e = e >= 0 ? load_act(x, e) : 0.f;
+  // among the selected, logits themselves tell without a bias whether their order is right
+  const float of_right = dpp<0x101>(of_e);
+  const int e_right = (int)dpp_u<0x101>((uint32_t)e);
   bool order = (int)(mine >> 8) - (int)(after >> 8) > margin;
-  if constexpr (sizeof(T) == 4) {
-    // among the selected, logits themselves tell whether their order is right
-    const float of_right = dpp<0x101>(of_e);
-    const int e_right = (int)dpp_u<0x101>((uint32_t)e);
-    if (!scored && l < k - 1) order = of_e > of_right || (of_e == of_right && e < e_right);
-  }
+  if (!p.bias && l < k - 1) order = of_e > of_right || (of_e == of_right && e < e_right);
   wide |= e >= 0 && after != 0u && !order;
   *again = (__ballot(wide && live) >> (lane & 48) & 0xFFFFu) != 0;
   return weigh(p, live ? e : -1, of_e, m, inv_sum, false);

@@ -13,8 +13,7 @@
 // Order: a chunk of tokens is a workgroup.  Each expert has a bit for every token of the
 // chunk, so a pair's rank in its expert's list is a count of bits: no order of atomics
 // decides anything.  Counts of all chunks are added up by a launch in between.
-#include "device_util.h"
-#include "mira_internal.h"
+#include "fp8_dev.h"
 
 namespace mira {
 
@@ -794,85 +793,150 @@ struct SelectGradParams {
   float scale;
 };
 
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+// Four values of a row from column c on; a lane at the row's end loads its last four and settle4(), called
+// once all loads are on their way, moves them to their places.
+template <typename T>
+__device__ __forceinline__ void load4(const T* row, int c, int cols, float (&v)[4]) {
+  if (cols >= 4) {  // (the same for all)
+    load_n(row + min(c, cols - 4), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c + i < cols ? load_act(row, c + i) : 0.f;
+  }
+}
+__device__ __forceinline__ void settle4(float (&v)[4], int c, int cols, float beyond) {
+  if (c + 4 <= cols) return;
+  if (cols >= 4) {
+    const int n = c + 4 - cols;
+    if (n & 2) v[0] = v[2], v[1] = v[3];
+    if (n & 1) v[0] = v[1], v[1] = v[2], v[2] = v[3];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = c + i < cols ? v[i] : beyond;
+}
+typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store4(float* row, int c, int cols, const float (&v)[4]) {
+  if (c + 4 <= cols) {
+    *(v4f_any*)(row + c) = v4f{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < cols) row[c + i] = v[i];
+  }
+}
+__device__ __forceinline__ void store4(uint16_t* row, int c, int cols, const float (&v)[4]) {
+  if (c + 4 <= cols) {
+    *(v2u_any*)(row + c) = v2u_any{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < cols) row[c + i] = to_bf16(v[i]);
+  }
+}
 
-// A row to L lanes, four experts l, l + L, .. to a lane; k <= L lanes hold its selection.
+// Adds what selection J of k, in lane J of each 16, has for a lane's experts, c + 64 q + i, and (N)
+// counts it.
+template <int J, bool N, int Q>
+__device__ __forceinline__ void spread(int sel, float g, int k, int c, float (&sum)[Q][4], float (&n)[Q][4]) {
+  if (J < k) {  // (the same for the whole wave)
+    const int at = (int)dpp_u<0x150 + J>((uint32_t)sel) - c;
+    const float of = dpp<0x150 + J>(g);
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sum[q][i] += at == 64 * q + i ? of : 0.f;
+        if (N) n[q][i] += at == 64 * q + i ? 1.f : 0.f;
+      }
+    if constexpr (J + 1 < MIRA_MAX_TOPK) spread<J + 1, N, Q>(sel, g, k, c, sum, n);
+  }
+}
+
+// A row to 16 lanes, experts 4 l + 64 q + 0 .. 3 to lane l; lane j has selection j.
 //   ds_e = scale (g_e - [renorm] A / D) / D on the selected, A = sum g s, D = sum s + 1e-20 (1 without renorm);
-//   sigmoid: dl_e = ds_e s_e (1 - s_e);  softmax: dl_e = s_e (ds_e - B), B = sum ds s, which with
-//   renorm is scale (A / D) (1e-20 / D): as a difference of its terms nothing of it would be left.
-template <int L, typename T>
+//   sigmoid: dl_e = ds_e s_e (1 - s_e), of the selected logits alone;  softmax: dl_e = s_e (ds_e - B), B = sum
+//   ds s, which with renorm is scale (A / D) (1e-20 / D): as a difference of its terms nothing of it
+//   would be left.
+// Bound by its bytes: 131072 x 256 fp32 softmax 69 us for 276 MB, sigmoid 47 us for 147 MB (the selected
+// logits are lines of their own). A row to 64 lanes, one in turn, waited for its loads three
+// times a row (89 and 72 us).
+template <int Q, typename T>
 __global__ __launch_bounds__(256) void route_select_grad_kernel(SelectGradParams p) {
-  const int l = threadIdx.x % L;
+  const int l = threadIdx.x & 15, c = 4 * l;
   // (whole groups of lanes leave the loop)
-  for (size_t row = (size_t)blockIdx.x * (256 / L) + threadIdx.x / L; row < (size_t)p.T; row += (size_t)gridDim.x * (256 / L)) {
-    int sel = -1;
-    float g = 0.f;
-    if (l < p.k) {
-      sel = p.idx[row * p.k + l];
-      if ((uint32_t)sel >= (uint32_t)p.E) sel = -1;
-      if (sel >= 0) g = p.dweight[row * p.k + l];
-    }
+  for (size_t row = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < (size_t)p.T; row += (size_t)gridDim.x * 16) {
     const T* x = (const T*)p.logits + row * p.ld;
-    float v[4], ge[4] = {0.f, 0.f, 0.f, 0.f}, n[4] = {0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = l + L * i < p.E ? load_act(x, l + L * i) : -INFINITY;
-    bool any = false;
-    for (int j = 0; j < p.k; ++j) {
-      const int e = __shfl(sel, j, L);
-      const float ge_j = __shfl(g, j, L);
-      any |= e >= 0;
-  #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (e == l + L * i) {
-          ge[i] += ge_j;
-          n[i] += 1.f;
-        }
+    float v[Q][4], o[Q][4], n[Q][4];
+    int sel = -1;
+    if (l < p.k) sel = p.idx[row * p.k + l];
+    if (!p.sigmoid) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) load4(x, c + 64 * q, p.E, v[q]);
     }
-    float s[4], rest[4];  // scores, and 1 - s for sigmoid
+    float add[Q][4];
+    if (p.add) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) load4((const T*)p.add + row * p.ld_add, c + 64 * q, p.E, add[q]);
+    }
+    if ((uint32_t)sel >= (uint32_t)p.E) sel = -1;
+    const float g = sel >= 0 ? p.dweight[row * p.k + l] : 0.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[q][i] = n[q][i] = 0.f;
     if (p.sigmoid) {
-  #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e = exp_neg(-fabsf(v[i])), r = __builtin_amdgcn_rcpf(1.f + e);
-        const bool up = v[i] >= 0.f;
-        s[i] = n[i] > 0.f ? (up ? r : e * r) : 0.f;
-        rest[i] = up ? e * r : r;
+      float s = 0.f, rest = 0.f;
+      if (sel >= 0) {
+        const float u = load_act(x, sel), e = exp_neg(-fabsf(u)), r = __builtin_amdgcn_rcpf(1.f + e);
+        s = u >= 0.f ? r : e * r;
+        rest = u >= 0.f ? e * r : r;
+        if (u == -INFINITY) s = 0.f;
       }
+      const float A = lanes_reduce<16, AddOp>(g * s), D = lanes_reduce<16, AddOp>(s) + kTiny;
+      const float inv = p.renorm ? 1.f / D : 1.f, mean = p.renorm ? A * inv : 0.f;
+      spread<0, false, Q>(sel, sel >= 0 ? p.scale * inv * (g - mean) * s * rest : 0.f, p.k, c, o, n);
     } else {
-      float m = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-      m = lanes_reduce<L, MaxOp>(m);
-      m = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
-  #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i] = exp_neg(v[i] - m);
-        sum += s[i];
+      if (p.renorm) spread<0, true, Q>(sel, g, p.k, c, o, n);
+      else spread<0, false, Q>(sel, g, p.k, c, o, n);
+      float m = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        settle4(v[q], c + 64 * q, p.E, -INFINITY);
+        m = fmaxf(m, fmaxf(fmaxf(v[q][0], v[q][1]), fmaxf(v[q][2], v[q][3])));
       }
-      sum = lanes_reduce<L, AddOp>(sum);
-      const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
-  #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] *= inv;
+      m = lanes_reduce<16, MaxOp>(m);
+      m = m == -INFINITY ? 0.f : m;
+      float sum = 0.f, A = 0.f, D = 0.f;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[q][i] = exp_neg(v[q][i] - m);
+          sum += v[q][i];
+          A = fmaf(o[q][i], v[q][i], A);
+          D = fmaf(n[q][i], v[q][i], D);
+        }
+      sum = lanes_reduce<16, AddOp>(sum);
+      const float to_score = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
+      A = lanes_reduce<16, AddOp>(A) * to_score;
+      D = lanes_reduce<16, AddOp>(D) * to_score + kTiny;
+      const float inv = p.renorm ? 1.f / D : 1.f, mean = p.renorm ? A * inv : 0.f;
+      const float B = p.scale * (p.renorm ? mean * (kTiny * inv) : A);
+      const bool any = lanes_reduce<16, MaxOp>(sel >= 0 ? 1.f : 0.f) > 0.f;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[q][i] = any ? v[q][i] * to_score * (p.scale * inv * (o[q][i] - n[q][i] * mean) - B) : 0.f;
     }
-    float A = 0.f, D = 0.f;
-  #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      A = fmaf(ge[i], s[i], A);
-      D = fmaf(n[i], s[i], D);
-    }
-    A = lanes_reduce<L, AddOp>(A);
-    D = lanes_reduce<L, AddOp>(D) + kTiny;
-    const float inv = p.renorm ? 1.f / D : 1.f, mean = p.renorm ? A * inv : 0.f;
-    const float B = p.scale * (p.renorm ? mean * (kTiny * inv) : A);
-    T* d = (T*)p.d + row * p.ld_d;
-  #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = l + L * i;
-      if (e >= p.E) continue;
-      const float ds = p.scale * inv * (ge[i] - n[i] * mean);
-      float o = !any ? 0.f : p.sigmoid ? ds * s[i] * rest[i] : s[i] * (ds - B);
-      if (p.sigmoid && n[i] == 0.f) o = 0.f;
-      if (p.add) o += load_act((const T*)p.add + row * p.ld_add, e);
-      store1(d + e, o);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (p.add) {
+        settle4(add[q], c + 64 * q, p.E, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[q][i] += add[q][i];
+      }
+      store4((T*)p.d + row * p.ld_d, c + 64 * q, p.E, o[q]);
     }
   }
 }
@@ -958,13 +1022,10 @@ hipError_t launch_route_select_grad(const mira_route_select_grad_args& a, hipStr
   p.renorm = a.flags & MIRA_ROUTE_RENORM;
   p.scale = a.scale;
   const bool f32 = a.logits_dtype == MIRA_F32;
-  if (p.E <= 64) {
-    const dim3 grid(min((p.T + 15) / 16, kMaxGrid));
-    launch_timed("route_select_grad", f32 ? route_select_grad_kernel<16, float> : route_select_grad_kernel<16, uint16_t>, grid, dim3(256), 0, st, p);
-  } else {
-    const dim3 grid(min((p.T + 3) / 4, kMaxGrid));
-    launch_timed("route_select_grad", f32 ? route_select_grad_kernel<64, float> : route_select_grad_kernel<64, uint16_t>, grid, dim3(256), 0, st, p);
-  }
+  auto kernel = p.E <= 64    ? f32 ? route_select_grad_kernel<1, float> : route_select_grad_kernel<1, uint16_t>
+                : p.E <= 128 ? f32 ? route_select_grad_kernel<2, float> : route_select_grad_kernel<2, uint16_t>
+                             : f32 ? route_select_grad_kernel<4, float> : route_select_grad_kernel<4, uint16_t>;
+  launch_timed("route_select_grad", kernel, dim3(min((p.T + 15) / 16, kMaxGrid)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 

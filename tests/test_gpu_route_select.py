@@ -216,7 +216,8 @@ def test_pair_positions_of_a_partial_order():
     assert pos.v[0].tolist() == [-1] * 10
 
 
-@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (16, 8, 2), (300, 61, 4), (77, 64, 16), (130, 100, 3), (65, 256, 8), (2000, 12, 5)])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (16, 8, 2), (300, 61, 4), (77, 64, 16), (130, 100, 3), (65, 256, 8), (2000, 12, 5),
+                                   (33, 2, 2), (50, 3, 1), (65, 5, 4), (19, 129, 16), (40, 255, 1)])
 @pytest.mark.parametrize("sigmoid,renorm,add,name,pad,shift", [(False, False, False, "f32", 0, 0), (False, True, True, "f32", 3, 1), (True, True, False, "bf16", 0, 0),
                                                                (True, False, True, "bf16", 5, 3), (False, False, True, "bf16", 1, 1), (True, True, True, "f32", 2, 0)])
 def test_gradient(T, E, k, sigmoid, renorm, add, name, pad, shift):
@@ -257,6 +258,22 @@ def test_gradient(T, E, k, sigmoid, renorm, add, name, pad, shift):
         mira.mira_route_select_grad(args)
         torch.cuda.synchronize()
         assert torch.equal(X.v, first)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("E", [4, 100, 200])
+def test_gradient_of_an_expert_selected_twice(sigmoid, renorm, E):
+    """Each entry counts, whatever it selects."""
+    rng = np.random.default_rng(E)
+    x = _logits(rng, 40, E, "f32")
+    idx = torch.from_numpy(rng.integers(0, 4, (40, 6)).astype(np.int32)).cuda()
+    g, d = torch.randn(40, 6, device="cuda"), torch.empty(40, E, device="cuda")
+    flags = (mira.MIRA_ROUTE_SIGMOID if sigmoid else 0) | (mira.MIRA_ROUTE_RENORM if renorm else 0)
+    mira.mira_route_select_grad(mira.RouteSelectGradArgs(logits=x, topk_idx=idx, dweight=g, n_tokens=40, n_experts=E, top_k=6, flags=flags, dlogits=d))
+    torch.cuda.synchronize()
+    want, mag = select_grad(f64(x), idx.cpu().numpy(), f64(g), sigmoid, renorm, 1.0)
+    assert (np.abs(f64(d) - want) <= 2 * STEPS * U32 * mag + 2.0 ** -120).all()
 
 
 @pytest.mark.parametrize("sigmoid", [False, True])

@@ -120,7 +120,7 @@ struct Raw8<uint16_t> {
 // Columns c .. c + 7 of a row.  A lane at the row's end loads the row's last eight, and settle(), called
 // once all loads are on their way, moves them to their places, zeros behind: a load behind a
 // condition of its own would be waited for before the next (a row's three loads one after another:
-// 30000 x 700 bf16 82 us for a norm's gradient, 43 so).
+// 30000 x 700 bf16 82 us for a norm's gradient, 42 so).
 template <typename T>
 __device__ __forceinline__ void load_raw(const T* row, int c, int cols, Raw8<T>& v) {
   if (cols >= 8) {  // (the same for all)

@@ -6,7 +6,9 @@
 // across the lanes, and every output is written from there.  A row is shared by as many waves
 // as hold it at eight values a lane (sixteen above 8192 columns), a workgroup of its own from two
 // waves on; rows of more than 16384 are read twice.  The gradient of the weight is summed in
-// registers over the rows that a workgroup walks, then over workgroups in order.
+// registers over the rows that a workgroup walks, then over workgroups in order.  4096 x 4096 bf16 with
+// residual, y and e4m3 30 us (151 MB, 5.0 TB/s; a copy of 1 GB reaches 5.2); the gradient of 16384 x 4096
+// 100 us (537 MB, 5.4 TB/s).
 #include "fp8_dev.h"
 
 namespace mira {
@@ -450,7 +452,7 @@ void launch_norm_of(const NormParams& p, hipStream_t st) {
 }
 
 // Parts of the weight's gradient: two rows to a workgroup where there are not many for each (1201 x
-// 2001 fp32: 13.0 us so, 14.2 with one, whose parts are as many bytes as the rows; 13.2 with three or four).
+// 2001 fp32: 12.7 us so, 14.2 with one, whose parts are as many bytes as the rows; 13.2 with three or four).
 constexpr int kPartRows = 2;
 int parts_for(int rows, int rows_per_block, int most) {
   const int few = (rows + rows_per_block - 1) / rows_per_block;  // one row after another

@@ -14,8 +14,8 @@
 // chunk, so a pair's rank in its expert's list is a count of bits: no order of atomics
 // decides anything.  Counts of all chunks are added up by a launch in between.
 //
-// 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 77 us (151 MB, for which a copy takes
-// 29): 66 for the selection, bound by instructions (some 730 to four rows, the vector units busy 60 %
+// 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 68 us (151 MB, for which a copy takes
+// 29): 55 for the selection, bound by instructions (some 610 to four rows, the vector units busy 57 %
 // of the time), 6 for the counts, 10 for the order.
 #include "fp8_dev.h"
 
@@ -291,6 +291,21 @@ __device__ __forceinline__ void best_keys(uint32_t (&a)[V]) {
   }
 }
 
+// The largest five of four pairs, each in order, descending, in front.
+__device__ __forceinline__ void best_of_pairs(uint32_t* a) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    order2(a[i], a[i + 3]);
+    order2(a[i + 1], a[i + 2]);
+    order2(a[i], a[i + 1]);
+    order2(a[i + 2], a[i + 3]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) order2(a[i], a[7 - i]);
+  order_bitonic<4>(a);
+  a[4] = max(max(a[4], a[5]), max(a[6], a[7]));
+}
+
 // c step + from is 1 for the least c and below 2^24 for the largest.
 __device__ __forceinline__ float fixed_step(float bias_max) { return 16777210.f / (1.f + 2.f * bias_max); }
 __device__ __forceinline__ float fixed_from(float bias_max) { return fmaf(bias_max, fixed_step(bias_max), 2.f); }
@@ -407,6 +422,7 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key[i] > 255u ? key[i] : 0u;
   }
+  bool paired = false;  // the keys of the groups kept are four pairs in order, in front
   if (groups > 1) {
     // The groups' scores in the units of the keys; below all others (and so before none) where a
     // group has no expert left.
@@ -423,15 +439,22 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
       const int each = size >> 4;
       int g = 0, left = each;
       uint32_t b1 = 0, b2 = 0;
+      if (V == 16 && each == 2) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const uint32_t o = part(i);
-        b2 = max(b2, min(b1, o));
-        b1 = max(b1, o);
-        if (--left == 0) {  // (the same for the whole wave)
-          scr.pair[g++][lane] = uint2{b1, b2};
-          b1 = b2 = 0;
-          left = each;
+        for (int i = 0; i + 1 < V; i += 2) {
+          order2(key[i], key[i + 1]);
+          scr.pair[i / 2][lane] = uint2{key[i], key[i + 1]};
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          b2 = max(b2, min(b1, key[i]));
+          b1 = max(b1, key[i]);
+          if (--left == 0) {  // (the same for the whole wave)
+            scr.pair[g++][lane] = uint2{b1, b2};
+            b1 = b2 = 0;
+            left = each;
+          }
         }
       }
       wave_sync();
@@ -452,7 +475,7 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
       }
       wave_sync();
       // (the lower group first among equals; lanes of no group last)
-      const int score = score_of(b1, b2);
+      const int score = score_of(b1 >> 8, b2 >> 8);
       const int ranked = (l & 7) < groups ? score * 16 + 15 - (l & 7) : (2 * kNone - l) * 16;
       int before = 0;
       rank_step<0>(ranked, before);
@@ -462,14 +485,28 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
         else most = score;
       }
       const uint32_t keep = (uint32_t)(__ballot(in) >> (lane & 48));
-      g = 0, left = each;
-      uint32_t all = (uint32_t)__builtin_amdgcn_sbfe(keep, 0, 1);
+      if (V == 16 && each == 2 && p.top_groups <= 4) {
+        // half of the keys at most are left: as pairs from LDS they need not be sorted among 16 (131072 x
+        // 256 in 8 groups, four kept: 68 us, 76 with the others masked)
+        paired = true;
+        uint32_t rest = keep & 255u;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        key[i] &= all;
-        if (--left == 0) {
-          left = each;
-          all = (uint32_t)__builtin_amdgcn_sbfe(keep, ++g, 1);
+        for (int i = 0; i < 4; ++i) {
+          const uint2 o = scr.pair[__builtin_ctz(rest | 256u) & 7][lane];
+          key[(2 * i) % V] = i < p.top_groups ? o.x : 0u;
+          key[(2 * i + 1) % V] = i < p.top_groups ? o.y : 0u;
+          rest &= rest - 1u;
+        }
+      } else {
+        g = 0, left = each;
+        uint32_t all = (uint32_t)__builtin_amdgcn_sbfe(keep, 0, 1);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          key[i] &= all;
+          if (--left == 0) {
+            left = each;
+            all = (uint32_t)__builtin_amdgcn_sbfe(keep, ++g, 1);
+          }
         }
       }
     } else {
@@ -528,7 +565,12 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
     const int group_margin = sums ? 2 * c_margin + 2 : margin;
     wide |= most > kNone && least - most <= group_margin;
   }
-  best_keys<V>(key);
+  if constexpr (V == 16) {
+    if (paired) best_of_pairs(key);
+    else best_keys<V>(key);
+  } else {
+    best_keys<V>(key);
+  }
   constexpr int D = kDepth<V>;
   const uint32_t last = key[D - 1];
   uint32_t mine = 0, next = 0;

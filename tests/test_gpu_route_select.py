@@ -86,6 +86,21 @@ def test_groups(T, E, k, groups, top, best, sigmoid, biased, name):
     Call(_logits(rng, T, E, name), k, 0, sigmoid, True, bias, None, groups, top, best, 2.0).run().check()
 
 
+@pytest.mark.parametrize("E,top,k", [(256, 1, 16), (256, 2, 8), (256, 3, 6), (256, 5, 8), (256, 7, 16), (160, 3, 8), (160, 4, 1), (192, 4, 16), (192, 6, 8), (224, 2, 9)])
+@pytest.mark.parametrize("sigmoid,biased,best,name", [(True, True, 2, "f32"), (False, False, 2, "f32"), (True, False, 1, "bf16"), (False, True, 1, "bf16")])
+def test_groups_of_32(E, top, k, sigmoid, biased, best, name):
+    rng = np.random.default_rng([E, top, k])
+    x = _logits(rng, 90, E, name)
+    x[20:40, 3::16] += 4.0                                              # most of the largest 16 apart
+    x[40:60][torch.from_numpy(rng.random((20, E)) < 0.8).cuda()] = float("-inf")
+    x[60:70, :32 * (E // 32 - 1)] = float("-inf")                       # one group left
+    x[70, :] = float("-inf")
+    x[71, 5] = 1.0
+    x[72:80] = torch.from_numpy(rng.integers(0, 3, (8, E)) * 0.5).to(x)  # ties
+    bias = torch.from_numpy(rng.normal(0, 0.1, E)).float().cuda() if biased else None
+    Call(x, k, 0, sigmoid, True, bias, None, E // 32, top, best, 2.0).run().check()
+
+
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("groups,top,best", [(1, 1, 1), (8, 3, 2), (8, 3, 1)])
 @pytest.mark.parametrize("E", [32, 64, 256])

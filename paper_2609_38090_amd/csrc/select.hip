@@ -311,7 +311,7 @@ __device__ __forceinline__ float fixed_step(float bias_max) { return 16777210.f 
 __device__ __forceinline__ float fixed_from(float bias_max) { return fmaf(bias_max, fixed_step(bias_max), 2.f); }
 
 __device__ __forceinline__ uint32_t order_key(float f) {
-  const uint32_t u = __float_as_uint(f);
+  const uint32_t u = __float_as_uint(f + 0.f);  // (-0 is 0)
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 

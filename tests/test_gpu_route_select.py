@@ -127,6 +127,18 @@ def test_ties_go_to_the_lower_index(sigmoid, biased):
         Call(x.bfloat16(), 6, 0, sigmoid, False, bias, None, groups, top, best).run().check()
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("E,groups,top,best", [(8, 1, 1, 1), (100, 1, 1, 1), (64, 4, 2, 1), (96, 12, 3, 1), (256, 8, 4, 2)])
+def test_zeros_of_either_sign_tie(E, groups, top, best, name):
+    rng = np.random.default_rng(E)
+    x = torch.from_numpy(np.where(rng.random((60, E)) < 0.5, -0.0, 0.0)).to(dt(name)).cuda()
+    x[20:40][torch.from_numpy(rng.random((20, E)) < 0.5).cuda()] = -1.0
+    x[40:][torch.from_numpy(rng.random((20, E)) < 0.1).cuda()] = 2.0 ** -20
+    for sigmoid in (False, True):
+        for k in (1, 3, 6):
+            Call(x, k, 0, sigmoid, True, None, None, groups, top, best).run().check()
+
+
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("biased", [False, True])
 @pytest.mark.parametrize("groups,top,best", [(1, 1, 1), (4, 2, 2)])

@@ -175,7 +175,7 @@ __device__ __forceinline__ Pick select_wide(const SelectParams& p, int row, Sele
       if (e >= p.E) continue;
       const double ex = scr.wide.group[e];
       const double c = (p.sigmoid ? 1.0 : ex) / (p.sigmoid ? 1.0 + ex : total) + (double)b[i];
-      if (scr.wide.c[e] != none) scr.wide.c[e] = c;
+      if (scr.wide.c[e] != none) scr.wide.c[e] = c == c ? c : none;  // (NaN biases: below, a maximum is one of c)
     }
   }
   wave_sync();

@@ -194,6 +194,28 @@ def test_special_logits(sigmoid, biased):
         assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("groups,top,best", [(1, 1, 1), (8, 3, 2)])
+@pytest.mark.parametrize("E,of", [(256, 256), (256, 250), (200, 200), (64, 64), (16, 3)])
+def test_biases_that_are_no_numbers(sigmoid, groups, top, best, E, of):
+    """Selections from biases that a program let become NaN or infinite: some experts, each once, and their pairs."""
+    rng = np.random.default_rng([E, of])
+    x = _logits(rng, 70, E, "f32")
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bias = torch.from_numpy(rng.normal(0, 0.1, E)).float().cuda()
+        bias[torch.from_numpy(rng.permutation(E)[:of]).cuda()] = value
+        c = Call(x, 3, 0, sigmoid, True, bias, None, groups, top, best).run()
+        torch.cuda.synchronize()
+        i, w, counts, offsets, order, pos = c.outputs()
+        assert all(g.intact() for g in (c.X, c.idx, c.w, c.counts, c.offsets, c.order, c.pos, c.ws))
+        assert ((i >= -1) & (i < E)).all()
+        for t in range(70):
+            got = i[t][i[t] >= 0]
+            assert len(set(got)) == len(got)
+        for got, want in zip((counts, offsets, order, pos), pairs(i.astype(np.int64), None, E, 0)):
+            assert np.array_equal(got, want)
+
+
 @pytest.mark.parametrize("outs", ["", "w", "c", "o", "f", "p", "wop"])
 @pytest.mark.parametrize("T", [20, 500])
 def test_optional_outputs(outs, T):

@@ -3,9 +3,9 @@
 //   dx = dsum + r (g - n mean(n g)),  g = dy w,  n = h r;   dweight = sum over rows of dy n.
 // Memory bound: a row is read once into registers, eight consecutive columns to a lane
 // (16 bytes of bf16; 16 lanes hold a block of 128 that shares a scale), its sums are taken
-// across the lanes, and every output is written from there.  A row is shared by as many waves
-// as hold it at eight values a lane (sixteen above 8192 columns), a workgroup of its own from two
-// waves on; rows of more than 16384 are read twice.  The gradient of the weight is summed in
+// across the lanes, and every output is written from there.  A row is shared by as many lanes
+// as hold it at eight values each (sixteen above 8192 columns): 16, 32 or a wave, a workgroup of its own from
+// two waves on; rows of more than 16384 are read twice.  The gradient of the weight is summed in
 // registers over the rows that a workgroup walks, then over workgroups in order.  4096 x 4096 bf16 with
 // residual, y and e4m3 30 us (151 MB, 5.0 TB/s; a copy of 1 GB reaches 5.2); the gradient of 16384 x 4096
 // 100 us (537 MB, 5.4 TB/s).
@@ -23,9 +23,11 @@ constexpr uint32_t kMaxGrid = 1u << 21;  // workgroups of a launch: fewer than 2
 // 2^24 squares of fp32's largest values fits then).
 constexpr float kDown = 8.271806125530276748714e-25f;
 
-// Workgroups of one row have 128 to 1024 threads, those of four rows (a wave each) 256: waves of one
-// row meet at barriers, which rows of one workgroup could not do apart.
+// Workgroups of one row have 128 to 1024 threads, those of several rows (16, 32 or 64 lanes each) 256: waves
+// of one row meet at barriers, which rows of one workgroup could not do apart.
+int row_lanes(int cols) { return cols <= 128 ? 16 : cols <= 256 ? 32 : cols <= 512 ? 64 : 0; }  // 0: the workgroup
 int row_threads(int cols) {
+  if (cols <= 512) return 256;
   const int n = cols <= 8192 ? cols : (cols + 1) / 2;
   return (n + 511) / 512 * 64;
 }
@@ -33,7 +35,7 @@ int row_threads(int cols) {
 // Workgroups that sum the gradient of the weight: as many to each CU, of no more than 1024 threads together
 // (17879 x 2787 bf16 in 682, which some CUs had two and some three of, 126 us, in 512 90; 6000 x 7168
 // in 292 102 us, in 256 70; with up to 1280 threads to a CU 117 and 70).
-int parts_of(int threads) { return threads == 64 ? 1024 : 256 * (1024 / threads); }
+int parts_of(int threads) { return 256 * (1024 / threads); }
 
 struct NormParams {
   const void* x;
@@ -69,12 +71,12 @@ __device__ __forceinline__ void load8(const void* p, size_t row_at, bool f32, in
   else load_cols((const uint16_t*)p + row_at, c, cols, v);
 }
 
-// Sum over the threads of a row, in all of them: a wave, or (ROW) the workgroup, whose waves meet in
+// Sum over the threads of a row, in all of them: LANES of them, or (0) the workgroup, whose waves meet in
 // LDS.  `turn` alternates between two sets of it, so that one barrier a sum suffices.
-template <bool ROW>
+template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float (*part)[16], int turn) {
-  v = lanes_reduce<64, AddOp>(v);
-  if constexpr (ROW) {
+  v = lanes_reduce<LANES ? LANES : 64, AddOp>(v);
+  if constexpr (LANES == 0) {
     if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.f;
@@ -83,11 +85,11 @@ __device__ __forceinline__ float row_sum(float v, float (*part)[16], int turn) {
   return v;
 }
 // Two sums at once.
-template <bool ROW>
+template <int LANES>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*part)[16], int turn) {
-  a = lanes_reduce<64, AddOp>(a);
-  b = lanes_reduce<64, AddOp>(b);
-  if constexpr (ROW) {
+  a = lanes_reduce<LANES ? LANES : 64, AddOp>(a);
+  b = lanes_reduce<LANES ? LANES : 64, AddOp>(b);
+  if constexpr (LANES == 0) {
     if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = float2{a, b};
     __syncthreads();
     a = b = 0.f;
@@ -98,14 +100,14 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*part)[16],
   }
 }
 
-template <bool ROW, int NV, typename T, typename W>
-__global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_kernel(NormParams p) {
-  constexpr int kRows = ROW ? 1 : 4;
+template <int LANES, int NV, typename T, typename W>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_kernel(NormParams p) {
+  constexpr int kRows = LANES ? 256 / LANES : 1;
   __shared__ float part[4][16];
-  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63;
+  const int L = LANES ? LANES : blockDim.x, l = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, in_block = LANES ? threadIdx.x / LANES : 0;
   const float inv_cols = 1.f / (float)p.cols;
   int turn = 0;
-  for (size_t r = (size_t)blockIdx.x * kRows + (ROW ? 0 : threadIdx.x >> 6); r < (size_t)p.rows; r += (size_t)gridDim.x * kRows) {
+  for (size_t r = (size_t)blockIdx.x * kRows + in_block; r < (size_t)p.rows; r += (size_t)gridDim.x * kRows) {
     const T* x = (const T*)p.x + r * p.ldx;
     float v[NV][8], ss = 0.f;
     Raw8<T> raw[NV], res[NV];
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_kernel(NormParams p)
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
-    ss = row_sum<ROW>(ss, part, turn & 1);
+    ss = row_sum<LANES>(ss, part, turn & 1);
     float rs;
     if (ss <= 3.4028234e38f || ss != ss) {
       rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_cols, p.eps));
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_kernel(NormParams p)
           v[i][j] *= kDown;
           ss = fmaf(v[i][j], v[i][j], ss);
         }
-      ss = row_sum<ROW>(ss, part, 2 + (turn & 1));
+      ss = row_sum<LANES>(ss, part, 2 + (turn & 1));
       rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_cols, p.eps * kDown * kDown));
     }
     ++turn;
@@ -206,8 +208,8 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormParams p) {
         down = fmaf(d, d, down);
       }
     }
-    ss = row_sum<true>(ss, part, turn & 1);
-    down = row_sum<true>(down, part, 2 + (turn & 1));
+    ss = row_sum<0>(ss, part, turn & 1);
+    down = row_sum<0>(down, part, 2 + (turn & 1));
     ++turn;
     const bool far = ss > 3.4028234e38f;
     const float rs = __builtin_amdgcn_rsqf(far ? fmaf(down, inv_cols, p.eps * kDown * kDown) : fmaf(ss, inv_cols, p.eps)), pre = far ? kDown : 1.f;
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormParams p) {
 struct RowGrad {
   float pre, rs, inner;  // n = h pre rs
 };
-template <bool ROW, int NV, typename T, typename D, typename W>
+template <int LANES, int NV, typename T, typename D, typename W>
 __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<D> (&d)[NV], W weights, float eps, float inv_cols,
                                              float2 (*part)[16], int turn) {
   RowGrad o;
@@ -251,7 +253,7 @@ __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<
         hg = fmaf(v, d[i][j] * w[j], hg);
       }
     }
-    row_sum2<ROW>(ss, hg, part, set);
+    row_sum2<LANES>(ss, hg, part, set);
   };
   sums(turn & 1);
   if (ss > 3.4028234e38f) {  // (the whole row's threads)
@@ -265,11 +267,11 @@ __device__ __forceinline__ RowGrad grad_sums(const Raw8<T> (&h)[NV], const Raw8<
   return o;
 }
 
-template <bool ROW, int NV, bool DW, typename T, typename D>
-__global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_grad_kernel(NormGradParams p) {
-  constexpr int kRows = ROW ? 1 : 4;
+template <int LANES, int NV, bool DW, typename T, typename D>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(NormGradParams p) {
+  constexpr int kRows = LANES ? 256 / LANES : 1;
   __shared__ float2 part[4][16];
-  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63;
+  const int L = LANES ? LANES : blockDim.x, l = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, in_block = LANES ? threadIdx.x / LANES : 0;
   const float inv_cols = 1.f / (float)p.cols;
   float held_w[8], acc[NV][8];
   load8(p.w, 0, p.w_f32, l * 8, p.cols, held_w);
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_grad_kernel(NormGrad
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
   int turn = 0;
-  for (size_t r = (size_t)blockIdx.x * kRows + (ROW ? 0 : threadIdx.x >> 6); r < (size_t)p.rows; r += (size_t)gridDim.x * kRows, ++turn) {
+  for (size_t r = (size_t)blockIdx.x * kRows + in_block; r < (size_t)p.rows; r += (size_t)gridDim.x * kRows, ++turn) {
     Raw8<T> h[NV], s[NV];
     Raw8<D> d[NV];
 #pragma unroll
@@ -311,7 +313,7 @@ __global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_grad_kernel(NormGrad
       settle(d[i], c, p.cols);
       settle(s[i], c, p.cols);
     }
-    const RowGrad o = grad_sums<ROW, NV>(h, d, weights, p.eps, inv_cols, part, turn);
+    const RowGrad o = grad_sums<LANES, NV>(h, d, weights, p.eps, inv_cols, part, turn);
     const float out_scale = o.rs * o.pre;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -328,13 +330,13 @@ __global__ __launch_bounds__(ROW ? 1024 : 256) void rmsnorm_grad_kernel(NormGrad
   }
   if constexpr (DW) {
     float* out = p.partial + (size_t)blockIdx.x * p.cols;
-    if constexpr (ROW) {
+    if constexpr (LANES == 0) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_cols(out, (i * L + l) * 8, p.cols, acc[i]);
     } else {
-      __shared__ float rows_acc[kRows][512];
+      __shared__ float rows_acc[kRows][LANES * 8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) rows_acc[threadIdx.x >> 6][l * 8 + j] = acc[0][j];
+      for (int j = 0; j < 8; ++j) rows_acc[in_block][l * 8 + j] = acc[0][j];
       __syncthreads();
       for (int c = threadIdx.x; c < p.cols; c += 256) {
         float s = 0.f;
@@ -376,10 +378,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradParams 
       }
     }
     const int b = (turn & 1) * 4;
-    ss = row_sum<true>(ss, part, b);
-    hg = row_sum<true>(hg, part, b + 1);
-    ds = row_sum<true>(ds, part, b + 2);
-    dg = row_sum<true>(dg, part, b + 3);
+    ss = row_sum<0>(ss, part, b);
+    hg = row_sum<0>(hg, part, b + 1);
+    ds = row_sum<0>(ds, part, b + 2);
+    dg = row_sum<0>(dg, part, b + 3);
     const bool far = ss > 3.4028234e38f;
     const float rs = __builtin_amdgcn_rsqf(far ? fmaf(ds, inv_cols, p.eps * kDown * kDown) : fmaf(ss, inv_cols, p.eps)), pre = far ? kDown : 1.f;
     const float inner = rs * (far ? dg : hg) * inv_cols;
@@ -434,47 +436,55 @@ __global__ __launch_bounds__(1024) void rmsnorm_weight_kernel(const float* __res
   }
 }
 
-uint32_t row_grid(int rows, int rows_per_block, uint32_t most) {
-  const uint32_t n = ((uint32_t)rows + rows_per_block - 1) / rows_per_block;
+int rows_per_block(int cols) { return row_lanes(cols) ? 256 / row_lanes(cols) : 1; }
+
+uint32_t row_grid(int rows, int per_block, uint32_t most) {
+  const uint32_t n = ((uint32_t)rows + per_block - 1) / per_block;
   return n < most ? n : most;
 }
 
 template <typename T, typename W>
 void launch_norm_of(const NormParams& p, hipStream_t st) {
-  const int threads = row_threads(p.cols);
+  const int lanes = row_lanes(p.cols);
   if (p.cols > kRegCols)
     launch_timed("rmsnorm_long", rmsnorm_long_kernel<T>, dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(1024), 0, st, p);
-  else if (threads == 64)
-    launch_timed("rmsnorm", rmsnorm_kernel<false, 1, T, W>, dim3(row_grid(p.rows, 4, kMaxGrid)), dim3(256), 0, st, p);
   else
-    launch_timed("rmsnorm", p.cols <= 8192 ? rmsnorm_kernel<true, 1, T, W> : rmsnorm_kernel<true, 2, T, W>,
-                 dim3(row_grid(p.rows, 1, kMaxGrid)), dim3(threads), 0, st, p);
+    launch_timed("rmsnorm",
+                 lanes == 16   ? rmsnorm_kernel<16, 1, T, W>
+                 : lanes == 32 ? rmsnorm_kernel<32, 1, T, W>
+                 : lanes == 64 ? rmsnorm_kernel<64, 1, T, W>
+                 : p.cols <= 8192 ? rmsnorm_kernel<0, 1, T, W>
+                                  : rmsnorm_kernel<0, 2, T, W>,
+                 dim3(row_grid(p.rows, rows_per_block(p.cols), kMaxGrid)), dim3(row_threads(p.cols)), 0, st, p);
 }
 
 // Parts of the weight's gradient: two rows to a workgroup where there are not many for each (1201 x
 // 2001 fp32: 12.7 us so, 14.2 with one, whose parts are as many bytes as the rows; 13.2 with three or four).
 constexpr int kPartRows = 2;
-int parts_for(int rows, int rows_per_block, int most) {
-  const int few = (rows + rows_per_block - 1) / rows_per_block;  // one row after another
+constexpr int kOneParts = 3;
+int parts_for(int rows, int per_block, int most) {
+  const int few = (int)(((uint32_t)rows + per_block - 1) / per_block);  // one row after another
+  if (few <= kOneParts) return min(few, 1);
   return min(most, max((few + kPartRows - 1) / kPartRows, min(few, 256)));
 }
 
 int grad_parts(int rows, int cols) {
   if (cols > kRegCols) return rows < kLongParts ? rows : kLongParts;
-  const int threads = row_threads(cols);
-  return parts_for(rows, threads == 64 ? 4 : 1, parts_of(threads));
+  return parts_for(rows, rows_per_block(cols), parts_of(row_threads(cols)));
 }
 
 // Launches the rows' pass; returns the parts of the weight's gradient that it leaves.
 template <bool DW, typename T, typename D>
 int launch_grad(const NormGradParams& p, hipStream_t st) {
-  const int threads = row_threads(p.cols);
-  const uint32_t grid = DW ? (uint32_t)grad_parts(p.rows, p.cols) : row_grid(p.rows, threads == 64 ? 4 : 1, kMaxGrid);
+  const int lanes = row_lanes(p.cols);
+  const uint32_t grid = DW ? (uint32_t)grad_parts(p.rows, p.cols) : row_grid(p.rows, rows_per_block(p.cols), kMaxGrid);
   launch_timed("rmsnorm_grad",
-               threads == 64      ? rmsnorm_grad_kernel<false, 1, DW, T, D>
-               : p.cols <= 8192 ? rmsnorm_grad_kernel<true, 1, DW, T, D>
-                                : rmsnorm_grad_kernel<true, 2, DW, T, D>,
-               dim3(grid), dim3(threads == 64 ? 256 : threads), 0, st, p);
+               lanes == 16   ? rmsnorm_grad_kernel<16, 1, DW, T, D>
+               : lanes == 32 ? rmsnorm_grad_kernel<32, 1, DW, T, D>
+               : lanes == 64 ? rmsnorm_grad_kernel<64, 1, DW, T, D>
+               : p.cols <= 8192 ? rmsnorm_grad_kernel<0, 1, DW, T, D>
+                                : rmsnorm_grad_kernel<0, 2, DW, T, D>,
+               dim3(grid), dim3(row_threads(p.cols)), 0, st, p);
   return (int)grid;
 }
 
@@ -549,10 +559,11 @@ hipError_t launch_rmsnorm_grad(const mira_rmsnorm_grad_args& a, hipStream_t st) 
     const bool is_long = a.cols > kRegCols;
     p.rstd = is_long ? (float*)a.workspace : nullptr;
     p.partial = (float*)((char*)a.workspace + (is_long ? align_up((size_t)a.rows * 4, 256) : 0));
+    if (grad_parts(a.rows, a.cols) == 1) p.partial = a.dweight;
   }
   int parts = 0;
   if (a.rows > 0) parts = a.x_dtype == MIRA_F32 ? launch_grad_of<float>(p, dw, st) : launch_grad_of<uint16_t>(p, dw, st);
-  if (dw)
+  if (dw && parts != 1)
     launch_timed("rmsnorm_weight", rmsnorm_weight_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, st, (const float*)p.partial,
                  parts, a.cols, a.dweight);
   return hipGetLastError();

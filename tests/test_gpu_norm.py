@@ -207,3 +207,42 @@ def test_far_rows():
     assert torch.equal(out[:, 512:512 + cols], dx)
     del far, out
     torch.cuda.empty_cache()
+
+
+# rows of 16 and 32 lanes and of a wave, at and beside their ends; rows that one workgroup takes in turn
+SHORT = [(r, c) for c in (15, 16, 127, 128, 129, 256, 257, 511) for r in (1, 16, 17, 49, 700)]
+CHAIN.update({c: 30 for _, c in SHORT})
+
+
+@pytest.mark.parametrize("rows,cols", SHORT + [(40000, 128), (3, 3000), (4, 3000), (2, 9000)])
+@pytest.mark.parametrize("x,w,y,extra,pad,shift", [("bf16", "bf16", "bf16", True, 0, 0), ("f32", "bf16", "f32", False, 3, 1)])
+def test_short_rows(rows, cols, x, w, y, extra, pad, shift):
+    if (rows, cols) in SHORT:
+        test_forward(rows, cols, x, w, y, extra, pad, shift)
+    test_gradient(rows, cols, x, w, y, extra, pad, shift)
+
+
+@pytest.mark.parametrize("cols", [10, 128, 200, 400])
+def test_far_and_near_rows_side_by_side(cols):
+    """Rows whose squares pass fp32's range beside others, of NaN and infinities too."""
+    rng = np.random.default_rng(cols)
+    rows = 70
+    x = _rows(rng, rows, cols)
+    x[1::3] *= 1e30
+    bad = list(range(2, rows, 9))
+    x[bad, 0] = torch.tensor([float("nan"), float("inf")], device="cuda").repeat(rows)[:len(bad)]
+    w = torch.ones(cols, device="cuda")
+    y, dx, dy = torch.empty_like(x), torch.empty_like(x), torch.from_numpy(rng.normal(0, 1, (rows, cols))).float().cuda()
+    mira.mira_rmsnorm(mira.RmsNormArgs(x=x, weight=w, x_dtype=0, w_dtype=0, y_dtype=0, rows=rows, cols=cols, eps=EPS, y=y))
+    mira.mira_rmsnorm_grad(mira.RmsNormGradArgs(dy=dy, h=x, weight=w, x_dtype=0, w_dtype=0, y_dtype=0, rows=rows, cols=cols, eps=EPS, dx=dx))
+    fine = [r for r in range(rows) if r not in bad]
+    dw, nb = torch.empty(cols, device="cuda"), mira.mira_rmsnorm_grad_workspace_bytes(len(fine), cols)
+    mira.mira_rmsnorm_grad(mira.RmsNormGradArgs(dy=dy[fine], h=x[fine], weight=w, x_dtype=0, w_dtype=0, y_dtype=0, rows=len(fine), cols=cols, eps=EPS,
+                                                dweight=dw, workspace=torch.empty(nb, dtype=torch.uint8, device="cuda"), workspace_bytes=nb))
+    torch.cuda.synchronize()
+    want, _ = norm(f64(x)[fine], 1.0, EPS)
+    assert (np.abs(f64(y)[fine] - want) <= 30 * U32 * np.abs(want)).all()
+    gx, gw, terms, wmag = norm_grad(f64(dy)[fine], None, f64(x)[fine], np.ones(cols), EPS)
+    assert (np.abs(f64(dx)[fine] - gx) <= 3 * 48 * U32 * terms + 1e-37).all()
+    assert (np.abs(f64(dw) - gw) <= (48 + 70 + 32) * U32 * wmag).all()
+    assert np.isnan(f64(y)[bad, 0]).all() and np.isnan(f64(y)[bad[0]]).all() and (f64(y)[bad[1], 1:] == 0).all()

@@ -73,19 +73,19 @@ __global__ __launch_bounds__(256) void swiglu_grad_kernel(SwigluGradParams p, in
   }
 }
 
-// A row's gradient in e4m3 for any number of columns up to kRowCols: a wave (ROW false, up to 512
-// columns, four rows to a workgroup) or a workgroup to a row.
+// A row's gradient in e4m3 for any number of columns up to kRowCols: 16, 32 or 64 lanes (LANES, up to 512
+// columns, as many rows to a workgroup as there are) or a workgroup (0) to a row.
 constexpr int kRowCols = 16384;
 typedef int v2i_bytes __attribute__((ext_vector_type(2), aligned(1)));  // (global stores take any alignment)
 
-template <bool ROW, int NV, typename T, typename D>
-__global__ __launch_bounds__(ROW ? 1024 : 256) void swiglu_grad_row_kernel(SwigluGradParams p) {
-  constexpr int kRows = ROW ? 1 : 4, kBlocks = ROW ? 2 * kRowCols / 128 : 8;
+template <int LANES, int NV, typename T, typename D>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void swiglu_grad_row_kernel(SwigluGradParams p) {
+  constexpr int kRows = LANES ? 256 / LANES : 1, kBlocks = LANES ? LANES / 8 : 2 * kRowCols / 128;
   __shared__ uint32_t largest[kRows][kBlocks];  // of each block of the result, as the bits of a magnitude
-  const int L = ROW ? blockDim.x : 64, l = ROW ? threadIdx.x : threadIdx.x & 63, w = ROW ? 0 : threadIdx.x >> 6;
+  const int L = LANES ? LANES : blockDim.x, l = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, w = LANES ? threadIdx.x / LANES : 0;
   const int blocks = (2 * p.cols + 127) / 128;
   auto meet = [] {
-    if constexpr (ROW) {
+    if constexpr (LANES == 0) {
       __syncthreads();
     } else {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -207,13 +207,16 @@ template <typename T, typename D>
 void launch_of(const SwigluGradParams& p, hipStream_t st) {
   const bool step = !p.q || p.cols % 128 == 0;
   if (!step && p.cols <= kRowCols) {
-    const int lanes = p.cols <= 8192 ? p.cols : (p.cols + 1) / 2, threads = (lanes + 511) / 512 * 64;
-    const uint32_t blocks = threads == 64 ? ((uint32_t)p.rows + 3) / 4 : (uint32_t)p.rows;
+    const int lanes = p.cols <= 128 ? 16 : p.cols <= 256 ? 32 : p.cols <= 512 ? 64 : 0, rows = lanes ? 256 / lanes : 1;
+    const int most = p.cols <= 8192 ? p.cols : (p.cols + 1) / 2, threads = lanes ? 256 : (most + 511) / 512 * 64;
+    const uint32_t blocks = ((uint32_t)p.rows + rows - 1) / rows;
     launch_timed("swiglu_grad_row",
-                 threads == 64      ? swiglu_grad_row_kernel<false, 1, T, D>
-                 : p.cols <= 8192 ? swiglu_grad_row_kernel<true, 1, T, D>
-                                  : swiglu_grad_row_kernel<true, 2, T, D>,
-                 dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(threads == 64 ? 256 : threads), 0, st, p);
+                 lanes == 16   ? swiglu_grad_row_kernel<16, 1, T, D>
+                 : lanes == 32 ? swiglu_grad_row_kernel<32, 1, T, D>
+                 : lanes == 64 ? swiglu_grad_row_kernel<64, 1, T, D>
+                 : p.cols <= 8192 ? swiglu_grad_row_kernel<0, 1, T, D>
+                                  : swiglu_grad_row_kernel<0, 2, T, D>,
+                 dim3(blocks < kMaxGrid ? blocks : kMaxGrid), dim3(threads), 0, st, p);
     return;
   }
   const int nb = (int)(((size_t)p.cols * (step ? 1 : 2) + 127) / 128);

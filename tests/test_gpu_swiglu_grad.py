@@ -86,3 +86,11 @@ def test_far_rows():
     assert torch.equal(far[:, 1024:1024 + 2 * cols], out[0][0]) and torch.equal(out[0][1], out[1][1]) and torch.equal(out[0][2], out[1][2])
     del far
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("cols", [1, 8, 63, 64, 65, 100, 127, 129, 136, 190, 192, 255, 257, 500])
+@pytest.mark.parametrize("rows", [1, 15, 17, 333])
+def test_short_rows(rows, cols):
+    """Rows of 16 and 32 lanes and of a wave, several to a workgroup."""
+    test_gradient(rows, cols, "bf16", "f32", "dxq", 3, 1)
+    test_gradient(rows, cols, "f32", "bf16", "q", 0, 0)

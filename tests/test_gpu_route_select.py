@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_38090_amd as mira
-from layer_reference import U32, Guarded, code, dt, f64, pairs, scores, select, select_grad, unit
+from layer_reference import TINY, U32, Guarded, code, dt, f64, pairs, scores, select, select_grad, unit
 
 pytestmark = pytest.mark.gpu
 # s: exp 4 half steps, 10 additions, the reciprocal 2, products; renormalised: 16 additions, a quotient, two products
@@ -45,7 +45,7 @@ class Call:
         T, P = self.T, self.T * (self.k + self.S)
         return [t.cpu().numpy() for t in (self.idx.v[:T], self.w.v[:T], self.counts.v[0], self.offsets.v[0], self.order.v[0, :P], self.pos.v[0, :P])]
 
-    def check(self, rows=None):
+    def check(self, rows=None, extra=0.0):
         torch.cuda.synchronize()
         guards = (self.X, self.idx, self.w, self.counts, self.offsets, self.order, self.pos, self.ws)
         assert all(g.intact() for g in guards)
@@ -54,7 +54,7 @@ class Call:
         idx, weight = select(x, self.k, bias=None if self.bias is None else f64(self.bias), mask=mask, **self.opt)
         i, w, counts, offsets, order, pos = self.outputs()
         assert np.array_equal(i, idx)
-        assert (np.abs(w - weight) <= STEPS * U32 * np.abs(weight) + 2.0 ** -120).all()
+        assert (np.abs(w - weight) <= STEPS * U32 * np.abs(weight) + 2.0 ** -120 + extra).all()
         for got, want in zip((counts, offsets, order, pos), pairs(idx, mask, self.E, self.S)):
             assert np.array_equal(got, want)
         return self
@@ -423,3 +423,72 @@ def test_many_tokens(T, E, k):
     assert torch.equal(c.counts.v[0].long(), torch.bincount(group, minlength=E + 2)[:E + 1])
     assert torch.equal(c.offsets.v[0, 1:].long(), c.counts.v[0].long().cumsum(0))
     assert all(b.intact() for b in (c.X, c.idx, c.w, c.counts, c.offsets, c.order, c.pos, c.ws))
+
+
+def _few_experts(E, k, name, seed):
+    """Rows with all that a row may have: usual ones, ties, experts of -inf, rows of them, neighbours that fp32 does not tell apart, NaN, infinities."""
+    rng = np.random.default_rng([E, k, seed])
+    T = 8800
+    x = _logits(rng, T, E, name)
+    x[1000:2000] = torch.from_numpy(rng.integers(-1, 2, (1000, E)) * 0.5).to(x)
+    x[2000:2400][torch.from_numpy(rng.random((400, E)) < 0.5).cuda()] = float("-inf")
+    x[2400:2410] = float("-inf")
+    x[2500:2600] = torch.from_numpy(rng.normal(0, 1, (100, 1)) + rng.normal(0, 1e-6, (100, E))).to(x)
+    x[2600:2700] *= 40
+    x[2700:2800] = torch.where(torch.from_numpy(rng.random((100, E)) < 0.5).cuda(), -0.0, 0.0).to(x)
+    return rng, x
+
+
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 2), (3, 1), (7, 4), (8, 2), (8, 4), (9, 3), (15, 4), (16, 1), (16, 4)])
+@pytest.mark.parametrize("sigmoid,renorm,biased,name,pad,shift", [(False, True, False, "f32", 0, 0), (True, True, True, "bf16", 3, 1),
+                                                                  (False, False, True, "f32", 1, 1), (True, False, False, "bf16", 0, 0)])
+def test_long_batches_of_few_experts(E, k, sigmoid, renorm, biased, name, pad, shift):
+    rng, x = _few_experts(E, k, name, 0)
+    T = len(x)
+    bias = torch.from_numpy(rng.normal(0, 0.1, E)).float().cuda() if biased else None
+    mask = torch.from_numpy((rng.random(T) < 0.9).astype(np.uint8)).cuda() if shift else None
+    c = Call(x, k, 2 if E < 9 else 0, sigmoid, renorm, bias, mask, scale=2.5, pad=pad, shift=shift).run()
+    # fp32 holds v - max to half a step, which is that much of exp(v - max) relatively, and no score below 2^-126; both count
+    # in rows of logits this far apart (half a step of -65 is 64 half steps of 1)
+    xs, i = f64(c.X.v), c.outputs()[0]
+    top, of = xs.max(1, keepdims=True), np.take_along_axis(xs, np.maximum(i, 0), 1)
+    s = np.where(i >= 0, np.take_along_axis(scores(xs, sigmoid), np.maximum(i, 0), 1), 0.0)
+    share = 2.5 / (s.sum(1, keepdims=True) + TINY) if renorm else 2.5
+    with np.errstate(invalid="ignore"):
+        apart = np.where((i >= 0) & ~np.isneginf(top), top - of, 0.0)
+    c.check(extra=(0.0 if sigmoid else U32 * apart * s * share) + 2.0 ** -126 * share)
+    # a batch that is not long: the same bits
+    d = Call(x[:4400], k, 0, sigmoid, renorm, bias, None if mask is None else mask[:4400], scale=2.5, pad=pad, shift=shift).run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.idx.v[:4400], d.idx.v) and torch.equal(c.w.v[:4400], d.w.v)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("biased", [False, True])
+def test_long_batches_special_logits(sigmoid, biased):
+    """NaN and infinities in a long batch of few experts: the selection and weights of a shorter one."""
+    rng, x = _few_experts(8, 3, "f32", 1)
+    x[torch.from_numpy(rng.random(tuple(x.shape)) < 0.02).cuda()] = float("nan")
+    x[torch.from_numpy(rng.random(tuple(x.shape)) < 0.02).cuda()] = float("inf")
+    bias = torch.from_numpy(rng.normal(0, 0.1, 8)).float().cuda() if biased else None
+    c, d = Call(x, 3, 0, sigmoid, True, bias).run(), Call(x[:4400], 3, 0, sigmoid, True, bias).run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.idx.v[:4400], d.idx.v) and torch.equal(c.w.v[:4400].view(torch.int32), d.w.v.view(torch.int32))
+    i = c.outputs()[0]
+    xs = x.cpu().numpy()
+    for t in range(len(xs)):
+        got = i[t][i[t] >= 0]
+        assert len(set(got)) == len(got) and not np.isnan(xs[t, got]).any()
+    for got, want in zip(c.outputs()[2:], pairs(i.astype(np.int64), None, 8, 0)):
+        assert np.array_equal(got, want)
+    assert all(b.intact() for b in (c.X, c.idx, c.w, c.counts, c.offsets, c.order, c.pos, c.ws))
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_long_batches_scores_that_fp32_does_not_tell_apart(sigmoid):
+    rng = np.random.default_rng(14)
+    row = np.float32(rng.normal(0, 1.5, 16))
+    bias = torch.from_numpy((0.75 - scores(row[None].astype(np.float64), sigmoid)[0]).astype(np.float32)).cuda()
+    x = torch.from_numpy(np.repeat(row[None], 8300, 0)).cuda()
+    x[1::2] += torch.from_numpy(rng.normal(0, 1e-6, (4150, 16)).astype(np.float32)).cuda()
+    Call(x, 4, 0, sigmoid, True, bias).run().check()

@@ -14,9 +14,9 @@
 // chunk, so a pair's rank in its expert's list is a count of bits: no order of atomics
 // decides anything.  Counts of all chunks are added up by a launch in between.
 //
-// 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 68 us (151 MB, for which a copy takes
+// 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 67 us (151 MB, for which a copy takes
 // 29): 55 for the selection, bound by instructions (some 610 to four rows, the vector units busy 57 %
-// of the time), 6 for the counts, 10 for the order.
+// of the time), 6 for the counts, 9 for the order.
 #include "fp8_dev.h"
 
 namespace mira {
@@ -715,6 +715,7 @@ __device__ __forceinline__ int scan256(int v, int* wave_sums, int* total) {
   return before + s - v;
 }
 
+constexpr int kHeld = 2;  // pairs that a thread keeps from marking them to placing them
 struct PlaceLds {
   uint32_t bits[MIRA_MAX_EXPERTS][kWords];
   int base[MIRA_MAX_EXPERTS];
@@ -722,23 +723,11 @@ struct PlaceLds {
 };
 
 // Order and positions of a chunk's pairs, by the whole workgroup.  sel(i) is the expert
-// of pair i of the chunk, kept(t) whether its token t has shared experts; total(g), called by
-// thread g, the pairs of group g in the call, before(g) those in earlier chunks.
-template <int THREADS, typename Sel, typename Kept, typename Total, typename Before>
-__device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, int chunk, Sel sel, Kept kept, Total total, Before before) {
+// of pair i of the chunk, kept(t) whether its token t has shared experts; thread g's `of` has the pairs of
+// group g in earlier chunks (x) and in the call (y).
+template <int THREADS, typename Sel, typename Kept>
+__device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, int chunk, Sel sel, Kept kept, int2 of) {
   const int t = threadIdx.x, G = p.E + p.S, t0 = chunk * p.chunk, n = min(p.chunk, p.T - t0);
-  for (int i = t; i < G * kWords; i += THREADS) (&L.bits[0][0])[i] = 0;
-  int all;
-  const int mine = t < G ? total(t) : 0;
-  const int off = scan256(mine, L.wave_sums, &all);  // (its barrier: the bits are zero)
-  if (t < G) {
-    L.base[t] = off + before(t);
-    if (chunk == 0) {
-      if (p.counts_out) p.counts_out[t] = mine;
-      if (p.offsets_out) p.offsets_out[t] = off;
-    }
-  }
-  if (chunk == 0 && t == 0 && p.offsets_out) p.offsets_out[G] = all;
   const int routed = n * p.k, pairs = routed + n * p.S;
   auto pair_of = [&](int i, int* tok) {  // the group of pair i of the chunk, or -1
     if (i < routed) {
@@ -749,16 +738,37 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
     *tok = i - routed - s * n;
     return kept(*tok) ? p.E + s : -1;
   };
-  for (int i = t; i < pairs; i += THREADS) {
+  int held_g[kHeld], held_tok[kHeld];  // a thread's first pairs, loaded beside the counts
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    held_g[u] = -1;
+    if (t + u * THREADS < pairs) held_g[u] = pair_of(t + u * THREADS, &held_tok[u]);
+  }
+  for (int i = t; i < G * kWords; i += THREADS) (&L.bits[0][0])[i] = 0;
+  int all;
+  const int mine = t < G ? of.y : 0;
+  const int off = scan256(mine, L.wave_sums, &all);  // (its barrier: the bits are zero)
+  if (t < G) {
+    L.base[t] = off + of.x;
+    if (chunk == 0) {
+      if (p.counts_out) p.counts_out[t] = mine;
+      if (p.offsets_out) p.offsets_out[t] = off;
+    }
+  }
+  if (chunk == 0 && t == 0 && p.offsets_out) p.offsets_out[G] = all;
+  auto mark = [&](int g, int tok) {
+    if (g >= 0) atomicOr(&L.bits[g][tok >> 5], 1u << (tok & 31));
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) mark(held_g[u], held_tok[u]);
+  for (int i = t + kHeld * THREADS; i < pairs; i += THREADS) {
     int tok;
     const int g = pair_of(i, &tok);
-    if (g >= 0) atomicOr(&L.bits[g][tok >> 5], 1u << (tok & 31));
+    mark(g, tok);
   }
   __syncthreads();
   const size_t P = (size_t)p.T * (p.k + p.S), Tk = (size_t)p.T * p.k;
-  for (int i = t; i < pairs; i += THREADS) {
-    int tok;
-    const int g = pair_of(i, &tok);
+  auto put = [&](int i, int g, int tok) {
     const size_t pair = i < routed ? (size_t)t0 * p.k + i : Tk + (size_t)((i - routed) / n) * p.T + t0 + tok;
     int at = -1;
     if (g >= 0) {
@@ -767,6 +777,14 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
       if (p.order) p.order[at] = (int)pair;
     }
     if (p.pos) p.pos[pair] = at;
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u)
+    if (t + u * THREADS < pairs) put(t + u * THREADS, held_g[u], held_tok[u]);
+  for (int i = t + kHeld * THREADS; i < pairs; i += THREADS) {
+    int tok;
+    const int g = pair_of(i, &tok);
+    put(i, g, tok);
   }
   if (p.order)
     for (size_t i = (size_t)all + (size_t)chunk * THREADS + t; i < P; i += (size_t)p.chunks * THREADS) p.order[i] = -1;
@@ -852,8 +870,8 @@ __global__ __launch_bounds__(ONE ? kOneThreads : LANE ? kChunk : kThreads) void 
   auto count = [&](int g) { return g < p.E ? hist[g] : kept; };
   if constexpr (ONE) {
     __shared__ PlaceLds place;
-    place_pairs<kOneThreads>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; }, count,
-                          [](int) { return 0; });
+    place_pairs<kOneThreads>(p, place, 0, [&](int i) { return (int)sel[i]; }, [&](int i) { return !p.mask || p.mask[i] != 0; },
+                             int2{0, t < p.E + p.S ? count(t) : 0});
   } else {
     if (t < p.E + p.S) p.counts[(size_t)blockIdx.x * (p.E + p.S) + t] = count(t);
   }
@@ -883,34 +901,53 @@ __global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(SelectParams
   __shared__ PlaceLds place;
   __shared__ int2 part[FEW ? kPlaceThreads : 1];  // pairs of earlier chunks, of all
   const int chunk = blockIdx.x, t0 = chunk * p.chunk, t = threadIdx.x, G = p.E + p.S;
-  int before = 0, total = 0;  // of group t
+  int2 of{0, 0};  // of group t
   if constexpr (FEW) {
     const int g = t & ((1 << log_groups) - 1), many = kPlaceThreads >> log_groups;
     int2 s{0, 0};
-    if (g < G) {
-#pragma unroll 8
-      for (int c = t >> log_groups; c < p.chunks; c += many) {
-        const int v = p.counts[(size_t)c * G + g];
-        s.x += c < chunk ? v : 0;
-        s.y += v;
+    if (log_groups < 6) {  // a wave's threads of the same group first (131072 of 4 of 13: 16.6 us, 17.3 all through LDS)
+      if (g < G) {
+        for (int c0 = t >> log_groups; c0 < p.chunks; c0 += 8 * many) {
+          int v[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u] = p.counts[min(c0 + u * many, p.chunks - 1) * G + g];  // (below 2^15)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int c = c0 + u * many;
+            s.x += c < chunk ? v[u] : 0;
+            s.y += c < p.chunks ? v[u] : 0;
+          }
+        }
       }
+      for (int o = 1 << log_groups; o < 64; o *= 2) {  // (a wave's threads of the same group)
+        s.x += __shfl_xor(s.x, o, 64);
+        s.y += __shfl_xor(s.y, o, 64);
+      }
+      if ((t & 63) < 1 << log_groups) part[((t >> 6) << log_groups) + (t & 63)] = s;
+    } else {  // (eight loads at once as the compiler arranges them: 16384 of 6 of 64 and 2 13.6 us, 14.4 as above)
+      if (g < G) {
+#pragma unroll 8
+        for (int c = t >> log_groups; c < p.chunks; c += many) {
+          const int v = p.counts[c * G + g];
+          s.x += c < chunk ? v : 0;
+          s.y += v;
+        }
+      }
+      part[t] = s;
     }
-    part[t] = s;
     __syncthreads();
     if (t < G)
-      for (int i = 0; i < many; ++i) {
+      for (int i = 0; i < min(many, kPlaceThreads / 64); ++i) {
         const int2 o = part[(i << log_groups) + t];
-        before += o.x;
-        total += o.y;
+        of.x += o.x;
+        of.y += o.y;
       }
   } else if (t < G) {
-    before = p.counts[(size_t)chunk * G + t];
-    total = p.totals[t];
+    of = int2{p.counts[(size_t)chunk * G + t], p.totals[t]};
   }
   const int32_t* idx = p.idx + (size_t)t0 * p.k;
   place_pairs<kPlaceThreads>(
-      p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; },
-      [&](int) { return total; }, [&](int) { return before; });
+      p, place, chunk, [&](int i) { return (int)idx[i]; }, [&](int i) { return !p.mask || p.mask[t0 + i] != 0; }, of);
 }
 
 // Most tokens of a call in one launch, a workgroup of 64 rows at a time (us, in one against two: 64 of

@@ -15,8 +15,8 @@
 // decides anything.  Counts of all chunks are added up by a launch in between.
 //
 // 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 67 us (151 MB, for which a copy takes
-// 29): 55 for the selection, bound by instructions (some 610 to four rows, the vector units busy 57 %
-// of the time), 6 for the counts, 9 for the order.
+// 29): 54 for the selection, bound by instructions (some 610 to four rows, the vector units busy 57 %
+// of the time), 5 for the counts, 9 for the order.
 #include "fp8_dev.h"
 
 namespace mira {

@@ -8,7 +8,8 @@
 // times the row's largest head is taken.  What is cut off and what fp32 rounds may hide the
 // order of two candidates: where two neighbours of the result, or the groups at the border,
 // lie closer than that (see `delta`), or a lane's best do not suffice, or a logit is NaN, a
-// whole wave does the row again with c in 64 bits.  In long batches of few experts a row is one lane's.
+// whole wave does the row again with c in 64 bits.  In long batches of up to 64 experts a
+// row is one or four lanes'.
 //
 // Order: a chunk of tokens is a workgroup.  Each expert has a bit for every token of the
 // chunk, so a pair's rank in its expert's list is a count of bits: no order of atomics
@@ -693,6 +694,136 @@ __device__ __forceinline__ bool select_lane(const SelectParams& p, int row, bool
   return wide && live;
 }
 
+// Of long batches of 17 to 64 experts and eight selected a row is four lanes', experts 16 i + 4 q + 0 .. 3 of
+// lane q's: each sorts its largest eight, which then meet in twice two, and so all have the row's, and in `next`
+// the ninth.  Comparisons, sums' order and bits are those of select_rows here too.  Lane q has picks q and q + 4.
+constexpr int kQuadMost = 8;
+__device__ __forceinline__ uint32_t of4(int q, uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return q & 2 ? (q & 1 ? d : c) : (q & 1 ? b : a); }
+__device__ __forceinline__ void order_eight(uint32_t* a) {  // of two fours in order
+  const uint32_t t4 = a[4], t5 = a[5];
+  a[4] = a[7];
+  a[5] = a[6];
+  a[6] = t5;
+  a[7] = t4;
+  order_bitonic<8>(a);
+}
+// The largest eight of two eights in order to a, in order; the largest of the others to next.
+__device__ __forceinline__ void meet_eights(uint32_t* a, const uint32_t (&o)[8], uint32_t& next) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    next = max(next, min(a[i], o[7 - i]));
+    a[i] = max(a[i], o[7 - i]);
+  }
+  order_bitonic<8>(a);
+}
+template <int CTRL>
+__device__ __forceinline__ void meet_lanes(uint32_t* a, uint32_t& next) {
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = dpp_u<CTRL>(a[i]);
+  next = max(next, dpp_u<CTRL>(next));
+  meet_eights(a, o, next);
+}
+template <typename T>
+__device__ __forceinline__ bool select_quad(const SelectParams& p, int row, bool live, const float* bias, float bias_max, Pick (&r)[2]) {
+  const int lane = threadIdx.x & 63, q = lane & 3;
+  const T* x = (const T*)p.logits + (size_t)row * p.ld;
+  float v[16], c[16], any = 0.f;
+  if (p.E == 64) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float o[4];
+      load_n(x + 16 * i + 4 * q, o);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[4 * i + j] = o[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = load_act(x, min(16 * (i >> 2) + 4 * q + (i & 3), p.E - 1));
+  }
+  auto expert = [&](int i) { return 16 * (i >> 2) + 4 * q + (i & 3); };
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    any += v[i];
+    v[i] = expert(i) < p.E ? v[i] : -INFINITY;
+  }
+  bool wide = any != any;
+  constexpr float kLog2e = 1.44269502162933349609375f;
+  const float step = fixed_step(bias_max);
+  float m = 0.f, inv_sum = 1.f, top = 1.f;
+  if (p.sigmoid && p.bias) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = fmaf(__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v[i] * -kLog2e)), step, bias[expert(i)]);
+  } else {
+    m = v[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) m = __builtin_amdgcn_fmed3f(m, v[i], INFINITY);
+    m = lanes_reduce<4, MaxOp>(m);
+    wide |= m == INFINITY;
+    m = m == -INFINITY ? 0.f : m;
+    if (!p.sigmoid && (p.bias || !p.renorm)) {
+      float sum[4];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        c[i] = __builtin_amdgcn_exp2f((v[i] - m) * kLog2e);
+        sum[i & 3] = i < 4 ? c[i] : sum[i & 3] + c[i];
+      }
+      const float all = lanes_reduce<4, AddOp>((sum[0] + sum[1]) + (sum[2] + sum[3]));
+      inv_sum = top = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
+    }
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = fmaf(c[i], inv_sum * step, bias[expert(i)]);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = fmaxf(fmaf(v[i] - m, 0x1p19f, 16777215.f), 1.f);
+    }
+  }
+  const int margin = p.bias ? score_margin(p.sigmoid, top, bias_max) : sizeof(T) == 4 ? 4 : -1;
+  uint32_t key[16], next = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t part = p.bias || sizeof(T) == 4 ? (uint32_t)c[i] << 8 : order_key(v[i]) & 0xFFFFFF00u;
+    key[i] = v[i] > -INFINITY && part != 0u ? part | (uint32_t)(255 - expert(i)) : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) sort4(key + i);
+  order_eight(key);
+  order_eight(key + 8);
+  {
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = key[8 + i];
+    meet_eights(key, o, next);
+  }
+  meet_lanes<0xB1>(key, next);  // quad_perm 1,0,3,2
+  meet_lanes<0x4E>(key, next);  // quad_perm 2,3,0,1
+  const uint32_t mine[2] = {of4(q, key[0], key[1], key[2], key[3]), of4(q, key[4], key[5], key[6], key[7])};
+  const uint32_t after[2] = {of4(q, key[1], key[2], key[3], key[4]), of4(q, key[5], key[6], key[7], next)};
+  float of[2], right[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    r[u].e = q + 4 * u < p.k && mine[u] != 0u ? 255 - (int)(mine[u] & 255u) : -1;
+    of[u] = r[u].e >= 0 ? load_act(x, r[u].e) : 0.f;
+  }
+  right[0] = dpp<0x39>(of[0]);  // quad_perm 1,2,3,0
+  right[1] = dpp<0x39>(of[1]);
+  if (q == 3) right[0] = right[1];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    bool order = (int)(mine[u] >> 8) - (int)(after[u] >> 8) > margin;
+    if (!p.bias && q + 4 * u < p.k - 1) order = of[u] > right[u] || (of[u] == right[u] && r[u].e < 255 - (int)(after[u] & 255u));
+    wide |= r[u].e >= 0 && after[u] != 0u && !order;
+    if (!live) r[u].e = -1;
+    r[u].w = r[u].e < 0 ? 0.f : p.sigmoid ? sigmoid(of[u]) : exp_neg(of[u] - m) * inv_sum;
+  }
+  float scale = p.scale;
+  if (p.renorm) scale *= __builtin_amdgcn_rcpf(lanes_reduce<4, AddOp>(r[0].w) + lanes_reduce<4, AddOp>(r[1].w) + kTiny);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) r[u].w = r[u].e < 0 ? 0.f : r[u].w * scale;
+  return (__ballot(wide && live) >> (lane & 60) & 15u) != 0;
+}
+
 // Exclusive sum over threads 0..255 (each its own count; others 0); total in all threads.
 __device__ __forceinline__ int scan256(int v, int* wave_sums, int* total) {
   const int t = threadIdx.x, lane = t & 63;
@@ -791,11 +922,12 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
 }
 
 // A chunk of tokens: a wave takes four rows at a time, then the rows that are to be done again, one by
-// one (within the loop the constants of a 64-bit exp would take the registers of half the waves); or (LANE) a thread a row.
+// one (within the loop the constants of a 64-bit exp would take the registers of half the waves).  LANES of
+// 4 and 1: rows of 4 lanes, or of one.
 // One chunk places its pairs at once (ONE); several leave their counts.
-template <int V, bool ONE, bool LANE, typename T>
-__global__ __launch_bounds__(ONE ? kOneThreads : LANE ? kChunk : kThreads) void route_select_kernel(SelectParams p) {
-  constexpr int kWaves = (ONE ? kOneThreads : LANE ? kChunk : kThreads) / 64;
+template <int V, bool ONE, int LANES, typename T>
+__global__ __launch_bounds__(ONE ? kOneThreads : LANES == 1 ? kChunk : kThreads, LANES == 4 ? 4 : 1) void route_select_kernel(SelectParams p) {
+  constexpr int kWaves = (ONE ? kOneThreads : LANES == 1 ? kChunk : kThreads) / 64;
   __shared__ SelectScratch scr[kWaves];
   __shared__ float bias[MIRA_MAX_EXPERTS];
   __shared__ float wave_max_bias[4];
@@ -826,7 +958,26 @@ __global__ __launch_bounds__(ONE ? kOneThreads : LANE ? kChunk : kThreads) void 
       if (r.e >= 0) atomicAdd(&hist[r.e], 1);
     }
   };
-  if constexpr (LANE) {  // (a chunk has a thread for each of its tokens at most)
+  if constexpr (LANES == 4) {
+    for (int i0 = wave * 16; i0 < n; i0 += kWaves * 16) {
+      const int i = i0 + (lane >> 2), q = lane & 3;
+      const bool in = i < n, live = in && (!p.mask || p.mask[t0 + min(i, n - 1)] != 0);
+      Pick r[2];
+      const bool again = select_quad<T>(p, t0 + min(i, n - 1), live, bias, bias_max, r);
+      if (!in) continue;
+      if (again && q == 0) rows_again[atomicAdd(&n_again, 1)] = (uint8_t)i;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (again || q + 4 * u >= p.k) continue;
+        const size_t at = (size_t)(t0 + i) * p.k + q + 4 * u;
+        p.idx[at] = r[u].e;
+        if (p.weight) p.weight[at] = r[u].w;
+        if (p.place && r[u].e >= 0) atomicAdd(&hist[r[u].e], 1);
+      }
+      if (p.place && live && q == 0) atomicAdd(&kept, 1);
+    }
+  }
+  if constexpr (LANES == 1) {  // (a chunk has a thread for each of its tokens at most)
     if (t < n) {
       const bool live = !p.mask || p.mask[t0 + t] != 0;
       Pick r[kLaneMost];
@@ -845,7 +996,7 @@ __global__ __launch_bounds__(ONE ? kOneThreads : LANE ? kChunk : kThreads) void 
       if (p.place && live) atomicAdd(&kept, 1);
     }
   }
-  for (int i0 = LANE ? n : wave * 4; i0 < n; i0 += kWaves * 4) {
+  for (int i0 = LANES < 16 ? n : wave * 4; i0 < n; i0 += kWaves * 4) {
     const int i = i0 + (lane >> 4);
     const bool live = i < n;
     float v[V];
@@ -964,19 +1115,22 @@ int chunk_count(int T, int E) { return (int)(((int64_t)T + chunk_tokens(T, E) - 
 
 template <int V, typename T>
 void launch_select(const SelectParams& p, hipStream_t st) {
-  launch_timed("route_select", p.chunks == 1 ? route_select_kernel<V, true, false, T> : route_select_kernel<V, false, false, T>, dim3(p.chunks),
+  launch_timed("route_select", p.chunks == 1 ? route_select_kernel<V, true, 16, T> : route_select_kernel<V, false, 16, T>, dim3(p.chunks),
                dim3(p.chunks == 1 ? kOneThreads : kThreads), 0, st, p);
 }
 
-// Tokens from which on rows of few experts are a lane's each (us by 16 lanes and by one: 131072 of 2 of 8 21.3 and 12.5, of 4 of 13
+// Tokens from which on rows of few experts are four lanes' (us by 16 lanes and by four: 131072 of 6 of 64 and 2 33.7 and 27.0, of
+// 8 of 64 bf16 with bias 37.6 and 29.7, 9000 of 6 of 64 and 2 12.8 and 12.1, of 2 of 17 9.0 and 8.7) or one's (by 16 lanes and by one: 131072 of 2 of 8 21.3 and 12.5, of 4 of 13
 // bf16 with bias and mask 25.4 and 17.4; 12000 9.5 and 8.7, 11.9 and 11.8; 8192 8.7 and 9.2, 10.7 and 12.1).
 constexpr int kLaneTokens = 8192;
 
 template <typename T>
 void launch_select_of(const SelectParams& p, hipStream_t st) {
   if (p.E <= 16 && p.k <= kLaneMost && p.groups == 1 && p.T > kLaneTokens)
-    launch_timed("route_select", p.E <= 8 ? route_select_kernel<8, false, true, T> : route_select_kernel<16, false, true, T>, dim3(p.chunks), dim3(kChunk), 0, st,
+    launch_timed("route_select", p.E <= 8 ? route_select_kernel<8, false, 1, T> : route_select_kernel<16, false, 1, T>, dim3(p.chunks), dim3(kChunk), 0, st,
                  p);
+  else if (p.E <= 64 && p.k <= kQuadMost && p.groups == 1 && p.T > kLaneTokens)
+    launch_timed("route_select", route_select_kernel<4, false, 4, T>, dim3(p.chunks), dim3(kThreads), 0, st, p);
   else if (p.E <= 16) launch_select<1, T>(p, st);
   else if (p.E <= 64) launch_select<4, T>(p, st);
   else if (p.E <= 128) launch_select<8, T>(p, st);

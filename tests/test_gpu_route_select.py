@@ -439,7 +439,8 @@ def _few_experts(E, k, name, seed):
     return rng, x
 
 
-@pytest.mark.parametrize("E,k", [(1, 1), (2, 2), (3, 1), (7, 4), (8, 2), (8, 4), (9, 3), (15, 4), (16, 1), (16, 4)])
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 2), (3, 1), (7, 4), (8, 2), (8, 4), (9, 3), (15, 4), (16, 1), (16, 4), (8, 5), (16, 8), (17, 1), (17, 8), (33, 5), (61, 7), (63, 8), (64, 6),
+                                 (64, 8)])
 @pytest.mark.parametrize("sigmoid,renorm,biased,name,pad,shift", [(False, True, False, "f32", 0, 0), (True, True, True, "bf16", 3, 1),
                                                                   (False, False, True, "f32", 1, 1), (True, False, False, "bf16", 0, 0)])
 def test_long_batches_of_few_experts(E, k, sigmoid, renorm, biased, name, pad, shift):
@@ -465,13 +466,14 @@ def test_long_batches_of_few_experts(E, k, sigmoid, renorm, biased, name, pad, s
 
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("biased", [False, True])
-def test_long_batches_special_logits(sigmoid, biased):
+@pytest.mark.parametrize("E,k", [(8, 3), (40, 6)])
+def test_long_batches_special_logits(sigmoid, biased, E, k):
     """NaN and infinities in a long batch of few experts: the selection and weights of a shorter one."""
-    rng, x = _few_experts(8, 3, "f32", 1)
+    rng, x = _few_experts(E, k, "f32", 1)
     x[torch.from_numpy(rng.random(tuple(x.shape)) < 0.02).cuda()] = float("nan")
     x[torch.from_numpy(rng.random(tuple(x.shape)) < 0.02).cuda()] = float("inf")
-    bias = torch.from_numpy(rng.normal(0, 0.1, 8)).float().cuda() if biased else None
-    c, d = Call(x, 3, 0, sigmoid, True, bias).run(), Call(x[:4400], 3, 0, sigmoid, True, bias).run()
+    bias = torch.from_numpy(rng.normal(0, 0.1, E)).float().cuda() if biased else None
+    c, d = Call(x, k, 0, sigmoid, True, bias).run(), Call(x[:4400], k, 0, sigmoid, True, bias).run()
     torch.cuda.synchronize()
     assert torch.equal(c.idx.v[:4400], d.idx.v) and torch.equal(c.w.v[:4400].view(torch.int32), d.w.v.view(torch.int32))
     i = c.outputs()[0]
@@ -479,16 +481,17 @@ def test_long_batches_special_logits(sigmoid, biased):
     for t in range(len(xs)):
         got = i[t][i[t] >= 0]
         assert len(set(got)) == len(got) and not np.isnan(xs[t, got]).any()
-    for got, want in zip(c.outputs()[2:], pairs(i.astype(np.int64), None, 8, 0)):
+    for got, want in zip(c.outputs()[2:], pairs(i.astype(np.int64), None, E, 0)):
         assert np.array_equal(got, want)
     assert all(b.intact() for b in (c.X, c.idx, c.w, c.counts, c.offsets, c.order, c.pos, c.ws))
 
 
 @pytest.mark.parametrize("sigmoid", [False, True])
-def test_long_batches_scores_that_fp32_does_not_tell_apart(sigmoid):
+@pytest.mark.parametrize("E,k", [(16, 4), (64, 8)])
+def test_long_batches_scores_that_fp32_does_not_tell_apart(sigmoid, E, k):
     rng = np.random.default_rng(14)
-    row = np.float32(rng.normal(0, 1.5, 16))
+    row = np.float32(rng.normal(0, 1.5, E))
     bias = torch.from_numpy((0.75 - scores(row[None].astype(np.float64), sigmoid)[0]).astype(np.float32)).cuda()
     x = torch.from_numpy(np.repeat(row[None], 8300, 0)).cuda()
-    x[1::2] += torch.from_numpy(rng.normal(0, 1e-6, (4150, 16)).astype(np.float32)).cuda()
-    Call(x, 4, 0, sigmoid, True, bias).run().check()
+    x[1::2] += torch.from_numpy(rng.normal(0, 1e-6, (4150, E)).astype(np.float32)).cuda()
+    Call(x, k, 0, sigmoid, True, bias).run().check()

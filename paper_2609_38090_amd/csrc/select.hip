@@ -7,7 +7,7 @@
 // index at once and equal values give the lower expert.  A lane sorts its best four or five; k + 1
 // times the row's largest head is taken.  What is cut off and what fp32 rounds may hide the
 // order of two candidates: where two neighbours of the result, or the groups at the border,
-// lie closer than that (see `delta`), or a lane's best do not suffice, or a logit is NaN, a
+// lie closer than that (see score_margin), or a lane's best do not suffice, or a logit is NaN, a
 // whole wave does the row again with c in 64 bits.  In long batches of up to 64 experts a
 // row is one or four lanes'.
 //
@@ -1119,16 +1119,17 @@ void launch_select(const SelectParams& p, hipStream_t st) {
                dim3(p.chunks == 1 ? kOneThreads : kThreads), 0, st, p);
 }
 
-// Tokens from which on rows of few experts are four lanes' (us by 16 lanes and by four: 131072 of 6 of 64 and 2 33.7 and 27.0, of
-// 8 of 64 bf16 with bias 37.6 and 29.7, 9000 of 6 of 64 and 2 12.8 and 12.1, of 2 of 17 9.0 and 8.7) or one's (by 16 lanes and by one: 131072 of 2 of 8 21.3 and 12.5, of 4 of 13
-// bf16 with bias and mask 25.4 and 17.4; 12000 9.5 and 8.7, 11.9 and 11.8; 8192 8.7 and 9.2, 10.7 and 12.1).
+// Tokens from which on rows of up to 64 experts are four lanes' or one's.  us by 16 lanes and by four: 131072 of 6 of 64 and 2 shared
+// 33.7 and 27.0, of 8 of 64 bf16 with bias 37.6 and 29.7, 9000 of 6 of 64 and 2 12.8 and 12.1, of 2 of 17 9.0 and 8.7.
+// By 16 and by one: 131072 of 2 of 8 21.3 and 12.5, of 4 of 13 bf16 with bias and mask 25.4 and 17.4; 12000 9.5 and
+// 8.7, 11.9 and 11.8; 8192 8.7 and 9.2, 10.7 and 12.1.
 constexpr int kLaneTokens = 8192;
 
 template <typename T>
 void launch_select_of(const SelectParams& p, hipStream_t st) {
   if (p.E <= 16 && p.k <= kLaneMost && p.groups == 1 && p.T > kLaneTokens)
-    launch_timed("route_select", p.E <= 8 ? route_select_kernel<8, false, 1, T> : route_select_kernel<16, false, 1, T>, dim3(p.chunks), dim3(kChunk), 0, st,
-                 p);
+    launch_timed("route_select", p.E <= 8 ? route_select_kernel<8, false, 1, T> : route_select_kernel<16, false, 1, T>, dim3(p.chunks),
+                 dim3(kChunk), 0, st, p);
   else if (p.E <= 64 && p.k <= kQuadMost && p.groups == 1 && p.T > kLaneTokens)
     launch_timed("route_select", route_select_kernel<4, false, 4, T>, dim3(p.chunks), dim3(kThreads), 0, st, p);
   else if (p.E <= 16) launch_select<1, T>(p, st);

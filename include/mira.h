@@ -740,7 +740,8 @@ int mira_combine_grad(const mira_combine_grad_args* a, hipStream_t stream);
  *   dgate = dact up s (1 + gate (1 - s)),  dup = dact gate s,
  * side by side as dx, in fp32 and rounded once, and as q and scale (mira_fp8_quantize
  * with block_rows 1 and eps q_eps on the fp32 values, [rows][2 cols]) for the product
- * with the gate and up matrices' transposed copies.  dgate is NaN for infinite gates, and dup for -inf. */
+ * with the gate and up matrices' transposed copies.  dgate is NaN for infinite gates, and dup for -inf.
+ * Below gates of -88.72, where exp(-gate) passes fp32's range, s is 0; products pass it only where results do. */
 typedef struct mira_swiglu_grad_args {
   const void* x;      /* [rows][2 cols] x_dtype */
   const void* dact;   /* [rows][cols] d_dtype */

@@ -27,7 +27,9 @@ struct SwigluGradParams {
 
 // exp(-g) = 2^t with the rounding of t carried along where |t| < 128 (beyond, it is infinite, or
 // nothing beside 1); 4 s = 1 / (1/4 + exp(-g)/4), since the reciprocal instruction gives 0
-// below 2^-126, where s times the rest is still a normal number.
+// below 2^-126, where s times the rest is still a normal number.  s times its factor, 1.1 at most, times the
+// larger of d and u, then the smaller: d u alone may pass fp32's range, or the small one's product with s fall
+// below it, where dgate does not (half of it until the end, since 1.1 times the larger may pass it too).
 __device__ __forceinline__ void swiglu_grad(float g, float u, float d, float* dg, float* du) {
   const float log2e = 1.44269502162933349609375f, rest = 1.92596299112661746887e-8f;
   const float t = -g * log2e;
@@ -36,7 +38,8 @@ __device__ __forceinline__ void swiglu_grad(float g, float u, float d, float* dg
   e = fabsf(t) < 128.f ? fmaf(e, r * 0.693147182464599609375f, e) : e;
   const float s4 = __builtin_amdgcn_rcpf(fmaf(e, 0.25f, 0.25f));
   const float off = e < INFINITY ? e * (s4 * 0.25f) : 1.f;  // 1 - s
-  *dg = (s4 * fmaf(g, off, 1.f)) * 0.25f * (d * u);
+  const bool up = fabsf(u) > fabsf(d);
+  *dg = (s4 * fmaf(g, off, 1.f)) * 0.125f * (up ? u : d) * (up ? d : u) * 2.f;
   *du = g * (s4 * 0.25f) * d;
 }
 

@@ -94,3 +94,43 @@ def test_short_rows(rows, cols):
     """Rows of 16 and 32 lanes and of a wave, several to a workgroup."""
     test_gradient(rows, cols, "bf16", "f32", "dxq", 3, 1)
     test_gradient(rows, cols, "f32", "bf16", "q", 0, 0)
+
+
+@pytest.mark.parametrize("cols", [40, 200, 256, 300, 1001, 16500])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_products_beyond_the_range(cols, name):
+    """dact up alone passes fp32's range, or falls below it, where dgate does not; dx, and blocks of e4m3."""
+    gates = [-100.0, -89.5, -88.0, -80.0, -60.0, -30.0, -3.0, 0.0, 2.5, 50.0]
+    factors = [(1e20, 3e19), (3e38, 2.0), (2.0, -3e38), (1e38, 1e10), (-1e10, 1e38), (1e-25, 3e25), (1e-8, 1e30), (1e30, -1e-8), (1e-30, 1e-20),
+               (2e38, 0.5), (3.3e38, 0.75), (0.0, 3e38), (1e35, 1e25), (2e38, 2e38)]
+    all_of = np.array([(g, d, u) for g in gates for d, u in factors])
+    wg, wu, _ = swiglu_grad(all_of[:, 0], all_of[:, 2], all_of[:, 1])
+    all_of = all_of[(np.abs(wg) < 3e38) & (np.abs(wu) < 3e38)]
+    at = all_of[np.arange(2 * cols).reshape(2, cols) % len(all_of)]
+    assert (np.abs(at[:, :, 1] * at[:, :, 2]) > 3.5e38).any()
+    x = torch.from_numpy(np.concatenate([at[:, :, 0], at[:, :, 2]], 1)).to(dt(name)).cuda()
+    d = torch.from_numpy(at[:, :, 1]).to(dt(name)).cuda()
+    wg, wu, mag = swiglu_grad(f64(x)[:, :cols], f64(x)[:, cols:], f64(d))
+    want = np.concatenate([wg, wu], 1)
+    # s below 2^-126 is nothing: its factors are off by that much
+    lost = 2.0 ** -126 * (f64(x)[:, :cols] < -87)
+    gate, up, dd = f64(x)[:, :cols], f64(x)[:, cols:], f64(d)
+    off = np.concatenate([STEPS * U32 * mag + lost * (1 + np.abs(gate)) * np.abs(up * dd), STEPS * U32 * np.abs(wu) + lost * np.abs(gate * dd)], 1) + 2.0 ** -147
+    nb = -(-2 * cols // 128)
+    dx, dx2, q = torch.empty_like(x), torch.empty_like(x), torch.empty(2, -(-2 * cols // 16) * 16, dtype=torch.uint8, device="cuda")
+    scale = torch.empty(2, nb, device="cuda")
+    base = dict(x=x, dact=d, x_dtype=code(name), d_dtype=code(name), rows=2, cols=cols)
+    mira.mira_swiglu_grad(mira.SwigluGradArgs(dx=dx, **base))
+    mira.mira_swiglu_grad(mira.SwigluGradArgs(dx=dx2, q=q, scale=scale, **base))
+    torch.cuda.synchronize()
+    assert torch.equal(dx, dx2)
+    # bf16 below 2^-126 has steps of 2^-133, of which a rounding is half: 1.4e-41 of these values, for one, is 0 in bf16
+    least = 0.0 if name == "f32" else 2.0 ** -134
+    assert (np.abs(f64(dx) - want) <= off + least + unit(name) * (np.abs(want) + off)).all()
+    full = np.zeros((2, nb * 128))
+    full[:, :2 * cols] = np.abs(want)
+    a = np.maximum(full.reshape(2, nb, 128).max(2), 1e-8) / 448
+    full[:, :2 * cols] = off
+    s = f64(scale)
+    assert (np.abs(s - a) <= 2 * U32 * a + full.reshape(2, nb, 128).max(2) / 448).all()
+    assert e4m3_close(q.cpu().numpy()[:, :2 * cols], scale.cpu().numpy(), want, TABLE, off).all()

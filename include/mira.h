@@ -640,16 +640,16 @@ int mira_route_select(const mira_route_select_args* a, hipStream_t stream);
 /* The gradient of the weights, with the selection held constant: for dweight
  * arriving at topk_weight,
  *   dlogits[t][e] = add[t][e] + sum over j of dweight[t][j] d weight[t][j] / d logits[t][e].
- * Entries of topk_idx outside 0..E-1 count for nothing; a row without others has
- * gradient 0 (plus add) whatever its logits.  So do experts whose logit is -inf.  In a row
- * with other entries a NaN logit, or for softmax +inf, makes the gradients NaN that depend on
+ * Entries of topk_idx outside 0..E-1, and those of experts whose logit is -inf, count for
+ * nothing, whatever their dweight; a row without others has gradient 0 (plus add) whatever
+ * its logits.  In a row with other entries a NaN logit, or for softmax +inf, makes the gradients NaN that depend on
  * it: of all experts for softmax, for sigmoid of that expert if it is selected, and with it
  * of the row's other selected ones where weights are renormalised.  fp32 arithmetic, rounded
  * once. */
 typedef struct mira_route_select_grad_args {
   const void* logits;      /* [T][E] logits_dtype */
   const int32_t* topk_idx; /* [T][k] */
-  const float* dweight;    /* [T][k]; read only where topk_idx selects an expert */
+  const float* dweight;    /* [T][k]; read only where topk_idx is in 0..E-1 */
   const void* add;         /* optional [T][E] logits_dtype: another gradient of the logits
                               (the balance loss's), added; may be dlogits itself (same ld) */
   int32_t logits_dtype;    /* mira_dtype of logits, add and dlogits */

@@ -1238,7 +1238,7 @@ __global__ __launch_bounds__(256) void route_select_grad_kernel(SelectGradParams
       for (int q = 0; q < Q; ++q) load4((const T*)p.add + row * p.ld_add, c + 64 * q, p.E, add[q]);
     }
     if ((uint32_t)sel >= (uint32_t)p.E) sel = -1;
-    const float g = sel >= 0 ? p.dweight[row * p.k + l] : 0.f;
+    float g = sel >= 0 ? p.dweight[row * p.k + l] : 0.f;
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
@@ -1249,12 +1249,20 @@ __global__ __launch_bounds__(256) void route_select_grad_kernel(SelectGradParams
         const float u = load_act(x, sel), e = exp_neg(-fabsf(u)), r = __builtin_amdgcn_rcpf(1.f + e);
         s = u >= 0.f ? r : e * r;
         rest = u >= 0.f ? e * r : r;
-        if (u == -INFINITY) s = 0.f;
+        if (u == -INFINITY) sel = -1, g = s = 0.f;  // (no entry, whatever arrives at it)
       }
       const float A = lanes_reduce<16, AddOp>(g * s), D = lanes_reduce<16, AddOp>(s) + kTiny;
       const float inv = p.renorm ? 1.f / D : 1.f, mean = p.renorm ? A * inv : 0.f;
       spread<0, false, Q>(sel, sel >= 0 ? p.scale * inv * (g - mean) * s * rest : 0.f, p.k, c, o, n);
     } else {
+      // Entries of experts of -inf are none.  Only a wave whose rows have such logits looks which those are (looked up in
+      // every row: 30011 x 61 bf16 7.2 us, 6.8 so).
+      float least[4] = {v[0][0], v[0][1], v[0][2], v[0][3]};  // -inf or NaN, if one of the lane's logits is
+#pragma unroll
+      for (int q = 1; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) least[i] += v[q][i];
+      if (__ballot(!((least[0] + least[1]) + (least[2] + least[3]) > -INFINITY)) && sel >= 0 && load_act(x, sel) == -INFINITY) sel = -1, g = 0.f;
       if (p.renorm) spread<0, true, Q>(sel, g, p.k, c, o, n);
       else spread<0, false, Q>(sel, g, p.k, c, o, n);
       float m = -INFINITY;

@@ -495,3 +495,38 @@ def test_long_batches_scores_that_fp32_does_not_tell_apart(sigmoid, E, k):
     x = torch.from_numpy(np.repeat(row[None], 8300, 0)).cuda()
     x[1::2] += torch.from_numpy(rng.normal(0, 1e-6, (4150, E)).astype(np.float32)).cuda()
     Call(x, k, 0, sigmoid, True, bias).run().check()
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("E", [6, 70, 130, 200])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_gradient_of_masked_experts_counts_for_nothing(sigmoid, renorm, E, name):
+    """Entries of experts of -inf leave the row what it is without them, whatever arrives at them."""
+    rng = np.random.default_rng([E, 5])
+    T, k = 64, 3
+    x = _logits(rng, T, E, name)
+    idx = np.argsort(rng.random((T, E)), 1)[:, :k].astype(np.int32)
+    g = rng.normal(0, 1, (T, k)).astype(np.float32)
+    gone = rng.random((T, k)) < 0.4
+    gone[:8] = True                      # all of the row's entries
+    for t, j in zip(*np.nonzero(gone)):
+        x[t, int(idx[t, j])] = float("-inf")
+    g[gone] = rng.choice(np.float32([np.nan, np.inf, -np.inf, 3e38, 1.0]), gone.sum())
+    free = [int(next(e for e in range(E) if e not in idx[t])) for t in range(8)]
+    for t in range(4):
+        x[t, free[t]] = float("nan") if t % 2 else float("inf")   # a row without other entries: 0 all the same
+    add, d = torch.from_numpy(rng.normal(0, 1, (T, E))).to(x), torch.empty_like(x)
+    flags = (mira.MIRA_ROUTE_SIGMOID if sigmoid else 0) | (mira.MIRA_ROUTE_RENORM if renorm else 0)
+    base = dict(logits=x, topk_idx=torch.from_numpy(idx).cuda(), dweight=torch.from_numpy(g).cuda(), logits_dtype=code(name), n_tokens=T, n_experts=E, top_k=k,
+                flags=flags, dlogits=d)
+    without = np.where(gone, -1, idx)
+    xs = f64(x)
+    xs[:4] = 0.0                         # (no entry: no logit of theirs counts)
+    want, mag = select_grad(xs, without, np.where(gone, 0.0, g.astype(np.float64)), sigmoid, renorm, 1.0)
+    for a in (None, add):
+        mira.mira_route_select_grad(mira.RouteSelectGradArgs(add=a, **base))
+        torch.cuda.synchronize()
+        w, m = (want, mag) if a is None else (want + f64(add), mag + np.abs(f64(add)))
+        off = 2 * STEPS * U32 * m
+        assert (np.abs(f64(d) - w) <= off + unit(name) * (np.abs(w) + off) + 2.0 ** -120).all()

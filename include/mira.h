@@ -591,7 +591,9 @@ int mira_rmsnorm_grad(const mira_rmsnorm_grad_args* a, hipStream_t stream);
  *      s + 1e-20).
  * Ties go to the lower index in both steps.  The selection is that of 64-bit
  * scores (where scores in fp32 do not tell two candidates apart they are computed
- * anew in 64 bits); weights are fp32 arithmetic.
+ * anew in 64 bits, which costs several times as much); weights are fp32 arithmetic.
+ * Biases of magnitudes from about 100 on, of one expert too, leave fp32 few digits of the
+ * scores beside them: switch an expert off by a logit of -inf.
  * An expert whose logit is -inf is never selected; where fewer than top_k remain,
  * the rest of the row's topk_idx is -1 with weight 0, and so is all of a row that
  * the mask drops, whatever its logits.  A row with a NaN logit, or for softmax

@@ -530,3 +530,21 @@ def test_gradient_of_masked_experts_counts_for_nothing(sigmoid, renorm, E, name)
         w, m = (want, mag) if a is None else (want + f64(add), mag + np.abs(f64(add)))
         off = 2 * STEPS * U32 * m
         assert (np.abs(f64(d) - w) <= off + unit(name) * (np.abs(w) + off) + 2.0 ** -120).all()
+
+
+@pytest.mark.parametrize("T,E,k,groups,top,best", [(70, 8, 2, 1, 1, 1), (70, 40, 6, 1, 1, 1), (70, 100, 8, 1, 1, 1), (70, 256, 8, 1, 1, 1), (70, 256, 8, 8, 4, 2),
+                                                   (70, 60, 4, 6, 2, 2), (70, 64, 4, 8, 3, 1), (8300, 8, 2, 1, 1, 1), (8300, 16, 4, 1, 1, 1), (8300, 40, 6, 1, 1, 1)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("biases", ["one at -1e9", "one at 1e4", "all at 1000", "one at 3e38", "all at 3e38", "one at -3.4e38", "both ends"])
+def test_biases_far_apart(T, E, k, groups, top, best, sigmoid, biases):
+    """Biases beside which a score is little or nothing, such as switch an expert off or on: the order is that of 64 bits."""
+    rng = np.random.default_rng([T, E, len(biases)])
+    b = np.float32(rng.normal(0, 0.1, E))
+    at = int(rng.integers(E))
+    if biases == "both ends":
+        b[at], b[(at + 1) % E] = 3.4e38, -3.4e38
+    elif biases.startswith("one"):
+        b[at] = np.float32(biases.split()[-1])
+    else:
+        b = np.float32(float(biases.split()[-1]) + (b if biases.endswith("1000") else 0 * b))
+    Call(_logits(rng, T, E, "f32"), k, 0, sigmoid, True, torch.from_numpy(b).cuda(), None, groups, top, best, 2.5).run().check()

@@ -548,3 +548,16 @@ def test_biases_far_apart(T, E, k, groups, top, best, sigmoid, biases):
     else:
         b = np.float32(float(biases.split()[-1]) + (b if biases.endswith("1000") else 0 * b))
     Call(_logits(rng, T, E, "f32"), k, 0, sigmoid, True, torch.from_numpy(b).cuda(), None, groups, top, best, 2.5).run().check()
+
+
+@pytest.mark.parametrize("T,E,k", [(131072, 255, 8), (131072, 24, 2), (60000, 100, 8)])
+def test_more_chunks_and_pairs_than_one_step_takes(T, E, k):
+    """Counts of chunks over several steps, with a carry and without a launch for them; more pairs in a chunk than its threads keep."""
+    test_many_tokens(T, E, k)
+
+
+@pytest.mark.parametrize("T,E,k,S", [(64, 100, 16, 17), (128, 64, 16, 3), (60, 256, 16, 0), (64, 200, 16, 56), (500, 64, 16, 60)])
+def test_many_pairs_of_few_tokens(T, E, k, S):
+    rng = np.random.default_rng([T, E, k, S])
+    mask = torch.from_numpy((rng.random(T) < 0.8).astype(np.uint8)).cuda()
+    Call(_logits(rng, T, E, "f32"), k, S, True, True, None, mask).run().check()

@@ -192,3 +192,11 @@ def test_far_rows():
     assert torch.equal(out, out2) and torch.equal(dw, dw2) and torch.equal(far[:, 512:512 + cols], dy)
     del far
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,k,S,cols", [(5, 16, 49, 130), (3, 8, 60, 700), (2, 1, 64, 33), (4, 5, 75, 130), (1, 16, 256, 2100), (3, 16, 48, 130)])
+@pytest.mark.parametrize("y,o,pad,shift", [("bf16", "bf16", 0, 0), ("f32", "bf16", 3, 1), ("f32", "f32", 5, 3)])
+def test_more_pairs_than_lanes(T, k, S, cols, y, o, pad, shift):
+    """Tokens of 64 and more pairs, missing ones among all of them."""
+    test_forward(T, k, S, cols, y, o, True, True, pad, shift, 0.3)
+    test_gradient(T, k, S, cols, y, o, "dyqw", True, pad, shift, 0.3)

@@ -246,3 +246,21 @@ def test_far_and_near_rows_side_by_side(cols):
     assert (np.abs(f64(dx)[fine] - gx) <= 3 * 48 * U32 * terms + 1e-37).all()
     assert (np.abs(f64(dw) - gw) <= (48 + 70 + 32) * U32 * wmag).all()
     assert np.isnan(f64(y)[bad, 0]).all() and np.isnan(f64(y)[bad[0]]).all() and (f64(y)[bad[1], 1:] == 0).all()
+
+
+def test_large_calls_repeat_their_bits():
+    rows, cols = 4096, 4096
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, res, dy = (torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(3))
+    w = (1 + 0.1 * torch.randn(cols, generator=g, device="cuda")).bfloat16()
+    nb = mira.mira_rmsnorm_grad_workspace_bytes(rows, cols)
+    ws, out = torch.empty(nb, dtype=torch.uint8, device="cuda"), []
+    for _ in range(3):
+        s, y, dx = (torch.empty_like(x) for _ in range(3))
+        q, scale, dw = torch.empty(rows, cols, dtype=torch.uint8, device="cuda"), torch.empty(rows, cols // 128, device="cuda"), torch.empty(cols, device="cuda")
+        mira.mira_rmsnorm(mira.RmsNormArgs(x=x, residual=res, weight=w, rows=rows, cols=cols, sum=s, y=y, q=q, scale=scale))
+        mira.mira_rmsnorm_grad(mira.RmsNormGradArgs(dy=dy, dsum=res, h=s, weight=w, rows=rows, cols=cols, dx=dx, dweight=dw, workspace=ws, workspace_bytes=nb))
+        out.append((s, y, q, scale, dx, dw))
+    torch.cuda.synchronize()
+    for o in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, out[0]))

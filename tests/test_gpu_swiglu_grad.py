@@ -134,3 +134,16 @@ def test_products_beyond_the_range(cols, name):
     s = f64(scale)
     assert (np.abs(s - a) <= 2 * U32 * a + full.reshape(2, nb, 128).max(2) / 448).all()
     assert e4m3_close(q.cpu().numpy()[:, :2 * cols], scale.cpu().numpy(), want, TABLE, off).all()
+
+
+def test_large_calls_repeat_their_bits():
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for rows, cols in ((8192, 14336), (3000, 13399)):
+        x, d = (torch.randn(rows, n, generator=g, device="cuda").bfloat16() for n in (2 * cols, cols))
+        out = [(torch.empty(rows, -(-2 * cols // 16) * 16, dtype=torch.uint8, device="cuda"), torch.empty(rows, -(-2 * cols // 128), device="cuda"))
+               for _ in range(3)]
+        for q, scale in out:
+            mira.mira_swiglu_grad(mira.SwigluGradArgs(x=x, dact=d, rows=rows, cols=cols, q=q, scale=scale))
+        torch.cuda.synchronize()
+        for q, scale in out[1:]:
+            assert torch.equal(q, out[0][0]) and torch.equal(scale, out[0][1])

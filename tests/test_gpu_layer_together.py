@@ -296,3 +296,39 @@ def test_two_layers_on_two_streams_at_once():
     for lay, w in zip((a, b), want):
         for x, y in zip(w, lay.results()):
             assert torch.equal(x, y)
+
+
+def test_gradients_with_the_router():
+    """The gradient that reaches the norm's input and the router's matrix, the selection's and the balance loss's going through
+    that matrix: the products with it are the caller's.  Bounds as of the whole without it."""
+    lay = Layer(200, 512, 256, 8, 2, 1, 1, 1, False)
+    lay.step()
+    torch.cuda.synchronize()
+    T, R, E = lay.T, lay.R, lay.E
+    without = lay.dx.clone()
+    lay.dy += lay.dlogits @ lay.wr.float()
+    dwr = lay.dlogits.t().contiguous() @ lay.y.float()
+    mira.mira_rmsnorm_grad(lay.norm_grad)
+    torch.cuda.synchronize()
+    x, wn, wr = (t.double().cpu().requires_grad_() for t in (lay.sum, lay.wn, lay.wr))
+    y = x / torch.sqrt((x * x).mean(1, keepdim=True) + EPS) * wn
+    logits = y @ wr.t()
+    sel = torch.sigmoid(logits).gather(1, lay.idx.long().cpu())
+    weight = 2.0 * sel / (sel.sum(1, keepdim=True) + 1e-20)
+    out = x * 1.0
+    for e in range(E + 1):
+        w1, w2 = (dequantize(lay.w[n][0][e], lay.w[n][1][e], 128, r, c).cpu() for n, r, c in (("w1", 2 * R, lay.C), ("w2", lay.C, R)))
+        h = y @ w1.t()
+        o = (torch.nn.functional.silu(h[:, :R]) * h[:, R:]) @ w2.t()
+        share = torch.where(lay.idx.cpu() == e, weight, torch.zeros_like(weight)).sum(1) if e < E else torch.ones(T, dtype=torch.float64)
+        out = out + share[:, None] * o
+    loss = (out * lay.dout.double().cpu()).sum() + (logits * lay.dbal.double().cpu()).sum()
+    gx, gw, gr = torch.autograd.grad(loss, (x, wn, wr))
+
+    def cosine(a, b):
+        a, b = a.double().cpu().reshape(-1), b.double().cpu().reshape(-1)
+        return float((a * b).sum() / (a.norm() * b.norm()))
+
+    res = lay.dout.double().cpu()
+    assert cosine(lay.dx.double().cpu() - res, gx - res) > 0.987 and cosine(lay.dwn, gw) > 0.987 and cosine(dwr, gr) > 0.987
+    assert cosine(lay.dx, gx) > cosine(without, gx)

@@ -547,7 +547,7 @@ int mira_rmsnorm(const mira_rmsnorm_args* a, hipStream_t stream);
  * fp32 arithmetic, sums in a fixed order.  A forward call whose result was quantized
  * takes the gradient that arrives at the product's operand as dy.  Without rows
  * dweight is 0.  Rows whose sum of squares passes fp32's range are scaled first, as in
- * the forward call. */
+ * the forward call; dy w, and a row's sum of h dy w, have to stay inside that range. */
 typedef struct mira_rmsnorm_grad_args {
   const void* dy;     /* [rows][cols] y_dtype */
   const void* dsum;   /* optional [rows][cols] x_dtype */

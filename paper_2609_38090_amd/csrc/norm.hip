@@ -8,7 +8,7 @@
 // two waves on; rows of more than 16384 are read twice.  The gradient of the weight is summed in
 // registers over the rows that a workgroup walks, then over workgroups in order.  4096 x 4096 bf16 with
 // residual, y and e4m3 30 us (151 MB, 5.0 TB/s; a copy of 1 GB reaches 5.2); the gradient of 16384 x 4096
-// 100 us (537 MB, 5.4 TB/s).
+// 102 us (537 MB, 5.3 TB/s).
 #include "fp8_dev.h"
 
 namespace mira {

@@ -16,8 +16,8 @@
 // decides anything.  Counts of all chunks are added up by a launch in between.
 //
 // 131072 x 256 fp32, 8 selected of 4 of 8 groups, sigmoid and bias: 67 us (151 MB, for which a copy takes
-// 29): 54 for the selection, bound by instructions (some 610 to four rows, the vector units busy 57 %
-// of the time), 5 for the counts, 9 for the order.
+// 29): 54 for the selection (some 610 instructions to four rows, in chains: the vector units are busy 57 % of
+// the time at four waves a SIMD, a fifth of LDS cycles are conflicts), 5 for the counts, 9 for the order.
 #include "fp8_dev.h"
 
 namespace mira {
@@ -307,7 +307,7 @@ __device__ __forceinline__ void best_of_pairs(uint32_t* a) {
   a[4] = max(max(a[4], a[5]), max(a[6], a[7]));
 }
 
-// c step + from is 1 for the least c and below 2^24 for the largest.
+// c step + from is 2 (but for roundings, together less than 1) for the least c and below 2^24 for the largest.
 __device__ __forceinline__ float fixed_step(float bias_max) { return 16777210.f / (1.f + 2.f * bias_max); }
 __device__ __forceinline__ float fixed_from(float bias_max) { return fmaf(bias_max, fixed_step(bias_max), 2.f); }
 
@@ -370,7 +370,7 @@ __device__ __forceinline__ Pick select_rows(const SelectParams& p, int row, bool
   }
   const bool holes = !full || __ballot(!(any > -INFINITY)) != 0;
   bool wide = any != any;
-  // Fixed point of what is compared.  c = s + bias from 1 for the least that it can be (bias is held as
+  // Fixed point of what is compared.  c = s + bias from 2 for the least that it can be (bias is held as
   // bias step + from); logits in steps of 2^-19 below the largest, down to 32 below.  Scores: with
   // t = x log2(e) rounded, 2^t is off by |t| half steps and a few; s (1 - s), or a share of the largest,
   // at most 2^-|t|, makes that less than 2^-22 of the largest score's whatever t.  The sum of a softmax
@@ -922,8 +922,9 @@ __device__ __forceinline__ void place_pairs(const SelectParams& p, PlaceLds& L, 
 }
 
 // A chunk of tokens: a wave takes four rows at a time, then the rows that are to be done again, one by
-// one (within the loop the constants of a 64-bit exp would take the registers of half the waves).  LANES of
-// 4 and 1: rows of 4 lanes, or of one.
+// one (within the loop the constants of a 64-bit exp would be held through it).  Registers are one number for the
+// whole kernel: up to 128 experts by 16 lanes and by one it is the 64-bit rows' (93 and 105; 57 to 70 and 38 to 75
+// without them), by four and above 128 experts the loop's.  LANES of 4 and 1: rows of 4 lanes, or of one.
 // One chunk places its pairs at once (ONE); several leave their counts.
 template <int V, bool ONE, int LANES, typename T>
 __global__ __launch_bounds__(ONE ? kOneThreads : LANES == 1 ? kChunk : kThreads, LANES == 4 ? 4 : 1) void route_select_kernel(SelectParams p) {
@@ -1216,9 +1217,9 @@ __device__ __forceinline__ void spread(int sel, float g, int k, int c, float (&s
 //   sigmoid: dl_e = ds_e s_e (1 - s_e), of the selected logits alone;  softmax: dl_e = s_e (ds_e - B), B = sum
 //   ds s, which with renorm is scale (A / D) (1e-20 / D): as a difference of its terms nothing of it
 //   would be left.
-// Bound by its bytes: 131072 x 256 fp32 softmax 69 us for 276 MB, sigmoid 47 us for 147 MB (the selected
-// logits are lines of their own). A row to 64 lanes, one in turn, waited for its loads three
-// times a row (89 and 72 us).
+// 131072 x 256 fp32 softmax 65 us for 276 MB (4.3 TB/s; a copy takes 54: 119 registers leave four waves a SIMD to
+// cover the loads), sigmoid 46 us for 147 MB (the selected logits are lines of their own). A row to 64 lanes, one
+// in turn, waited for its loads three times a row (89 and 72 us).
 template <int Q, typename T>
 __global__ __launch_bounds__(256) void route_select_grad_kernel(SelectGradParams p) {
   const int l = threadIdx.x & 15, c = 4 * l;

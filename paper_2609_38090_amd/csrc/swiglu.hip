@@ -4,7 +4,7 @@
 // read once, eight columns of gate, up and d to a lane, and both results leave from there.
 // Where cols is no multiple of 128, e4m3 blocks do not line up between the halves: a row then
 // belongs to a wave or a workgroup, whose blocks' maxima meet in LDS (maxima do not depend on the
-// order of their atomics).  8192 x 14336 bf16 to e4m3: 167 us (947 MB, 5.7 TB/s).  30000 x 333 bf16 26 us
+// order of their atomics).  8192 x 14336 bf16 to e4m3: 171 us (947 MB, 5.5 TB/s).  30000 x 333 bf16 26 us
 // by rows, 46 by the blocks of each half, which read the three values twice.
 #include "fp8_dev.h"
 
